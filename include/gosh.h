@@ -518,6 +518,87 @@ int gosh_train_parts(const gosh_csr *g_host, float *M_host, int32_t d, int32_t k
                      uint64_t device_budget_bytes, int32_t P_gpu, int32_t S_gpu, int32_t B,
                      int32_t force_K, uint32_t flags, gosh_parts_stats *stats_out);
 
+/* ---- a head on the embedding ------------------------------------------------------------- */
+/* What is trained on the rows of an embedding, or on products of the rows of vertex pairs: layer norm, linear layers
+ * with an activation and a residual, and 8-bit copies of activations kept between the two passes (no passage of the
+ * paper: Sec. 4.1 fits a classifier on such products).  All entry points are asynchronous on the stream, allocate
+ * nothing and give the same bits for the same arguments; a wrong pointer, size or type is GOSH_EINVAL before anything
+ * is launched.  Sums, statistics and accumulators are kept in 32 bits and rounded once, to the type of the output. */
+
+typedef enum { GOSH_F32 = 0, GOSH_BF16 = 1, GOSH_F16 = 2 } gosh_type;
+
+/* Borrowed view of a rows x cols device matrix, entry (r, c) at data[r * ld + c]; ld in elements, ld >= cols.  Rows
+ * need no alignment beyond that of their elements (they are read fastest where data and rows are 16-byte aligned).
+ * 0 <= rows < 2^31 - 1, 1 <= cols <= GOSH_MAT_MAX_COLS, ld <= GOSH_MAT_MAX_LD; data may be NULL if rows = 0.
+ * packed = 0: data holds entries of `type`; exps, ld_exps are ignored.
+ * packed = 1: the 8-bit form of a matrix of `type`.  data holds int8 q, and entry (r, c) stands for
+ * q * 2^(exps[r * ld_exps + c / 32] - 127), or NaN where that byte is 255; ld_exps >= ceil(cols / 32).  The exponent
+ * of a group of 32 columns of a row (the last one of a row may be shorter) is the smallest e for which its largest
+ * magnitude is at most 127 * 2^e, e >= -126 (GOSH_F16: -24, the unit of that type), and q = x / 2^e rounded to the
+ * nearest whole number, ties to even: an error of half a unit at most, 1/127 of the group's largest magnitude or less
+ * above that lowest e.
+ * Every such value is exact in `type`.  Where rounding up would leave the type (a largest magnitude within 1.6 % of
+ * its largest number) q stops at 63 units.  A group with an entry that is not finite in `type` stands for NaN. */
+#define GOSH_MAT_MAX_COLS 65536
+#define GOSH_MAT_MAX_LD 1048576
+typedef struct {
+  void *data;
+  uint8_t *exps;
+  int64_t rows, ld, ld_exps;
+  int32_t cols;
+  int32_t type; /* gosh_type */
+  int32_t packed;
+} gosh_mat;
+
+/* x (not packed) to its 8-bit form q, and q back to x.  Same shape; pack: the same type; unpack: any. */
+int gosh_pack8(const gosh_mat *x, const gosh_mat *q, void *hip_stream);
+int gosh_unpack8(const gosh_mat *q, const gosh_mat *x, void *hip_stream);
+
+/* Layer norm of each row: mean = sum x / cols, rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps), xhat = (x - mean) * rstd,
+ * y = xhat * gamma + beta.  gamma, beta: cols floats.  mean, rstd: rows floats, or NULL.  xhat8, y8: packed matrices
+ * of x's type for the backward pass, or NULL: xhat for gosh_layer_norm_backward, y for the x of a linear layer (both
+ * from the values in 32 bits).  eps >= 0.  y may be x. */
+int gosh_layer_norm(const gosh_mat *x, const float *gamma, const float *beta, float eps, const gosh_mat *y, float *mean,
+                    float *rstd, const gosh_mat *xhat8, const gosh_mat *y8, void *hip_stream);
+
+/* Its gradient: with g = dy * gamma and m(.) the mean over the columns,
+ *   dx = rstd * (g - m(g) - xhat * m(g * xhat)) + add;  dgamma = sum over rows dy * xhat;  dbeta = sum over rows dy.
+ * x: the rows that were normalised, with their mean; or packed, the xhat8 of gosh_layer_norm (mean is ignored then).
+ * add: the gradient that reaches x beside the norm (a residual branch), or NULL.  dx may be dy or add.  dx, or both
+ * dgamma and dbeta, may be NULL.  With rows = 0 dgamma and dbeta are zero.
+ * workspace: device memory of at least gosh_layer_norm_workspace(rows, cols) bytes, 16-byte aligned, that no other
+ * work uses until the call's is done (nothing is kept in it; NULL where that is 0 or dgamma is NULL). */
+int gosh_layer_norm_backward(const gosh_mat *dy, const gosh_mat *x, const float *gamma, const float *mean,
+                             const float *rstd, const gosh_mat *add, const gosh_mat *dx, float *dgamma, float *dbeta,
+                             void *workspace, uint64_t workspace_bytes, void *hip_stream);
+uint64_t gosh_layer_norm_workspace(int64_t rows, int32_t cols);
+
+/* Activations: z; max(z, 0); z * s(2 sqrt(2/pi) (z + 0.044715 z^3)), GELU in its form with tanh; z * s(z).  s is the
+ * logistic function.  The slope of RELU at 0 is 0. */
+#define GOSH_ACT_NONE 0
+#define GOSH_ACT_RELU 1
+#define GOSH_ACT_GELU 2
+#define GOSH_ACT_SILU 3
+
+/* Linear layer: z = x w^T + bias, y = act(z) + residual.  x: rows x in; w: out x in; y: rows x out; all of one type,
+ * not packed.  bias: out floats, or NULL.  residual: as y, or NULL; it may be y itself.  z, y8: what the backward pass
+ * wants, or NULL: z as y, or packed; y8 packed, of y (both from the values in 32 bits).  y must not overlap x or w.
+ * Products are summed in 32 bits; those of GOSH_F32 have the accuracy of 32-bit products.  Not-finite entries reach the
+ * results that they are part of and no others; an infinite one of GOSH_F32 (or one over 3.39e38) may give NaN there. */
+int gosh_linear(const gosh_mat *x, const gosh_mat *w, const float *bias, int32_t act, const gosh_mat *residual,
+                const gosh_mat *y, const gosh_mat *z, const gosh_mat *y8, void *hip_stream);
+
+/* Its gradient: dz = dy * act'(z), dx = dz w, dw = dz^T x, db = sum over rows dz (the residual's gradient is dy).
+ * dy: rows x out.  x: rows x in, or packed.  w: out x in.  z: rows x out, or packed; NULL with GOSH_ACT_NONE.  dx:
+ * rows x in; dw: out x in; db: out floats.  Any of the three may be NULL; w may be NULL if dx is, x if dw is.  All
+ * of one type, but dw may be GOSH_F32.  dz is rounded to that type before the two products, not in db.  With rows = 0
+ * dw and db are zero.  dx must not overlap dy, x, w or z.
+ * workspace: as above, at least gosh_linear_backward_workspace bytes. */
+int gosh_linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, const gosh_mat *z, int32_t act,
+                         const gosh_mat *dx, const gosh_mat *dw, float *db, void *workspace, uint64_t workspace_bytes,
+                         void *hip_stream);
+uint64_t gosh_linear_backward_workspace(int64_t rows, int32_t in, int32_t out, int32_t type, int32_t act);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,6 +23,10 @@ GOSH_FLAG_PAIR_LEVELS = 32
 GOSH_FLAG_CONCURRENT_LAYOUT = 64
 GOSH_EDIVERGED = -5
 GOSH_MAX_DIM = 512
+GOSH_F32, GOSH_BF16, GOSH_F16 = 0, 1, 2
+GOSH_ACT_NONE, GOSH_ACT_RELU, GOSH_ACT_GELU, GOSH_ACT_SILU = 0, 1, 2, 3
+GOSH_MAT_MAX_COLS = 65536
+GOSH_MAT_MAX_LD = 1048576
 GOSH_MAX_NEG = 15
 GOSH_STATIC_MAX_N = 1 << 26
 
@@ -68,6 +72,12 @@ class gosh_placement_info(C.Structure):
                 ("search_ms", C.c_double)]
 
 
+class gosh_mat(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("exps", C.c_void_p), ("rows", C.c_int64), ("ld", C.c_int64),
+                ("ld_exps", C.c_int64), ("cols", C.c_int32), ("type", C.c_int32), ("packed", C.c_int32)]
+
+
+_MAT = C.POINTER(gosh_mat)
 EXPORTS = {
     "gosh_last_error": (C.c_char_p, []),
     "gosh_tuning_defaults": (None, [C.POINTER(gosh_tuning)]),
@@ -131,6 +141,17 @@ EXPORTS = {
     "gosh_matrix_place": (C.c_int, [C.c_int64, C.c_int32, C.c_uint64, C.POINTER(C.c_void_p),
                                     C.POINTER(gosh_placement_info)]),
     "gosh_matrix_release": (C.c_int, [C.c_void_p]),
+    "gosh_pack8": (C.c_int, [_MAT, _MAT, C.c_void_p]),
+    "gosh_unpack8": (C.c_int, [_MAT, _MAT, C.c_void_p]),
+    "gosh_layer_norm": (C.c_int, [_MAT, C.c_void_p, C.c_void_p, C.c_float, _MAT, C.c_void_p, C.c_void_p,
+                                  _MAT, _MAT, C.c_void_p]),
+    "gosh_layer_norm_backward": (C.c_int, [_MAT, _MAT, C.c_void_p, C.c_void_p, C.c_void_p, _MAT, _MAT,
+                                           C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]),
+    "gosh_layer_norm_workspace": (C.c_uint64, [C.c_int64, C.c_int32]),
+    "gosh_linear": (C.c_int, [_MAT, _MAT, C.c_void_p, C.c_int32, _MAT, _MAT, _MAT, _MAT, C.c_void_p]),
+    "gosh_linear_backward": (C.c_int, [_MAT, _MAT, _MAT, _MAT, C.c_int32, _MAT, _MAT, C.c_void_p,
+                                       C.c_void_p, C.c_uint64, C.c_void_p]),
+    "gosh_linear_backward_workspace": (C.c_uint64, [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
 }
 
 _lib = None
@@ -565,3 +586,122 @@ def gosh_train_parts(n: int, xadj: torch.Tensor, adj: torch.Tensor, M_host: torc
     _check(lib().gosh_train_parts(C.byref(g), ptr, d, k_neg, epochs, lr0, seed, level,
                                   device_budget_bytes, P_gpu, S_gpu, B, force_K, flags, C.byref(st)), as_dict)
     return as_dict()
+
+
+# ---- a head on the embedding ---------------------------------------------------------------
+
+_TYPES = {torch.float32: GOSH_F32, torch.bfloat16: GOSH_BF16, torch.float16: GOSH_F16}
+
+
+class Packed8:
+    """The 8-bit form of a rows x cols matrix of `dtype`: int8 entries `q` (rows padded to 16) and one exponent byte for
+    each group of 32 columns, `exps`.  Uninitialised; gosh_pack8, gosh_layer_norm and gosh_linear write it."""
+
+    def __init__(self, rows: int, cols: int, dtype: torch.dtype, device="cuda"):
+        if dtype not in _TYPES:
+            raise TypeError("dtype must be float32, bfloat16 or float16")
+        self.rows, self.cols, self.dtype = rows, cols, dtype
+        self.q = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.int8, device=device)
+        self.exps = torch.empty(rows, -(-cols // 32), dtype=torch.uint8, device=device)
+        self._mat = gosh_mat(self.q.data_ptr() or None, self.exps.data_ptr() or None, rows, self.q.shape[1],
+                             self.exps.shape[1], cols, _TYPES[dtype], 1)
+
+
+def _mat(m, name: str):
+    """A 2-D tensor whose rows are contiguous, or a Packed8, as the library sees it."""
+    if isinstance(m, Packed8):
+        return m._mat
+    if m is None:
+        return None
+    kind = _TYPES.get(m.dtype)
+    if kind is None or m.dim() != 2:
+        raise TypeError(f"{name} must be a 2-D float32, bfloat16 or float16 tensor")
+    rows, cols = m.shape
+    ld, along = m.stride()
+    if along != 1 and cols > 1:
+        raise TypeError(f"{name}: the entries of a row must be contiguous")
+    return gosh_mat(m.data_ptr() or None, None, rows, ld if rows > 1 else max(cols, 1), 0, cols, kind, 0)
+
+
+def _floats(t, name: str, count: int):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != count or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous float32 tensor of {count} entries")
+    return t.data_ptr() or None
+
+
+def _workspace(given, nbytes: int, stream, device):
+    """The caller's uint8 tensor, or a new one that belongs to the stream of the call."""
+    if given is not None:
+        if given.dtype != torch.uint8 or not given.is_contiguous():
+            raise TypeError("workspace must be a contiguous uint8 tensor")
+        return given
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def gosh_pack8(x: torch.Tensor, q: Packed8, stream=None) -> None:
+    _check(lib().gosh_pack8(_mat(x, "x"), _mat(q, "q"), _stream(stream)))
+
+
+def gosh_unpack8(q: Packed8, x: torch.Tensor, stream=None) -> None:
+    _check(lib().gosh_unpack8(_mat(q, "q"), _mat(x, "x"), _stream(stream)))
+
+
+def gosh_layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, y: torch.Tensor, mean=None, rstd=None,
+                    eps: float = 1e-5, xhat8: Packed8 = None, y8: Packed8 = None, stream=None) -> None:
+    """y = layer norm of the rows of x; on request their mean and 1/deviation, and 8-bit forms of the normalised rows
+    (for gosh_layer_norm_backward) and of y (for gosh_linear_backward)."""
+    v = _mat(x, "x")
+    _check(lib().gosh_layer_norm(v, _floats(gamma, "gamma", v.cols), _floats(beta, "beta", v.cols), eps, _mat(y, "y"),
+                                 _floats(mean, "mean", v.rows), _floats(rstd, "rstd", v.rows), _mat(xhat8, "xhat8"),
+                                 _mat(y8, "y8"), _stream(stream)))
+
+
+def gosh_layer_norm_workspace(rows: int, cols: int) -> int:
+    return int(lib().gosh_layer_norm_workspace(rows, cols))
+
+
+def gosh_layer_norm_backward(dy: torch.Tensor, x, gamma: torch.Tensor, mean, rstd: torch.Tensor, dx, dgamma=None,
+                             dbeta=None, add=None, workspace=None, stream=None) -> None:
+    """dx (plus `add`), dgamma and dbeta.  x: the rows that were normalised, with their mean; or the xhat8 of
+    gosh_layer_norm, with mean None."""
+    v = _mat(dy, "dy")
+    nbytes = 0
+    if dgamma is not None:
+        nbytes = gosh_layer_norm_workspace(v.rows, v.cols)
+        workspace = _workspace(workspace, nbytes, stream, dy.device)
+        nbytes = workspace.numel()
+    _check(lib().gosh_layer_norm_backward(v, _mat(x, "x"), _floats(gamma, "gamma", v.cols), _floats(mean, "mean", v.rows),
+                                          _floats(rstd, "rstd", v.rows), _mat(add, "add"), _mat(dx, "dx"),
+                                          _floats(dgamma, "dgamma", v.cols), _floats(dbeta, "dbeta", v.cols),
+                                          workspace.data_ptr() or None if nbytes else None, nbytes, _stream(stream)))
+
+
+def gosh_linear(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, bias=None, act: int = GOSH_ACT_NONE, residual=None,
+                z=None, y8: Packed8 = None, stream=None) -> None:
+    """y = act(x w^T + bias) + residual.  z: a tensor or a Packed8 that receives x w^T + bias; y8: y in 8 bits."""
+    v = _mat(w, "w")
+    _check(lib().gosh_linear(_mat(x, "x"), v, _floats(bias, "bias", v.rows), act, _mat(residual, "residual"), _mat(y, "y"),
+                             _mat(z, "z"), _mat(y8, "y8"), _stream(stream)))
+
+
+def gosh_linear_backward_workspace(rows: int, in_: int, out: int, type_: int, act: int) -> int:
+    return int(lib().gosh_linear_backward_workspace(rows, in_, out, type_, act))
+
+
+def gosh_linear_backward(dy: torch.Tensor, x, w, z, act: int = GOSH_ACT_NONE, dx=None, dw=None, db=None, workspace=None,
+                         stream=None) -> None:
+    """dx, dw and db (those that are given) of gosh_linear; x and z: tensors or Packed8."""
+    v = _mat(dy, "dy")
+    into = dx if dx is not None else dw
+    cols = into.shape[1] if into is not None else 1
+    workspace = _workspace(workspace, gosh_linear_backward_workspace(v.rows, cols, v.cols, v.type, act), stream, dy.device)
+    _check(lib().gosh_linear_backward(v, _mat(x, "x"), _mat(w, "w"), _mat(z, "z"), act, _mat(dx, "dx"), _mat(dw, "dw"),
+                                      _floats(db, "db", v.cols), workspace.data_ptr() or None, workspace.numel(),
+                                      _stream(stream)))

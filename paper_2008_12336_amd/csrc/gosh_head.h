@@ -1,0 +1,279 @@
+// Shared by the units of the head (layer norm, linear layers, 8-bit activations): views of matrices, their checks,
+// the element types and the 8-bit form.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "gosh_common.h"
+
+namespace gosh {
+
+// ---- host: arguments --------------------------------------------------------------------
+
+enum MatUse : int { kMayBePacked = 1, kMustBePacked = 2, kOptional = 4 };
+
+// A matrix argument: its fields, and that its memory is there.  GOSH_OK also for an optional one that is null.
+int check_mat(const gosh_mat *m, const char *what, int use = 0);
+// Two matrices of one shape, or GOSH_EINVAL.
+int check_shape(const gosh_mat *m, const char *what, int64_t rows, int32_t cols);
+int check_type(const gosh_mat *m, const char *what, int32_t type);
+int check_floats(const float *p, int64_t count, const char *what, bool optional);
+int check_workspace(const void *p, uint64_t have, uint64_t need);
+// Sums `parts` arrays of n floats, each `stride` floats after the one before, in ascending order within fixed groups
+// (the same bits every time), into out (float, or `type`), n = rows x cols with rows of ld entries.
+int join_parts(const float *parts, int count, int64_t stride, int64_t rows, int32_t cols, void *out, int64_t ld,
+               int32_t type, hipStream_t st);
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// ---- device: element types --------------------------------------------------------------
+
+typedef float F4 __attribute__((ext_vector_type(4)));
+typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+typedef uint32_t U2 __attribute__((ext_vector_type(2)));
+
+struct F32 {
+  typedef float Store;
+  static constexpr int32_t kType = GOSH_F32;
+  static __device__ __forceinline__ float up(float v) { return v; }
+  static __device__ __forceinline__ float down(float v) { return v; }
+};
+struct Bf16 {
+  typedef __bf16 Store;
+  static constexpr int32_t kType = GOSH_BF16;
+  static __device__ __forceinline__ float up(__bf16 v) { return static_cast<float>(v); }
+  static __device__ __forceinline__ __bf16 down(float v) { return static_cast<__bf16>(v); }
+};
+struct F16 {
+  typedef _Float16 Store;
+  static constexpr int32_t kType = GOSH_F16;
+  static __device__ __forceinline__ float up(_Float16 v) { return static_cast<float>(v); }
+  static __device__ __forceinline__ _Float16 down(float v) { return static_cast<_Float16>(v); }
+};
+
+// N entries in a row of memory that is aligned to one of them only: the hardware takes 128-bit accesses at any
+// multiple of an entry's size, so there is no second path for odd strides.
+template <typename T, int N>
+struct Entries {
+  typedef typename T::Store S;
+  typedef S Vec __attribute__((ext_vector_type(N)));
+  typedef Vec Loose __attribute__((aligned(sizeof(S))));
+  // The first `count` of N; the others are zero.
+  static __device__ __forceinline__ void load(const S *p, int count, float (&v)[N]) {
+    if (count >= N) {
+      const Vec x = *reinterpret_cast<const Loose *>(p);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = T::up(x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = i < count ? T::up(p[i]) : 0.f;
+    }
+  }
+  static __device__ __forceinline__ void store(S *p, int count, const float (&v)[N]) {
+    if (count >= N) {
+      Vec x;
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = T::down(v[i]);
+      *reinterpret_cast<Loose *>(p) = x;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (i < count) p[i] = T::down(v[i]);
+    }
+  }
+};
+
+// ---- device: the 8-bit form -------------------------------------------------------------
+
+constexpr int kGroup = 32;          // columns that share an exponent
+constexpr uint32_t kNotFinite = 255;
+
+// The exponent byte of a group whose largest magnitude has the bits `most`: with that magnitude = f * 2^E, f in [1, 2),
+// the smallest e with 64 f <= 127 * 2^(e + 6 - E) is E - 6, or E - 5 from f > 127/64 on, which the carry decides.
+template <typename T>
+__device__ __forceinline__ uint32_t exponent_byte(uint32_t most) {
+  // what rounds to infinity in T, and infinities and NaN themselves
+  constexpr uint32_t too_big = T::kType == GOSH_F32 ? 0x7f800000u : T::kType == GOSH_BF16 ? 0x7f7f8000u : 0x477ff000u;
+  constexpr uint32_t low = T::kType == GOSH_F16 ? 127 - 24 : 1;
+  if (most >= too_big) return kNotFinite;
+  const uint32_t e = (most + 0x1ffffu) >> 23;
+  return e < low + 6 ? low : e - 6;
+}
+
+// 2^(byte - 127); byte 1 to 254.
+__device__ __forceinline__ float unit_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+// What an entry of a group is multiplied by: NaN for one that stands for NaN.
+__device__ __forceinline__ float read_unit(uint32_t byte) {
+  return byte == kNotFinite ? __uint_as_float(0x7fc00000u) : unit_of(byte);
+}
+// 2^(127 - byte).
+__device__ __forceinline__ float inverse_unit(uint32_t byte) {
+  return byte <= 253 ? __uint_as_float((254 - byte) << 23) : 0.f;
+}
+// The unit at which 64 of them leave T.
+template <typename T>
+__device__ __forceinline__ float top_of(uint32_t byte) {
+  constexpr uint32_t top = T::kType == GOSH_F16 ? 137 : 249;
+  return byte >= top ? 63.f : 127.f;
+}
+
+// N entries' q as bytes of words, from entries in 32 bits.  inv = inverse_unit, top = top_of.
+template <int N>
+__device__ __forceinline__ void quantise(const float (&v)[N], uint32_t byte, float top, uint32_t (&q)[N / 4]) {
+  const float inv = inverse_unit(byte);
+#pragma unroll
+  for (int w = 0; w < N / 4; ++w) {
+    q[w] = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = byte == kNotFinite ? 0.f : rintf(v[4 * w + i] * inv);
+      const int n = static_cast<int>(fminf(fmaxf(x, -top), top));
+      q[w] |= (static_cast<uint32_t>(n) & 255u) << (8 * i);
+    }
+  }
+}
+
+// The largest magnitude, as bits, of N entries and of those of the other lanes of a group of `lanes` (1 to 8).
+// Bits order as magnitudes do, with infinity and then NaN on top, where a comparison of floats would drop a NaN.
+template <int N>
+__device__ __forceinline__ uint32_t most_bits(const float (&v)[N], int lanes) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+  for (int s = 1; s < lanes; s *= 2) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), s)));
+  return most;
+}
+
+// count of N bytes at p (any alignment).
+template <int N>
+__device__ __forceinline__ void store_bytes(int8_t *p, int count, const uint32_t (&q)[N / 4]) {
+  typedef uint32_t W __attribute__((ext_vector_type(N / 4)));
+  typedef W Loose __attribute__((aligned(1)));
+  if (count >= N) {
+    W w;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) w[i] = q[i];
+    *reinterpret_cast<Loose *>(p) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < count) p[i] = static_cast<int8_t>(q[i / 4] >> (8 * (i % 4)));
+  }
+}
+template <int N>
+__device__ __forceinline__ void load_bytes(const int8_t *p, int count, uint32_t (&q)[N / 4]) {
+  typedef uint32_t W __attribute__((ext_vector_type(N / 4)));
+  typedef W Loose __attribute__((aligned(1)));
+  if (count >= N) {
+    const W w = *reinterpret_cast<const Loose *>(p);
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) q[i] = w[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) q[i] = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < count) q[i / 4] |= static_cast<uint32_t>(static_cast<uint8_t>(p[i])) << (8 * (i % 4));
+  }
+}
+template <int N>
+__device__ __forceinline__ void widen(const uint32_t (&q)[N / 4], float unit, float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    v[i] = static_cast<float>(static_cast<int32_t>(q[i / 4] << (24 - 8 * (i % 4))) >> 24) * unit;
+}
+
+// A matrix as a kernel sees it.
+struct Plane {
+  void *data;
+  uint8_t *exps;
+  int64_t ld, ld_exps;
+};
+inline Plane plane_of(const gosh_mat *m) {
+  return m == nullptr ? Plane{nullptr, nullptr, 0, 0} : Plane{m->data, m->exps, m->ld, m->ld_exps};
+}
+inline Plane rows_from(Plane p, int64_t row, int32_t type, bool packed) {
+  if (p.data == nullptr) return p;
+  p.data = static_cast<char *>(p.data) + row * p.ld * (packed ? 1 : type == GOSH_F32 ? 4 : 2);
+  if (packed) p.exps += row * p.ld_exps;
+  return p;
+}
+
+// N entries at (row, col), of which `count` are there, from a matrix that may be packed.
+template <typename T, int N>
+__device__ __forceinline__ void load_entries(const Plane &m, bool packed, int64_t row, int col, int count, float (&v)[N]) {
+  if (packed) {
+    uint32_t q[N / 4];
+    load_bytes<N>(static_cast<const int8_t *>(m.data) + row * m.ld + col, count, q);
+    widen<N>(q, count > 0 ? read_unit(m.exps[row * m.ld_exps + col / kGroup]) : 0.f, v);
+  } else {
+    Entries<T, N>::load(static_cast<const typename T::Store *>(m.data) + row * m.ld + col, count, v);
+  }
+}
+
+// N entries at (row, col) into a packed matrix, by the lanes of a group together: kGroup / N of them, or fewer where
+// `lanes` says so, hold a group's columns.  Entries past `count` are zero.  Every lane of the group calls it.
+template <typename T, int N>
+__device__ __forceinline__ void store_packed(const Plane &m, int64_t row, int col, int count, const float (&v)[N],
+                                             bool first_of_group, int lanes) {
+  const uint32_t byte = exponent_byte<T>(most_bits<N>(v, lanes));
+  if (count <= 0) return;
+  uint32_t q[N / 4];
+  quantise<N>(v, byte, top_of<T>(byte), q);
+  store_bytes<N>(static_cast<int8_t *>(m.data) + row * m.ld + col, count, q);
+  if (first_of_group) m.exps[row * m.ld_exps + col / kGroup] = static_cast<uint8_t>(byte);
+}
+
+// ---- device: activations ----------------------------------------------------------------
+
+template <int Act>
+struct Activation;
+
+__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
+
+template <>
+struct Activation<GOSH_ACT_NONE> {
+  static __device__ __forceinline__ float value(float z) { return z; }
+  static __device__ __forceinline__ float slope(float) { return 1.f; }
+};
+template <>
+struct Activation<GOSH_ACT_RELU> {  // a NaN stays one
+  static __device__ __forceinline__ float value(float z) { return z <= 0.f ? 0.f : z; }
+  static __device__ __forceinline__ float slope(float z) { return z <= 0.f ? 0.f : z != z ? z : 1.f; }
+};
+template <>
+struct Activation<GOSH_ACT_SILU> {
+  static __device__ __forceinline__ float value(float z) { return z * logistic(z); }
+  // beyond +-88 the slope is 1 or 0 to the last bit, and an infinity times the zero of s (1 - s) would be NaN
+  static __device__ __forceinline__ float slope(float z) {
+    z = z > 88.f ? 88.f : z < -88.f ? -88.f : z;
+    const float s = logistic(z);
+    return s + z * s * (1.f - s);
+  }
+};
+template <>
+struct Activation<GOSH_ACT_GELU> {
+  static constexpr float kC = 1.5957691216057308f;             // 2 sqrt(2/pi)
+  static constexpr float kD = 1.5957691216057308f * 0.044715f;
+  static __device__ __forceinline__ float value(float z) { return z * logistic(z * (kC + kD * z * z)); }
+  static __device__ __forceinline__ float slope(float z) {
+    z = z > 12.f ? 12.f : z < -12.f ? -12.f : z;  // as above
+    const float s = logistic(z * (kC + kD * z * z));
+    return s + z * s * (1.f - s) * (kC + 3.f * kD * z * z);
+  }
+};
+
+// Calls f with the activation as a type: the branch is taken once, outside the loops.
+template <typename F>
+__device__ __forceinline__ void with_activation(int act, F f) {
+  switch (act) {
+    case GOSH_ACT_RELU: f(Activation<GOSH_ACT_RELU>{}); break;
+    case GOSH_ACT_GELU: f(Activation<GOSH_ACT_GELU>{}); break;
+    case GOSH_ACT_SILU: f(Activation<GOSH_ACT_SILU>{}); break;
+    default: f(Activation<GOSH_ACT_NONE>{}); break;
+  }
+}
+
+}  // namespace gosh

@@ -1,0 +1,336 @@
+// Linear layers: gosh_linear and gosh_linear_backward.  The products of many rows are gosh_product.h's; here are those
+// of a few rows, and the gradient of the activation.
+#include <algorithm>
+
+#include "gosh_product.h"
+
+namespace gosh {
+namespace {
+
+// ---- a few rows -----------------------------------------------------------------------------
+
+constexpr int kFewRows = 8;   // rows up to which a call reads w once at the rate of memory instead of filling tiles
+constexpr int kFewCols = 2;   // rows of w a wavefront takes together
+
+// y = act(x w^T + bias) + residual for R rows: every lane has 8 (16-bit) or 4 entries of a row of w at a time, and its
+// wavefront sums the lanes' products.
+template <typename T, int R>
+__global__ __launch_bounds__(256) void few_rows_kernel(const Plane x, const Plane w, const ForwardOut f, int rows, int n, int k) {
+  constexpr int E = T::kType == GOSH_F32 ? 4 : 8;
+  typedef typename T::Store S;
+  const int wave = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x & 63;
+  const int col = wave * kFewCols;
+  if (col >= n) return;
+  float acc[kFewCols][R];
+#pragma unroll
+  for (int c = 0; c < kFewCols; ++c)
+#pragma unroll
+    for (int r = 0; r < R; ++r) acc[c][r] = 0.f;
+  for (int k0 = lane * E; k0 < k; k0 += 64 * E) {
+    const int count = k - k0;
+    float wv[kFewCols][E];
+#pragma unroll
+    for (int c = 0; c < kFewCols; ++c)
+      Entries<T, E>::load(static_cast<const S *>(w.data) + (col + c < n ? col + c : col) * w.ld + k0, count, wv[c]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float xv[E];
+      Entries<T, E>::load(static_cast<const S *>(x.data) + (r < rows ? r : 0) * x.ld + k0, count, xv);
+#pragma unroll
+      for (int c = 0; c < kFewCols; ++c)
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[c][r] = fmaf(wv[c][e], xv[e], acc[c][r]);
+    }
+  }
+  float v = 0.f;
+#pragma unroll
+  for (int c = 0; c < kFewCols; ++c)
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float sum = acc[c][r];
+#pragma unroll
+      for (int s = 32; s > 0; s /= 2) sum += __shfl_xor(sum, s);
+      if (lane == c * R + r) v = sum;
+    }
+  const int r = lane % R, to = col + lane / R;
+  if (lane >= kFewCols * R || r >= rows || to >= n) return;
+  if (f.bias != nullptr) v += f.bias[to];
+  if (f.z.data != nullptr) static_cast<S *>(f.z.data)[r * f.z.ld + to] = T::down(v);
+  with_activation(f.act, [&](auto a) { v = decltype(a)::value(v); });
+  if (f.residual.data != nullptr) v += T::up(static_cast<const S *>(f.residual.data)[r * f.residual.ld + to]);
+  static_cast<S *>(f.y.data)[r * f.y.ld + to] = T::down(v);
+}
+
+template <typename T>
+int launch_few_rows(const gosh_mat *x, const gosh_mat *w, const ForwardOut &f, hipStream_t st) {
+  const int rows = static_cast<int>(x->rows), n = static_cast<int>(w->rows), k = x->cols;
+  const dim3 grid(static_cast<unsigned>(ceil_div(n, 4 * kFewCols))), block(256);
+  const Plane xp = plane_of(x), wp = plane_of(w);
+  if (rows == 1) few_rows_kernel<T, 1><<<grid, block, 0, st>>>(xp, wp, f, rows, n, k);
+  else if (rows == 2) few_rows_kernel<T, 2><<<grid, block, 0, st>>>(xp, wp, f, rows, n, k);
+  else if (rows <= 4) few_rows_kernel<T, 4><<<grid, block, 0, st>>>(xp, wp, f, rows, n, k);
+  else few_rows_kernel<T, 8><<<grid, block, 0, st>>>(xp, wp, f, rows, n, k);
+  return check_launch("linear layer of a few rows");
+}
+
+// ---- tiles ------------------------------------------------------------------------------------
+
+constexpr int64_t kTilesPerLaunch = int64_t{1} << 22;  // a grid's threads stay below 2^31
+
+// Tiles of 128 x 128 once they fill the device's 256 CUs, of 64 x 64 before.
+bool small_tiles(int64_t M, int64_t N) { return ceil_div(M, 128) * ceil_div(N, 128) < 256; }
+
+template <typename T>
+int product_of_rows(ProductKind kind, ProductArgs g, int64_t rows, hipStream_t st) {
+  const bool small = small_tiles(rows, g.N);
+  const int64_t side = small ? 64 : 128;
+  g.tiles_n = static_cast<int32_t>(ceil_div(g.N, side));
+  g.splits = 1;
+  g.k_per_split = ceil_div(g.K, product_depth(T::kType, small)) * product_depth(T::kType, small);
+  const int64_t rows_per_launch = kTilesPerLaunch / g.tiles_n * side;
+  const ProductArgs all = g;
+  for (int64_t r = 0; r < rows; r += rows_per_launch) {
+    g.M = std::min(rows_per_launch, rows - r);
+    g.tiles_m = static_cast<int32_t>(ceil_div(g.M, side));
+    g.a = rows_from(all.a, r, T::kType, false);
+    g.out = rows_from(all.out, r, T::kType, false);
+    g.forward.residual = rows_from(all.forward.residual, r, T::kType, false);
+    g.forward.y = rows_from(all.forward.y, r, T::kType, false);
+    g.forward.z = rows_from(all.forward.z, r, T::kType, all.forward.z_packed != 0);
+    g.forward.y8 = rows_from(all.forward.y8, r, T::kType, true);
+    if (int rc = launch_product<T>(kind, small, g, st)) return rc;
+  }
+  return GOSH_OK;
+}
+
+// How dw is split along the rows: enough workgroups for two on every CU, at least 8 steps each.
+struct DwPlan {
+  bool small;
+  int32_t tiles_m, tiles_n, splits;
+  int64_t k_per_split;
+};
+DwPlan plan_dw(int64_t rows, int32_t in, int32_t out, int32_t type) {
+  DwPlan p;
+  p.small = std::min(in, out) <= 64;
+  const int side = p.small ? 64 : 128, depth = product_depth(type, p.small);
+  p.tiles_m = static_cast<int32_t>(ceil_div(out, side));
+  p.tiles_n = static_cast<int32_t>(ceil_div(in, side));
+  const int64_t tiles = static_cast<int64_t>(p.tiles_m) * p.tiles_n;
+  const int64_t most = std::max<int64_t>(1, rows / (8 * depth));
+  const int64_t want = std::min(most, std::max<int64_t>(1, 512 / tiles));
+  p.k_per_split = ceil_div(ceil_div(std::max<int64_t>(rows, 1), want), depth) * depth;
+  p.splits = static_cast<int32_t>(ceil_div(rows, p.k_per_split));
+  return p;
+}
+
+// ---- the activation's gradient ------------------------------------------------------------------
+
+// dz = dy * act'(z) and its sums over rows.  A lane has 8 columns; 2^shift lanes lie along a row, the others of the
+// workgroup on rows of their own.  parts: gridDim.y x n sums.
+template <typename T>
+__global__ __launch_bounds__(256) void slope_kernel(const Plane dy, const Plane z, bool z_packed, int act, const Plane dz,
+                                                    float *parts, int64_t rows, int n, int shift, int64_t rows_per_block) {
+  __shared__ float lds[256][8];
+  const int along = threadIdx.x & ((1 << shift) - 1), step = 256 >> shift;
+  const int col = (static_cast<int>(blockIdx.x) << shift) * 8 + along * 8;
+  const int count = n - col < 8 ? n - col : 8;
+  const int64_t r0 = blockIdx.y * rows_per_block, r1 = r0 + rows_per_block < rows ? r0 + rows_per_block : rows;
+  float sum[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+  if (count > 0) {
+    with_activation(act, [&](auto a) {
+      typedef decltype(a) A;
+      for (int64_t r = r0 + (threadIdx.x >> shift); r < r1; r += step) {
+        float g[8], s[8];
+        Entries<T, 8>::load(static_cast<const typename T::Store *>(dy.data) + r * dy.ld + col, count, g);
+        if (z.data != nullptr) {
+          load_entries<T, 8>(z, z_packed, r, col, count, s);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) g[e] *= A::slope(s[e]);
+        }
+        if (dz.data != nullptr) Entries<T, 8>::store(static_cast<typename T::Store *>(dz.data) + r * dz.ld + col, count, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += g[e];
+      }
+    });
+  }
+  if (parts == nullptr) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) lds[threadIdx.x][e] = sum[e];
+  __syncthreads();
+  if (threadIdx.x >> shift != 0 || count <= 0) return;
+  for (int s = 1; s < step; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += lds[(s << shift) + along][e];
+  Entries<F32, 8>::store(parts + static_cast<int64_t>(blockIdx.y) * n + col, count, sum);
+}
+
+struct SlopePlan {
+  int shift;
+  unsigned blocks_x, blocks_y;
+  int64_t rows_per_block;
+};
+SlopePlan plan_slope(int64_t rows, int32_t n) {
+  SlopePlan p;
+  p.shift = 0;
+  while (p.shift < 6 && (8 << p.shift) < n) ++p.shift;
+  p.blocks_x = static_cast<unsigned>(ceil_div(n, 8 << p.shift));
+  const int64_t step = 256 >> p.shift;
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 4 * step), ceil_div(2048, p.blocks_x)));
+  p.rows_per_block = ceil_div(ceil_div(std::max<int64_t>(rows, 1), want), step) * step;
+  p.blocks_y = static_cast<unsigned>(ceil_div(rows, p.rows_per_block));
+  return p;
+}
+
+uint64_t round_up(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+struct BackwardPlan {
+  DwPlan dw;
+  SlopePlan slope;
+  int64_t dz_ld;
+  uint64_t dz, dw_parts, db_parts, bytes;  // offsets, and the whole
+};
+BackwardPlan plan_backward(int64_t rows, int32_t in, int32_t out, int32_t type, int32_t act) {
+  BackwardPlan p;
+  p.dw = plan_dw(rows, in, out, type);
+  p.slope = plan_slope(rows, out);
+  p.dz_ld = (out + 7) / 8 * 8;
+  p.dz = 0;
+  p.dw_parts = act == GOSH_ACT_NONE ? 0 : round_up(static_cast<uint64_t>(rows) * p.dz_ld * (type == GOSH_F32 ? 4 : 2));
+  p.db_parts = p.dw_parts + round_up(static_cast<uint64_t>(p.dw.splits) * in * out * 4);
+  p.bytes = p.db_parts + round_up(static_cast<uint64_t>(p.slope.blocks_y) * out * 4);
+  return p;
+}
+
+template <typename T>
+int linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, const gosh_mat *z, int32_t act,
+                    const gosh_mat *dx, const gosh_mat *dw, float *db, void *workspace, int32_t in, int32_t out,
+                    hipStream_t st) {
+  const int64_t rows = dy->rows;
+  const BackwardPlan p = plan_backward(rows, in, out, T::kType, act);
+  char *const ws = static_cast<char *>(workspace);
+  float *const dw_parts = reinterpret_cast<float *>(ws + p.dw_parts), *const db_parts = reinterpret_cast<float *>(ws + p.db_parts);
+  Plane dz = plane_of(dy);
+  if (rows > 0 && (db != nullptr || act != GOSH_ACT_NONE)) {
+    Plane to{nullptr, nullptr, 0, 0};
+    if (act != GOSH_ACT_NONE && (dx != nullptr || dw != nullptr)) dz = to = Plane{ws + p.dz, nullptr, p.dz_ld, 0};
+    slope_kernel<T><<<dim3(p.slope.blocks_x, p.slope.blocks_y), dim3(256), 0, st>>>(
+        plane_of(dy), act == GOSH_ACT_NONE ? Plane{nullptr, nullptr, 0, 0} : plane_of(z), z != nullptr && z->packed, act, to,
+        db != nullptr ? db_parts : nullptr, rows, out, p.slope.shift, p.slope.rows_per_block);
+    if (int rc = check_launch("gradient of the activation")) return rc;
+  }
+  if (db != nullptr)
+    if (int rc = join_parts(db_parts, static_cast<int>(p.slope.blocks_y), out, 1, out, db, out, GOSH_F32, st)) return rc;
+  if (dx != nullptr && rows > 0) {
+    ProductArgs g{};
+    g.a = dz;
+    g.b = plane_of(w);
+    g.N = in;
+    g.K = out;
+    g.out = plane_of(dx);
+    if (int rc = product_of_rows<T>(kProductDx, g, rows, st)) return rc;
+  }
+  if (dw != nullptr) {
+    if (rows > 0) {
+      ProductArgs g{};
+      g.a = dz;
+      g.b = plane_of(x);
+      g.M = out;
+      g.N = in;
+      g.K = rows;
+      g.k_per_split = p.dw.k_per_split;
+      g.tiles_m = p.dw.tiles_m;
+      g.tiles_n = p.dw.tiles_n;
+      g.splits = p.dw.splits;
+      g.parts = dw_parts;
+      if (int rc = launch_product<T>(x->packed ? kProductDwPacked : kProductDw, p.dw.small, g, st)) return rc;
+    }
+    if (int rc = join_parts(dw_parts, p.dw.splits, static_cast<int64_t>(out) * in, out, in, dw->data, dw->ld, dw->type, st)) return rc;
+  }
+  return GOSH_OK;
+}
+
+}  // namespace
+}  // namespace gosh
+
+extern "C" {
+
+int gosh_linear(const gosh_mat *x, const gosh_mat *w, const float *bias, int32_t act, const gosh_mat *residual,
+                const gosh_mat *y, const gosh_mat *z, const gosh_mat *y8, void *hip_stream) {
+  using namespace gosh;
+  if (int rc = check_mat(x, "x")) return rc;
+  if (int rc = check_mat(w, "w")) return rc;
+  if (int rc = check_mat(y, "y")) return rc;
+  if (int rc = check_mat(residual, "residual", kOptional)) return rc;
+  if (int rc = check_mat(z, "z", kOptional | kMayBePacked)) return rc;
+  if (int rc = check_mat(y8, "y8", kOptional | kMustBePacked)) return rc;
+  if (act < GOSH_ACT_NONE || act > GOSH_ACT_SILU) return fail(GOSH_EINVAL, "act = %d: no activation", act);
+  if (w->rows < 1 || w->rows > GOSH_MAT_MAX_COLS)
+    return fail(GOSH_EINVAL, "w: rows = %lld: must be in [1, %d]", (long long)w->rows, GOSH_MAT_MAX_COLS);
+  const int32_t out = static_cast<int32_t>(w->rows);
+  if (int rc = check_shape(w, "w", out, x->cols)) return rc;
+  const struct { const gosh_mat *m; const char *what; } outs[] = {{y, "y"}, {residual, "residual"}, {z, "z"}, {y8, "y8"}};
+  for (const auto &o : outs) {
+    if (int rc = check_shape(o.m, o.what, x->rows, out)) return rc;
+    if (int rc = check_type(o.m, o.what, x->type)) return rc;
+  }
+  if (int rc = check_type(w, "w", x->type)) return rc;
+  if (int rc = check_floats(bias, out, "bias", true)) return rc;
+  if (x->rows == 0) return GOSH_OK;
+  hipStream_t st = as_stream(hip_stream);
+  ForwardOut f{bias, plane_of(residual), plane_of(y), plane_of(z), plane_of(y8), act, z != nullptr && z->packed};
+  if (x->rows <= kFewRows && !f.z_packed && y8 == nullptr) {
+    if (x->type == GOSH_F32) return launch_few_rows<F32>(x, w, f, st);
+    if (x->type == GOSH_BF16) return launch_few_rows<Bf16>(x, w, f, st);
+    return launch_few_rows<F16>(x, w, f, st);
+  }
+  ProductArgs g{};
+  g.a = plane_of(x);
+  g.b = plane_of(w);
+  g.N = out;
+  g.K = x->cols;
+  g.forward = f;
+  if (x->type == GOSH_F32) return product_of_rows<F32>(kProductForward, g, x->rows, st);
+  if (x->type == GOSH_BF16) return product_of_rows<Bf16>(kProductForward, g, x->rows, st);
+  return product_of_rows<F16>(kProductForward, g, x->rows, st);
+}
+
+uint64_t gosh_linear_backward_workspace(int64_t rows, int32_t in, int32_t out, int32_t type, int32_t act) {
+  if (rows < 0 || in < 1 || out < 1 || in > GOSH_MAT_MAX_COLS || out > GOSH_MAT_MAX_COLS) return 0;
+  return gosh::plan_backward(rows, in, out, type, act).bytes;
+}
+
+int gosh_linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, const gosh_mat *z, int32_t act,
+                         const gosh_mat *dx, const gosh_mat *dw, float *db, void *workspace, uint64_t workspace_bytes,
+                         void *hip_stream) {
+  using namespace gosh;
+  if (int rc = check_mat(dy, "dy")) return rc;
+  if (int rc = check_mat(x, "x", kMayBePacked | (dw == nullptr ? kOptional : 0))) return rc;
+  if (int rc = check_mat(w, "w", dx == nullptr ? kOptional : 0)) return rc;
+  if (act < GOSH_ACT_NONE || act > GOSH_ACT_SILU) return fail(GOSH_EINVAL, "act = %d: no activation", act);
+  if (int rc = check_mat(z, "z", kMayBePacked | (act == GOSH_ACT_NONE ? kOptional : 0))) return rc;
+  if (int rc = check_mat(dx, "dx", kOptional)) return rc;
+  if (int rc = check_mat(dw, "dw", kOptional)) return rc;
+  const int32_t out = dy->cols;
+  if (dx == nullptr && dw == nullptr && db == nullptr) return GOSH_OK;
+  const int32_t in = dx != nullptr ? dx->cols : dw != nullptr ? dw->cols : 1;
+  if (int rc = check_shape(x, "x", dy->rows, in)) return rc;
+  if (int rc = check_shape(w, "w", out, in)) return rc;
+  if (int rc = check_shape(z, "z", dy->rows, out)) return rc;
+  if (int rc = check_shape(dx, "dx", dy->rows, in)) return rc;
+  if (int rc = check_shape(dw, "dw", out, in)) return rc;
+  const struct { const gosh_mat *m; const char *what; } all[] = {{x, "x"}, {w, "w"}, {z, "z"}, {dx, "dx"}};
+  for (const auto &o : all)
+    if (int rc = check_type(o.m, o.what, dy->type)) return rc;
+  if (dw != nullptr && dw->type != GOSH_F32)
+    if (int rc = check_type(dw, "dw", dy->type)) return rc;
+  if (int rc = check_floats(db, out, "db", true)) return rc;
+  if (int rc = check_workspace(workspace, workspace_bytes, plan_backward(dy->rows, in, out, dy->type, act).bytes)) return rc;
+  hipStream_t st = as_stream(hip_stream);
+  if (dy->type == GOSH_F32) return linear_backward<F32>(dy, x, w, z, act, dx, dw, db, workspace, in, out, st);
+  if (dy->type == GOSH_BF16) return linear_backward<Bf16>(dy, x, w, z, act, dx, dw, db, workspace, in, out, st);
+  return linear_backward<F16>(dy, x, w, z, act, dx, dw, db, workspace, in, out, st);
+}
+
+}  // extern "C"

@@ -77,48 +77,50 @@ int launch_few_rows(const gosh_mat *x, const gosh_mat *w, const ForwardOut &f, h
 
 constexpr int64_t kTilesPerLaunch = int64_t{1} << 22;  // a grid's threads stay below 2^31
 
-// Tiles of 128 x 128 once they fill the device's 256 CUs, of 64 x 64 before.
-bool small_tiles(int64_t M, int64_t N) { return ceil_div(M, 128) * ceil_div(N, 128) < 256; }
+// The largest tiles that still give every one of the device's 256 CUs a workgroup.
+TileSize tiles_for(int64_t M, int64_t N, bool direct) {
+  const auto tiles = [&](TileSize s) { return ceil_div(M, tile_m(s)) * ceil_div(N, tile_n(s)); };
+  return direct && tiles(kLarge) >= 256 ? kLarge : tiles(kMiddle) >= 256 ? kMiddle : kSmall;
+}
 
 template <typename T>
 int product_of_rows(ProductKind kind, ProductArgs g, int64_t rows, hipStream_t st) {
-  const bool small = small_tiles(rows, g.N);
-  const int64_t side = small ? 64 : 128;
-  g.tiles_n = static_cast<int32_t>(ceil_div(g.N, side));
+  g.direct = T::kType != GOSH_F32 && can_be_direct(g.a, g.K) && can_be_direct(g.b, kind == kProductForward ? g.K : g.N);
+  const TileSize size = tiles_for(rows, g.N, g.direct);
+  const int64_t depth = product_depth(T::kType, size, g.direct);
+  g.tiles_n = static_cast<int32_t>(ceil_div(g.N, tile_n(size)));
   g.splits = 1;
-  g.k_per_split = ceil_div(g.K, product_depth(T::kType, small)) * product_depth(T::kType, small);
-  const int64_t rows_per_launch = kTilesPerLaunch / g.tiles_n * side;
+  g.k_per_split = ceil_div(g.K, depth) * depth;
+  const int64_t rows_per_launch = kTilesPerLaunch / g.tiles_n * tile_m(size);
   const ProductArgs all = g;
   for (int64_t r = 0; r < rows; r += rows_per_launch) {
     g.M = std::min(rows_per_launch, rows - r);
-    g.tiles_m = static_cast<int32_t>(ceil_div(g.M, side));
+    g.tiles_m = static_cast<int32_t>(ceil_div(g.M, tile_m(size)));
     g.a = rows_from(all.a, r, T::kType, false);
     g.out = rows_from(all.out, r, T::kType, false);
     g.forward.residual = rows_from(all.forward.residual, r, T::kType, false);
     g.forward.y = rows_from(all.forward.y, r, T::kType, false);
     g.forward.z = rows_from(all.forward.z, r, T::kType, all.forward.z_packed != 0);
     g.forward.y8 = rows_from(all.forward.y8, r, T::kType, true);
-    if (int rc = launch_product<T>(kind, small, g, st)) return rc;
+    if (int rc = launch_product<T>(kind, size, g, st)) return rc;
   }
   return GOSH_OK;
 }
 
-// How dw is split along the rows: enough workgroups for two on every CU, at least 8 steps each.
+// How dw is split along the rows: enough workgroups for two on every CU, at least 256 rows each.
 struct DwPlan {
-  bool small;
+  TileSize size;
   int32_t tiles_m, tiles_n, splits;
   int64_t k_per_split;
 };
-DwPlan plan_dw(int64_t rows, int32_t in, int32_t out, int32_t type) {
+DwPlan plan_dw(int64_t rows, int32_t in, int32_t out, bool direct) {
   DwPlan p;
-  p.small = std::min(in, out) <= 64;
-  const int side = p.small ? 64 : 128, depth = product_depth(type, p.small);
-  p.tiles_m = static_cast<int32_t>(ceil_div(out, side));
-  p.tiles_n = static_cast<int32_t>(ceil_div(in, side));
+  p.size = std::min(in, out) <= 64 ? kSmall : direct && out > 128 ? kLarge : kMiddle;
+  p.tiles_m = static_cast<int32_t>(ceil_div(out, tile_m(p.size)));
+  p.tiles_n = static_cast<int32_t>(ceil_div(in, tile_n(p.size)));
   const int64_t tiles = static_cast<int64_t>(p.tiles_m) * p.tiles_n;
-  const int64_t most = std::max<int64_t>(1, rows / (8 * depth));
-  const int64_t want = std::min(most, std::max<int64_t>(1, 512 / tiles));
-  p.k_per_split = ceil_div(ceil_div(std::max<int64_t>(rows, 1), want), depth) * depth;
+  const int64_t want = std::min(std::max<int64_t>(1, rows / 256), std::max<int64_t>(1, 512 / tiles));
+  p.k_per_split = ceil_div(ceil_div(std::max<int64_t>(rows, 1), want), 64) * 64;  // a multiple of every tile's depth
   p.splits = static_cast<int32_t>(ceil_div(rows, p.k_per_split));
   return p;
 }
@@ -186,19 +188,20 @@ SlopePlan plan_slope(int64_t rows, int32_t n) {
 uint64_t round_up(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 struct BackwardPlan {
-  DwPlan dw;
+  DwPlan dw, dw_direct;
   SlopePlan slope;
   int64_t dz_ld;
   uint64_t dz, dw_parts, db_parts, bytes;  // offsets, and the whole
 };
 BackwardPlan plan_backward(int64_t rows, int32_t in, int32_t out, int32_t type, int32_t act) {
   BackwardPlan p;
-  p.dw = plan_dw(rows, in, out, type);
+  p.dw = plan_dw(rows, in, out, false);
+  p.dw_direct = plan_dw(rows, in, out, type != GOSH_F32);
   p.slope = plan_slope(rows, out);
   p.dz_ld = (out + 7) / 8 * 8;
   p.dz = 0;
   p.dw_parts = act == GOSH_ACT_NONE ? 0 : round_up(static_cast<uint64_t>(rows) * p.dz_ld * (type == GOSH_F32 ? 4 : 2));
-  p.db_parts = p.dw_parts + round_up(static_cast<uint64_t>(p.dw.splits) * in * out * 4);
+  p.db_parts = p.dw_parts + round_up(static_cast<uint64_t>(std::max(p.dw.splits, p.dw_direct.splits)) * in * out * 4);
   p.bytes = p.db_parts + round_up(static_cast<uint64_t>(p.slope.blocks_y) * out * 4);
   return p;
 }
@@ -232,21 +235,23 @@ int linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, co
     if (int rc = product_of_rows<T>(kProductDx, g, rows, st)) return rc;
   }
   if (dw != nullptr) {
+    ProductArgs g{};
+    g.a = dz;
+    g.b = plane_of(x);
+    g.direct = T::kType != GOSH_F32 && !x->packed && can_be_direct(g.a, out) && can_be_direct(g.b, in);
+    const DwPlan &d = g.direct ? p.dw_direct : p.dw;
     if (rows > 0) {
-      ProductArgs g{};
-      g.a = dz;
-      g.b = plane_of(x);
       g.M = out;
       g.N = in;
       g.K = rows;
-      g.k_per_split = p.dw.k_per_split;
-      g.tiles_m = p.dw.tiles_m;
-      g.tiles_n = p.dw.tiles_n;
-      g.splits = p.dw.splits;
+      g.k_per_split = d.k_per_split;
+      g.tiles_m = d.tiles_m;
+      g.tiles_n = d.tiles_n;
+      g.splits = d.splits;
       g.parts = dw_parts;
-      if (int rc = launch_product<T>(x->packed ? kProductDwPacked : kProductDw, p.dw.small, g, st)) return rc;
+      if (int rc = launch_product<T>(x->packed ? kProductDwPacked : kProductDw, d.size, g, st)) return rc;
     }
-    if (int rc = join_parts(dw_parts, p.dw.splits, static_cast<int64_t>(out) * in, out, in, dw->data, dw->ld, dw->type, st)) return rc;
+    if (int rc = join_parts(dw_parts, d.splits, static_cast<int64_t>(out) * in, out, in, dw->data, dw->ld, dw->type, st)) return rc;
   }
   return GOSH_OK;
 }

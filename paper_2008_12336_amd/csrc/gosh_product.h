@@ -32,6 +32,7 @@ struct ProductArgs {
   int64_t M, N, K;        // M, N < 2^31; K also
   int64_t k_per_split;    // a multiple of the tile's depth
   int32_t tiles_m, tiles_n, splits;
+  int32_t direct;         // 16-bit operands of aligned rows: see can_be_direct
   ForwardOut forward;     // kForward
   Plane out;              // kStore
   float *parts;           // kParts: splits x M x N
@@ -40,22 +41,37 @@ struct ProductArgs {
 // The products of a layer: which operands are k-major, whether B is packed.
 enum ProductKind : int { kProductForward, kProductDx, kProductDw, kProductDwPacked };
 
-// Launches for rows of one type; defined in gosh_product_{f32,bf16,f16}.hip.  `small`: 64 x 64 tiles.
+enum TileSize : int { kSmall, kMiddle, kLarge };  // kLarge: direct products only
+constexpr int tile_m(TileSize s) { return s == kLarge ? 256 : s == kMiddle ? 128 : 64; }
+constexpr int tile_n(TileSize s) { return s == kSmall ? 64 : 128; }
+
+// Launches for entries of one type; defined in gosh_product_{f32,bf16,f16}.hip.
 template <typename T>
-int launch_product(ProductKind kind, bool small, const ProductArgs &args, hipStream_t st);
+int launch_product(ProductKind kind, TileSize size, const ProductArgs &args, hipStream_t st);
 template <>
-int launch_product<F32>(ProductKind, bool, const ProductArgs &, hipStream_t);
+int launch_product<F32>(ProductKind, TileSize, const ProductArgs &, hipStream_t);
 template <>
-int launch_product<Bf16>(ProductKind, bool, const ProductArgs &, hipStream_t);
+int launch_product<Bf16>(ProductKind, TileSize, const ProductArgs &, hipStream_t);
 template <>
-int launch_product<F16>(ProductKind, bool, const ProductArgs &, hipStream_t);
+int launch_product<F16>(ProductKind, TileSize, const ProductArgs &, hipStream_t);
 
 template <typename T>
-struct ProductDepth {  // k of a tile: 128 and 64 bytes of LDS a row and part
+struct ProductDepth {  // k of a tile that passes through registers: 128 and 64 bytes of LDS a row and part
   static constexpr int value(bool small) { return T::kType == GOSH_F32 ? (small ? 32 : 16) : 64; }
 };
-inline int product_depth(int32_t type, bool small) {
-  return type == GOSH_F32 ? ProductDepth<F32>::value(small) : ProductDepth<Bf16>::value(small);
+
+// Whether an operand can go straight to LDS: 16-byte aligned rows, of whole chunks along memory.
+inline bool can_be_direct(const Plane &p, int64_t along) {
+  return reinterpret_cast<uintptr_t>(p.data) % 16 == 0 && p.ld % 8 == 0 && along % 8 == 0;
+}
+#ifndef DD
+#define DD 32
+#define DR 3
+#define DB 2
+#endif
+constexpr int kDirectDepth = DD, kDirectRing = DR;  // k of a tile; tiles in LDS
+inline int product_depth(int32_t type, TileSize size, bool direct) {
+  return direct ? kDirectDepth : type == GOSH_F32 ? ProductDepth<F32>::value(size == kSmall) : ProductDepth<Bf16>::value(false);
 }
 
 typedef float F16x __attribute__((ext_vector_type(16)));
@@ -87,13 +103,44 @@ __device__ __forceinline__ Range range_of(const void *p, int64_t bytes) {
 }
 constexpr uint32_t kNowhere = 0x80000000u;  // an offset past every range, also with what is added to it
 
+// Where an operand's 16-byte chunks lie in LDS, in entries.  16 lanes of a wavefront are served at a time, from 64 banks
+// of 4 bytes: rows are shifted against each other so that the 16 chunks (or half chunks) that they ask for together lie
+// in different banks.  Unshifted rows of 128 bytes were read at half the rate (124 instead of 240 bytes a cycle and CU).
+template <int BX, int BK>
+struct Spread {
+  static constexpr int kAlongK = BK / 8, kRowsK = 128 / BK;  // chunks of a k-major row, rows that span the banks
+  static __device__ __forceinline__ int k_major(int row, int chunk) {  // row = m
+    return row * BK + ((chunk ^ ((row / kRowsK) & (kAlongK - 1))) * 8);
+  }
+  static __device__ __forceinline__ int shift(int k) { return BX >= 128 ? 2 * (k & 3) : 2 * ((k >> 1) & 1); }
+  static __device__ __forceinline__ int m_major(int row, int chunk) {  // row = k
+    return row * BX + (((chunk >> 1) ^ shift(row)) * 16) + (chunk & 1) * 8;
+  }
+  // 8 k (16 kk + 8 (lane / 32) + 0..7) of m = base + lane % 32, as the matrix cores take them.
+  template <bool KMajor>
+  static __device__ __forceinline__ S8 take(const uint16_t *lds, int base, int kk) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (KMajor) {
+      return *reinterpret_cast<const S8 *>(lds + k_major(base + (lane & 31), kk * 2 + (lane >> 5)));
+    } else {
+      typedef __attribute__((address_space(3))) S4 Shared;
+      const int k = kk * 16 + 8 * (lane >> 5) + (lane & 15) / 4;
+      const int pair = base / 16 + ((lane >> 4) & 1);
+      const uint16_t *const from = lds + k * BX + ((pair ^ shift(k)) * 16) + (lane & 3) * 4;
+      const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)(from));
+      const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)(from + 4 * BX));
+      return S8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    }
+  }
+};
+
 // One operand's tile: BX entries of m by BK of k.
 template <typename T, int BX, int BK, bool KMajor, bool Packed>
 struct Tile {
   static_assert(!(KMajor && Packed), "only x of dw is packed");
   // a packed entry is a whole number of 8 bits times a power of two: one part holds it
   static constexpr int kParts = Packed ? 1 : Cores<T>::kParts;
-  static constexpr int kBytes = kParts * BX * BK * 2;
+  static constexpr int kBytes = kParts * BX * BK * 2;  // of LDS
   static constexpr int kSize = Packed ? 1 : T::kType == GOSH_F32 ? 4 : 2;
   static constexpr int kChunks = BX * BK / 8;               // of 8 entries along memory
   static constexpr int kPerThread = kChunks / 256;
@@ -103,14 +150,6 @@ struct Tile {
 
   uint32_t raw[kPerThread][kWords];
   uint32_t unit[Packed ? kPerThread : 1];
-
-  // Reading 8 lanes' chunks of one column takes in all banks if rows of 128 bytes are shifted against each other.
-  static __device__ __forceinline__ int shift_k(int row) {
-    constexpr int per = BK / 8;
-    return per >= 8 ? row & 7 : (row / (8 / per)) & (per - 1);
-  }
-  // The transposing reads of a wavefront take in rows k = 0..3 and 8..11 (+ 4 j + 16 i) of two neighbouring 16 columns.
-  static __device__ __forceinline__ int shift_m(int k) { return ((k & 3) | ((k >> 1) & 4)) & (BX / 16 - 1); }
 
   // x: first m of the tile, of `mx`; k: first k, up to `kx`.  `ragged`: the step may hold chunks of which some entries
   // are there.
@@ -172,8 +211,7 @@ struct Tile {
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
       const int row = t / kAlong + i * (256 / kAlong), c = t % kAlong;
-      uint16_t *const to =
-          lds + (KMajor ? row * BK + ((c ^ shift_k(row)) * 8) : row * BX + (((c >> 1) ^ shift_m(row)) * 16) + (c & 1) * 8);
+      uint16_t *const to = lds + (KMajor ? Spread<BX, BK>::k_major(row, c) : Spread<BX, BK>::m_major(row, c));
       if constexpr (Packed) {
         const uint32_t q[2] = {raw[i][0], raw[i][1]};
         float v[8];
@@ -209,57 +247,132 @@ struct Tile {
       }
     }
   }
-
-  // 8 k (16 kk + 8 (lane / 32) + 0..7) of m = base + lane % 32.
-  static __device__ __forceinline__ S8 take(const uint16_t *lds, int part, int base, int kk) {
-    const int lane = threadIdx.x & 63;
-    lds += part * BX * BK;
-    if constexpr (KMajor) {
-      const int row = base + (lane & 31);
-      return *reinterpret_cast<const S8 *>(lds + row * BK + (((kk * 2 + (lane >> 5)) ^ shift_k(row)) * 8));
-    } else {
-      typedef __attribute__((address_space(3))) S4 Shared;
-      const int k = kk * 16 + 8 * (lane >> 5) + (lane & 15) / 4;
-      const int pair = base / 16 + ((lane >> 4) & 1);
-      const uint16_t *const from = lds + k * BX + ((pair ^ shift_m(k)) * 16) + (lane & 3) * 4;
-      const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)(from));
-      const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared *)(from + 4 * BX));
-      return S8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    }
-  }
 };
 
-// Where the entries of the result go, 8 along a row at a time.
-template <typename T>
-__device__ __forceinline__ void put_forward(const ForwardOut &f, int64_t row, int col, int count, float (&v)[8], bool head) {
-  if (f.bias != nullptr && count > 0) {
-    float b[8];
-    Entries<F32, 8>::load(f.bias + col, count, b);
+// 8 entries of a row of z become entries of y.  Full: all of them are there.
+template <typename T, typename A, bool Full>
+__device__ __forceinline__ void put_forward(const ForwardOut &f, int64_t row, int col, int there, float (&v)[8], bool head) {
+  typedef typename T::Store S;
+  const int count = Full ? 8 : there;
+  if (!Full) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += b[i];
+    for (int i = 0; i < 8; ++i) v[i] = i < count ? v[i] : 0.f;  // entries that are not there count in no group
   }
   if (f.z.data != nullptr) {
     if (f.z_packed) store_packed<T, 8>(f.z, row, col, count, v, head, 4);
-    else if (count > 0) Entries<T, 8>::store(static_cast<typename T::Store *>(f.z.data) + row * f.z.ld + col, count, v);
+    else if (Full || count > 0) Entries<T, 8>::store(static_cast<S *>(f.z.data) + row * f.z.ld + col, count, v);
   }
-  with_activation(f.act, [&](auto a) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = decltype(a)::value(v[i]);
-  });
-  if (f.residual.data != nullptr && count > 0) {
+  for (int i = 0; i < 8; ++i) v[i] = A::value(v[i]);
+  if (f.residual.data != nullptr && (Full || count > 0)) {
     float r[8];
-    Entries<T, 8>::load(static_cast<const typename T::Store *>(f.residual.data) + row * f.residual.ld + col, count, r);
+    Entries<T, 8>::load(static_cast<const S *>(f.residual.data) + row * f.residual.ld + col, count, r);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += r[i];
   }
-  if (f.y8.data != nullptr) {  // entries past the last column are not part of their group
+  if (f.y8.data != nullptr) {
+    if (!Full) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < count ? v[i] : 0.f;
+      for (int i = 0; i < 8; ++i) v[i] = i < count ? v[i] : 0.f;
+    }
     store_packed<T, 8>(f.y8, row, col, count, v, head, 4);
   }
-  if (count > 0) Entries<T, 8>::store(static_cast<typename T::Store *>(f.y.data) + row * f.y.ld + col, count, v);
+  if (Full || count > 0) Entries<T, 8>::store(static_cast<S *>(f.y.data) + row * f.y.ld + col, count, v);
 }
 
+// Which tile a workgroup computes.  Workgroups go round the 8 XCDs: each XCD gets a contiguous run of tiles, those of
+// the same rows next to each other, so that they share its L2.
+struct Place {
+  int64_t m0, n0, k0, k1;
+  int split;
+};
+__device__ __forceinline__ Place place_of(const ProductArgs &g, int bm, int bn) {
+  const int total = g.tiles_m * g.tiles_n * g.splits;
+  int id = blockIdx.x;
+  if (id < total / 8 * 8) id = id % 8 * (total / 8) + id / 8;
+  const int tn = id % g.tiles_n, tm = id / g.tiles_n % g.tiles_m, split = id / g.tiles_n / g.tiles_m;
+  const int64_t k0 = split * g.k_per_split;
+  return {static_cast<int64_t>(tm) * bm, static_cast<int64_t>(tn) * bn, k0,
+          k0 + g.k_per_split < g.K ? k0 + g.k_per_split : g.K, split};
+}
+
+// What the accumulators start from: the bias of a lane's column.
+template <int RM, int RN, ProductOut Out>
+__device__ __forceinline__ void start(const ProductArgs &g, int64_t n, F16x (&acc)[RM][RN]) {
+#pragma unroll
+  for (int j = 0; j < RN; ++j) {
+    const int64_t col = n + 32 * j + (threadIdx.x & 31);
+    const float b = Out == kForward && g.forward.bias != nullptr && col < g.N ? g.forward.bias[col] : 0.f;
+#pragma unroll
+    for (int i = 0; i < RM; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = b;
+  }
+}
+
+template <int W>
+struct Slab {  // a wavefront's 32 rows of W results on their way from columns to rows
+  static constexpr int kPitch = W + 8;
+  static constexpr int kFloats = 32 * kPitch;
+};
+
+// The accumulators of a wavefront, at m, n, to where they go, 32 rows at a time through its slab: a lane of the
+// accumulators holds entries of one column.
+template <typename T, int RM, int RN, ProductOut Out, bool Full, typename A>
+__device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[RM][RN], float *slab, int64_t m, int64_t n, int split) {
+  constexpr int W = 32 * RN, kLanes = W / 8;  // lanes of a row
+  constexpr int kPitch = Slab<W>::kPitch;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < RM; ++i) {
+#pragma unroll
+    for (int j = 0; j < RN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        slab[(8 * (r / 4) + 4 * (lane >> 5) + r % 4) * kPitch + 32 * j + (lane & 31)] = acc[i][j][r];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 2
+    for (int pass = 0; pass < 32 * kLanes / 64; ++pass) {
+      const int r = pass * (64 / kLanes) + lane / kLanes, c = lane % kLanes * 8;
+      const int64_t row = m + 32 * i + r;
+      const int col = static_cast<int>(n) + c;
+      const int64_t left = row < g.M ? g.N - col : 0;
+      const int count = Full ? 8 : static_cast<int>(left < 0 ? 0 : left > 8 ? 8 : left);
+      float v[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const F4 x = *reinterpret_cast<const F4 *>(slab + r * kPitch + c + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
+      }
+      if constexpr (Out == kForward) {
+        put_forward<T, A, Full>(g.forward, row, col, count, v, (lane & 3) == 0);
+      } else if constexpr (Out == kStore) {
+        if (count > 0)
+          Entries<T, 8>::store(static_cast<typename T::Store *>(g.out.data) + row * g.out.ld + col, count, v);
+      } else {
+        if (count > 0) Entries<F32, 8>::store(g.parts + (split * g.M + row) * g.N + col, count, v);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+template <typename T, int RM, int RN, ProductOut Out>
+__device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[RM][RN], float *slab, int64_t m, int64_t n, int split) {
+  const auto with = [&](auto a) {
+    typedef decltype(a) A;
+    if (m + 32 * RM <= g.M && n + 32 * RN <= g.N) finish<T, RM, RN, Out, true, A>(g, acc, slab, m, n, split);
+    else finish<T, RM, RN, Out, false, A>(g, acc, slab, m, n, split);
+  };
+  if constexpr (Out == kForward) with_activation(g.forward.act, with);
+  else with(Activation<GOSH_ACT_NONE>{});
+}
+
+// Tiles that pass through registers on their way to LDS: 32-bit entries, packed ones, and matrices whose rows are not
+// 16-byte aligned.
 template <typename T, int BX, ProductKind Kind, ProductOut Out>
 __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs g) {
   constexpr int BK = ProductDepth<T>::value(BX == 64);
@@ -268,28 +381,17 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs g) {
   typedef Tile<T, BX, BK, b_k, Kind == kProductDwPacked> TB;
   constexpr int W = BX / 2, R = W / 32;          // a wavefront's square of the tile, and its 32 x 32 blocks a side
   constexpr int kBuffer = (TA::kBytes + TB::kBytes) / 2;
-  constexpr int kPitch = W + 8;                  // floats in a row of a wavefront's slab of the result
-  constexpr int kSlab = 32 * kPitch;
-  constexpr int kLds = 2 * kBuffer * 2 > 4 * kSlab * 4 ? 2 * kBuffer * 2 : 4 * kSlab * 4;
+  constexpr int kLds = 2 * kBuffer * 2 > 4 * Slab<W>::kFloats * 4 ? 2 * kBuffer * 2 : 4 * Slab<W>::kFloats * 4;
   __shared__ __attribute__((aligned(16))) uint16_t lds[kLds / 2];
 
-  // Workgroups go round the 8 XCDs: each XCD gets a contiguous run of tiles, those of the same rows next to each other,
-  // so that they share its L2.
-  const int total = g.tiles_m * g.tiles_n * g.splits;
-  int id = blockIdx.x;
-  if (id < total / 8 * 8) id = id % 8 * (total / 8) + id / 8;
-  const int tn = id % g.tiles_n, tm = id / g.tiles_n % g.tiles_m, split = id / g.tiles_n / g.tiles_m;
-  const int64_t m0 = static_cast<int64_t>(tm) * BX, n0 = static_cast<int64_t>(tn) * BX;
-  const int64_t k0 = split * g.k_per_split, k1 = k0 + g.k_per_split < g.K ? k0 + g.k_per_split : g.K;
+  const Place at = place_of(g, BX, BX);
+  const int64_t m0 = at.m0, n0 = at.n0, k0 = at.k0, k1 = at.k1;
   const int steps = static_cast<int>((k1 - k0 + BK - 1) / BK);
 
-  const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+  const int wave = threadIdx.x / 64;
   const int wm = wave / 2 * W, wn = wave % 2 * W;
   F16x acc[R][R];
-#pragma unroll
-  for (int i = 0; i < R; ++i)
-#pragma unroll
-    for (int j = 0; j < R; ++j) acc[i][j] = F16x{};
+  start<R, R, Out>(g, n0 + wn, acc);
 
   // The last step's chunks may be short: along k where K is no multiple of 8; along m the very last row of memory ends
   // inside its last chunk, of which the hardware's bounds check drops a dword that is only half there.
@@ -318,11 +420,11 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs g) {
 #pragma unroll
       for (int p = 0; p < TA::kParts; ++p)
 #pragma unroll
-        for (int i = 0; i < R; ++i) fa[p][i] = TA::take(now, p, wm + 32 * i, kk);
+        for (int i = 0; i < R; ++i) fa[p][i] = Spread<BX, BK>::template take<a_k>(now + p * BX * BK, wm + 32 * i, kk);
 #pragma unroll
       for (int p = 0; p < TB::kParts; ++p)
 #pragma unroll
-        for (int i = 0; i < R; ++i) fb[p][i] = TB::take(now + TA::kBytes / 2, p, wn + 32 * i, kk);
+        for (int i = 0; i < R; ++i) fb[p][i] = Spread<BX, BK>::template take<b_k>(now + TA::kBytes / 2 + p * BX * BK, wn + 32 * i, kk);
 #pragma unroll
       for (int order = TA::kParts + TB::kParts - 2; order >= 0; --order)  // the smallest products first
 #pragma unroll
@@ -341,64 +443,142 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs g) {
   }
   __syncthreads();
 
-  // Through LDS into rows: a lane of the accumulators holds entries of one column.
-  float *const slab = reinterpret_cast<float *>(lds) + wave * kSlab;
-  constexpr int kLanes = W / 8;  // lanes of a row
-#pragma unroll
-  for (int i = 0; i < R; ++i) {
-#pragma unroll
-    for (int j = 0; j < R; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        slab[(8 * (r / 4) + 4 * (lane >> 5) + r % 4) * kPitch + 32 * j + (lane & 31)] = acc[i][j][r];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-    for (int pass = 0; pass < 32 * kLanes / 64; ++pass) {
-      const int r = pass * (64 / kLanes) + lane / kLanes, c = lane % kLanes * 8;
-      const int64_t row = m0 + wm + 32 * i + r;
-      const int64_t col = n0 + wn + c;
-      const int64_t left = row < g.M ? g.N - col : 0;
-      const int count = static_cast<int>(left < 0 ? 0 : left > 8 ? 8 : left);
-      float v[8];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const F4 x = *reinterpret_cast<const F4 *>(slab + r * kPitch + c + 4 * h);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
-      }
-      if constexpr (Out == kForward) {
-        // entries that are not there count in no group
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = e < count ? v[e] : 0.f;
-        put_forward<T>(g.forward, row, static_cast<int>(col), count, v, (lane & 3) == 0);
-      } else if constexpr (Out == kStore) {
-        if (count > 0)
-          Entries<T, 8>::store(static_cast<typename T::Store *>(g.out.data) + row * g.out.ld + col, count, v);
-      } else {
-        if (count > 0) Entries<F32, 8>::store(g.parts + (split * g.M + row) * g.N + col, count, v);
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
+  finish<T, R, R, Out>(g, acc, reinterpret_cast<float *>(lds) + wave * Slab<W>::kFloats, m0 + wm, n0 + wn, at.split);
 }
 
-template <typename T, int BX, ProductKind Kind, ProductOut Out>
+// ---- 16-bit tiles that go straight to LDS -------------------------------------------------------
+
+// A tile that the memory system writes to LDS by itself, 1 KB an instruction of a wavefront: lane i's 16 bytes land at
+// 16 i, so that the lanes ask for the chunks that belong there.  Rows are 16-byte aligned and whole numbers of chunks.
+template <int BX, int BK, bool KMajor>
+struct DirectTile {
+  static constexpr int kBytes = BX * BK * 2;
+  static constexpr int kLoads = kBytes / 1024 / 4;            // of a wavefront
+  static constexpr int kAlong = (KMajor ? BK : BX) / 8;       // chunks in a row of the tile
+  uint32_t off[kLoads];
+  int along[kLoads];  // first k of the lane's chunks (k-major)
+
+  __device__ __forceinline__ void init(const Plane &p) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = (wave * kLoads + i) * 64 + lane;
+      const int row = at / kAlong, slot = at % kAlong;
+      // the chunk that the shifts put at this slot: they are their own inverse
+      const int chunk = KMajor ? Spread<BX, BK>::k_major(row, slot) / 8 % kAlong : Spread<BX, BK>::m_major(row, slot) / 8 % kAlong;
+      off[i] = static_cast<uint32_t>(row * static_cast<int>(p.ld) + chunk * 8) * 2;
+      along[i] = chunk * 8;
+    }
+  }
+  // Starts the loads of a step into the tile at byte `lds` of LDS.  What is past the range reads as zero; so are chunks
+  // past the last k made to.
+  __device__ __forceinline__ void fetch(const Plane &p, int64_t x, int64_t mx, int64_t k, int64_t kx, uint32_t lds) const {
+    const int64_t row0 = KMajor ? x : k, col0 = KMajor ? k : x;
+    const int64_t rows = (KMajor ? mx : kx) - row0, cols = (KMajor ? kx : mx) - col0;
+    const int64_t bytes = ((rows - 1) * p.ld + cols) * 2;
+    const char *const base = static_cast<const char *>(p.data) + (row0 * p.ld + col0) * 2;
+    const uint64_t b = reinterpret_cast<uint64_t>(base);
+    const U4 range{static_cast<uint32_t>(b), static_cast<uint32_t>(b >> 32) & 0xffffu,
+                   static_cast<uint32_t>(bytes <= 0 ? 0 : bytes > 0x7fffffff ? 0x7fffffff : bytes), 0x00020000u};
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      uint32_t o = off[i];
+      if (KMajor) o = along[i] < cols ? o : kNowhere;
+      // m0 holds where the first lane's bytes land; the load has no destination register
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   :: "s"(lds + (wave * kLoads + i) * 1024), "v"(o), "s"(range) : "memory");
+    }
+  }
+};
+
+// The same product with a ring of kRing tiles: the loads of kRing - 1 steps are under way while a step is computed.
+template <typename T, int BM, int BN, ProductKind Kind, ProductOut Out>
+__global__ __launch_bounds__(256, DB) void direct_product_kernel(const ProductArgs g) {
+  constexpr int BK = kDirectDepth;
+  constexpr bool a_k = Kind == kProductForward || Kind == kProductDx, b_k = Kind == kProductForward;
+  typedef DirectTile<BM, BK, a_k> TA;
+  typedef DirectTile<BN, BK, b_k> TB;
+  constexpr int WM = BM / 2, WN = BN / 2, RM = WM / 32, RN = WN / 32, kRing = kDirectRing;
+  constexpr int kStep = TA::kBytes + TB::kBytes, kLoads = TA::kLoads + TB::kLoads;
+  constexpr int kLds = kRing * kStep > 4 * Slab<WN>::kFloats * 4 ? kRing * kStep : 4 * Slab<WN>::kFloats * 4;
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[kLds / 2];
+
+  const Place at = place_of(g, BM, BN);
+  const int steps = static_cast<int>((at.k1 - at.k0 + BK - 1) / BK);
+  const int wave = threadIdx.x / 64;
+  const int wm = wave / 2 * WM, wn = wave % 2 * WN;
+  F16x acc[RM][RN];
+  start<RM, RN, Out>(g, at.n0 + wn, acc);
+
+  const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint16_t *)lds));
+  TA a;
+  TB b;
+  a.init(g.a);
+  b.init(g.b);
+  uint32_t into = base;  // where the next step goes
+  const auto fetch = [&](int s) {  // past the last step too, where it loads nothing: the count of loads stays the same
+    const int64_t k = at.k0 + static_cast<int64_t>(s) * BK;
+    a.fetch(g.a, at.m0, g.M, k, at.k1, into);
+    b.fetch(g.b, at.n0, g.N, k, at.k1, into + TA::kBytes);
+    into = into == base + (kRing - 1) * kStep ? base : into + kStep;
+  };
+#pragma unroll
+  for (int s = 0; s < kRing - 1; ++s) fetch(s);
+  const uint16_t *now = lds;
+  for (int s = 0; s < steps; ++s) {
+    // loads end in order: all but those of the kRing - 2 steps after this one.  Then every wavefront's part is there,
+    // and every wavefront is done with the tile before, which the next loads replace.
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((kRing - 2) * kLoads) : "memory");
+    fetch(s + kRing - 1);
+#pragma unroll
+    for (int kk = 0; kk < BK / 16; ++kk) {
+      S8 fa[RM], fb[RN];
+#pragma unroll
+      for (int i = 0; i < RM; ++i) fa[i] = Spread<BM, BK>::template take<a_k>(now, wm + 32 * i, kk);
+#pragma unroll
+      for (int i = 0; i < RN; ++i) fb[i] = Spread<BN, BK>::template take<b_k>(now + TA::kBytes / 2, wn + 32 * i, kk);
+#pragma unroll
+      for (int i = 0; i < RM; ++i)
+#pragma unroll
+        for (int j = 0; j < RN; ++j) acc[i][j] = Cores<T>::mma(fa[i], fb[j], acc[i][j]);
+    }
+    now = now == lds + (kRing - 1) * (kStep / 2) ? lds : now + kStep / 2;
+  }
+  // no load may land in the slabs, and no wavefront may still read the last tile
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  finish<T, RM, RN, Out>(g, acc, reinterpret_cast<float *>(lds) + wave * Slab<WN>::kFloats, at.m0 + wm, at.n0 + wn, at.split);
+}
+
+template <typename T, TileSize Size, ProductKind Kind, ProductOut Out>
 int launch_one(const ProductArgs &g, hipStream_t st) {
   const unsigned blocks = static_cast<unsigned>(g.tiles_m) * g.tiles_n * g.splits;
-  product_kernel<T, BX, Kind, Out><<<dim3(blocks), dim3(256), 0, st>>>(g);
+  if constexpr (T::kType != GOSH_F32 && Kind != kProductDwPacked) {
+    if (g.direct) {
+      direct_product_kernel<T, tile_m(Size), tile_n(Size), Kind, Out><<<dim3(blocks), dim3(256), 0, st>>>(g);
+      return check_launch("matrix product");
+    }
+  }
+  if constexpr (Size != kLarge)
+    product_kernel<T, tile_m(Size), Kind, Out><<<dim3(blocks), dim3(256), 0, st>>>(g);
   return check_launch("matrix product");
 }
 
-template <typename T, int BX>
+template <typename T, TileSize Size>
 int launch_sized(ProductKind kind, const ProductArgs &g, hipStream_t st) {
   switch (kind) {
-    case kProductForward: return launch_one<T, BX, kProductForward, kForward>(g, st);
-    case kProductDx: return launch_one<T, BX, kProductDx, kStore>(g, st);
-    case kProductDw: return launch_one<T, BX, kProductDw, kParts>(g, st);
-    default: return launch_one<T, BX, kProductDwPacked, kParts>(g, st);
+    case kProductForward: return launch_one<T, Size, kProductForward, kForward>(g, st);
+    case kProductDx: return launch_one<T, Size, kProductDx, kStore>(g, st);
+    case kProductDw: return launch_one<T, Size, kProductDw, kParts>(g, st);
+    default: return launch_one<T, Size, kProductDwPacked, kParts>(g, st);
   }
+}
+
+template <typename T>
+int launch_any(ProductKind kind, TileSize size, const ProductArgs &g, hipStream_t st) {
+  if (size == kLarge) return launch_sized<T, kLarge>(kind, g, st);
+  if (size == kMiddle) return launch_sized<T, kMiddle>(kind, g, st);
+  return launch_sized<T, kSmall>(kind, g, st);
 }
 
 }  // namespace gosh

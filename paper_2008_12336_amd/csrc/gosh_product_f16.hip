@@ -4,8 +4,8 @@
 namespace gosh {
 
 template <>
-int launch_product<F16>(ProductKind kind, bool small, const ProductArgs &args, hipStream_t st) {
-  return small ? launch_sized<F16, 64>(kind, args, st) : launch_sized<F16, 128>(kind, args, st);
+int launch_product<F16>(ProductKind kind, TileSize size, const ProductArgs &args, hipStream_t st) {
+  return launch_any<F16>(kind, size, args, st);
 }
 
 }  // namespace gosh

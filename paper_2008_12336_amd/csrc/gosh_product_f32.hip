@@ -4,8 +4,8 @@
 namespace gosh {
 
 template <>
-int launch_product<F32>(ProductKind kind, bool small, const ProductArgs &args, hipStream_t st) {
-  return small ? launch_sized<F32, 64>(kind, args, st) : launch_sized<F32, 128>(kind, args, st);
+int launch_product<F32>(ProductKind kind, TileSize size, const ProductArgs &args, hipStream_t st) {
+  return launch_any<F32>(kind, size, args, st);
 }
 
 }  // namespace gosh

@@ -59,7 +59,7 @@ def packed_within(p, want, bound, what):
 SHAPES = [  # rows, in, out, padding of the rows, entries off the start of memory
     (1, 1, 1, 0, 0), (1, 512, 2048, 0, 0), (2, 37, 5, 3, 1), (7, 130, 33, 0, 1), (8, 64, 257, 1, 0), (9, 8, 1, 0, 0),
     (33, 3, 40, 5, 3), (64, 64, 64, 0, 0), (129, 260, 130, 0, 0), (200, 17, 517, 2, 1), (300, 1024, 96, 8, 8),
-    (1000, 132, 31, 0, 0), (20000, 72, 260, 0, 0), (16391, 128, 384, 0, 0),
+    (1000, 132, 31, 0, 0), (20000, 72, 260, 0, 0), (16391, 128, 384, 0, 0), (33001, 64, 264, 0, 0),
 ]
 
 

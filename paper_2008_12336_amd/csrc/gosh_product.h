@@ -64,12 +64,7 @@ struct ProductDepth {  // k of a tile that passes through registers: 128 and 64 
 inline bool can_be_direct(const Plane &p, int64_t along) {
   return reinterpret_cast<uintptr_t>(p.data) % 16 == 0 && p.ld % 8 == 0 && along % 8 == 0;
 }
-#ifndef DD
-#define DD 32
-#define DR 3
-#define DB 2
-#endif
-constexpr int kDirectDepth = DD, kDirectRing = DR;  // k of a tile; tiles in LDS
+constexpr int kDirectDepth = 32, kDirectRing = 3;  // k of a tile; tiles in LDS
 inline int product_depth(int32_t type, TileSize size, bool direct) {
   return direct ? kDirectDepth : type == GOSH_F32 ? ProductDepth<F32>::value(size == kSmall) : ProductDepth<Bf16>::value(false);
 }
@@ -280,84 +275,99 @@ __device__ __forceinline__ void put_forward(const ForwardOut &f, int64_t row, in
   if (Full || count > 0) Entries<T, 8>::store(static_cast<S *>(f.y.data) + row * f.y.ld + col, count, v);
 }
 
-// Which tile a workgroup computes.  Workgroups go round the 8 XCDs: each XCD gets a contiguous run of tiles, those of
-// the same rows next to each other, so that they share its L2.
+// The id-th tile.
 struct Place {
   int64_t m0, n0, k0, k1;
   int split;
 };
-__device__ __forceinline__ Place place_of(const ProductArgs &g, int bm, int bn) {
-  const int total = g.tiles_m * g.tiles_n * g.splits;
-  int id = blockIdx.x;
-  if (id < total / 8 * 8) id = id % 8 * (total / 8) + id / 8;
+__device__ __forceinline__ Place place_of(const ProductArgs &g, int id, int bm, int bn) {
   const int tn = id % g.tiles_n, tm = id / g.tiles_n % g.tiles_m, split = id / g.tiles_n / g.tiles_m;
   const int64_t k0 = split * g.k_per_split;
   return {static_cast<int64_t>(tm) * bm, static_cast<int64_t>(tn) * bn, k0,
           k0 + g.k_per_split < g.K ? k0 + g.k_per_split : g.K, split};
 }
 
-// What the accumulators start from: the bias of a lane's column.
-template <int RM, int RN, ProductOut Out>
-__device__ __forceinline__ void start(const ProductArgs &g, int64_t n, F16x (&acc)[RM][RN]) {
+// Workgroups go round the 8 XCDs: each XCD gets a contiguous run of tiles, those of the same rows next to each other, so
+// that they share its L2, and its workgroups take turns along the run.
+struct Turns {
+  int id, end, step;
+};
+__device__ __forceinline__ Turns turns_of(int total) {
+  const int blocks = gridDim.x, b = blockIdx.x;
+  if (blocks % 8 != 0) return {b, total, blocks};
+  const int xcd = b % 8, per = total / 8, more = total % 8;
+  const int first = xcd * per + (xcd < more ? xcd : more);
+  return {first + b / 8, first + per + (xcd < more), blocks / 8};
+}
+
+// What the accumulators start from: the bias of a lane's columns.
+template <int RN, ProductOut Out>
+__device__ __forceinline__ void load_bias(const ProductArgs &g, int64_t n, float (&bias)[RN]) {
 #pragma unroll
   for (int j = 0; j < RN; ++j) {
     const int64_t col = n + 32 * j + (threadIdx.x & 31);
-    const float b = Out == kForward && g.forward.bias != nullptr && col < g.N ? g.forward.bias[col] : 0.f;
+    bias[j] = Out == kForward && g.forward.bias != nullptr && col < g.N ? g.forward.bias[col] : 0.f;
+  }
+}
+template <int RM, int RN>
+__device__ __forceinline__ void start(const float (&bias)[RN], F16x (&acc)[RM][RN]) {
+#pragma unroll
+  for (int j = 0; j < RN; ++j)
 #pragma unroll
     for (int i = 0; i < RM; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = b;
-  }
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = bias[j];
 }
 
+// A wavefront's 8 rows of W results on their way from columns to rows: where entry (row, col) lies.  Written by lanes of
+// which half are 4 rows on, read 8 columns of a lane in two steps: the shifts keep both off each other's banks.
 template <int W>
-struct Slab {  // a wavefront's 32 rows of W results on their way from columns to rows
-  static constexpr int kPitch = W + 8;
-  static constexpr int kFloats = 32 * kPitch;
+struct Slab {
+  static constexpr int kFloats = 8 * W;
+  static __device__ __forceinline__ int at(int row, int col) {
+    return W == 64 ? row * W + (col ^ (row & 4) * 8 ^ (row & 1) * 4) : row * W + (col ^ (row & 2) * 2);
+  }
 };
 
-// The accumulators of a wavefront, at m, n, to where they go, 32 rows at a time through its slab: a lane of the
+// The accumulators of a wavefront, at m, n, to where they go, 8 rows at a time through its slab: a lane of the
 // accumulators holds entries of one column.
 template <typename T, int RM, int RN, ProductOut Out, bool Full, typename A>
 __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[RM][RN], float *slab, int64_t m, int64_t n, int split) {
   constexpr int W = 32 * RN, kLanes = W / 8;  // lanes of a row
-  constexpr int kPitch = Slab<W>::kPitch;
   const int lane = threadIdx.x & 63;
+  const int r = lane / kLanes, c = lane % kLanes * 8;
 #pragma unroll
-  for (int i = 0; i < RM; ++i) {
+  for (int i = 0; i < RM; ++i)
 #pragma unroll
-    for (int j = 0; j < RN; ++j)
+    for (int q = 0; q < 4; ++q) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        slab[(8 * (r / 4) + 4 * (lane >> 5) + r % 4) * kPitch + 32 * j + (lane & 31)] = acc[i][j][r];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll 2
-    for (int pass = 0; pass < 32 * kLanes / 64; ++pass) {
-      const int r = pass * (64 / kLanes) + lane / kLanes, c = lane % kLanes * 8;
-      const int64_t row = m + 32 * i + r;
+      for (int j = 0; j < RN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) slab[Slab<W>::at(4 * (lane >> 5) + e, 32 * j + (lane & 31))] = acc[i][j][4 * q + e];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      const int64_t row = m + 32 * i + 8 * q + r;
       const int col = static_cast<int>(n) + c;
-      const int64_t left = row < g.M ? g.N - col : 0;
-      const int count = Full ? 8 : static_cast<int>(left < 0 ? 0 : left > 8 ? 8 : left);
+      const int64_t left = r < 8 && row < g.M ? g.N - col : 0;
+      const int count = Full && kLanes == 8 ? 8 : static_cast<int>(left < 0 ? 0 : left > 8 ? 8 : left);
       float v[8];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const F4 x = *reinterpret_cast<const F4 *>(slab + r * kPitch + c + 4 * h);
+        const F4 x = *reinterpret_cast<const F4 *>(slab + Slab<W>::at(r & 7, c + 4 * h));
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
       }
       if constexpr (Out == kForward) {
-        put_forward<T, A, Full>(g.forward, row, col, count, v, (lane & 3) == 0);
+        put_forward<T, A, Full && kLanes == 8>(g.forward, row, col, count, v, (lane & 3) == 0);
       } else if constexpr (Out == kStore) {
         if (count > 0)
           Entries<T, 8>::store(static_cast<typename T::Store *>(g.out.data) + row * g.out.ld + col, count, v);
       } else {
         if (count > 0) Entries<F32, 8>::store(g.parts + (split * g.M + row) * g.N + col, count, v);
       }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
 }
 
 template <typename T, int RM, int RN, ProductOut Out>
@@ -384,14 +394,16 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs g) {
   constexpr int kLds = 2 * kBuffer * 2 > 4 * Slab<W>::kFloats * 4 ? 2 * kBuffer * 2 : 4 * Slab<W>::kFloats * 4;
   __shared__ __attribute__((aligned(16))) uint16_t lds[kLds / 2];
 
-  const Place at = place_of(g, BX, BX);
+  const Place at = place_of(g, turns_of(g.tiles_m * g.tiles_n * g.splits).id, BX, BX);
   const int64_t m0 = at.m0, n0 = at.n0, k0 = at.k0, k1 = at.k1;
   const int steps = static_cast<int>((k1 - k0 + BK - 1) / BK);
 
-  const int wave = threadIdx.x / 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int wm = wave / 2 * W, wn = wave % 2 * W;
   F16x acc[R][R];
-  start<R, R, Out>(g, n0 + wn, acc);
+  float bias[R];
+  load_bias<R, Out>(g, n0 + wn, bias);
+  start<R, R>(bias, acc);
 
   // The last step's chunks may be short: along k where K is no multiple of 8; along m the very last row of memory ends
   // inside its last chunk, of which the hardware's bounds check drops a dword that is only half there.
@@ -470,84 +482,131 @@ struct DirectTile {
       along[i] = chunk * 8;
     }
   }
-  // Starts the loads of a step into the tile at byte `lds` of LDS.  What is past the range reads as zero; so are chunks
-  // past the last k made to.
-  __device__ __forceinline__ void fetch(const Plane &p, int64_t x, int64_t mx, int64_t k, int64_t kx, uint32_t lds) const {
+  // The tile of m from x, of mx, and of k from k, up to kx: uniform, in scalar registers.
+  uint64_t base;
+  int64_t bytes;
+  int left;  // k
+  __device__ __forceinline__ void begin(const Plane &p, int64_t x, int64_t mx, int64_t k, int64_t kx) {
     const int64_t row0 = KMajor ? x : k, col0 = KMajor ? k : x;
     const int64_t rows = (KMajor ? mx : kx) - row0, cols = (KMajor ? kx : mx) - col0;
-    const int64_t bytes = ((rows - 1) * p.ld + cols) * 2;
-    const char *const base = static_cast<const char *>(p.data) + (row0 * p.ld + col0) * 2;
-    const uint64_t b = reinterpret_cast<uint64_t>(base);
-    const U4 range{static_cast<uint32_t>(b), static_cast<uint32_t>(b >> 32) & 0xffffu,
+    base = reinterpret_cast<uint64_t>(p.data) + (row0 * p.ld + col0) * 2;
+    bytes = ((rows - 1) * p.ld + cols) * 2;
+    left = static_cast<int>(kx - k);
+  }
+  // Starts the loads of the next step into the tile at byte `lds` of LDS.  What is past the range reads as zero; so are
+  // chunks past the last k made to.
+  __device__ __forceinline__ void fetch(const Plane &p, uint32_t lds) {
+    const U4 range{static_cast<uint32_t>(base), static_cast<uint32_t>(base >> 32) & 0xffffu,
                    static_cast<uint32_t>(bytes <= 0 ? 0 : bytes > 0x7fffffff ? 0x7fffffff : bytes), 0x00020000u};
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       uint32_t o = off[i];
-      if (KMajor) o = along[i] < cols ? o : kNowhere;
+      if (KMajor) o = along[i] < left ? o : kNowhere;
       // m0 holds where the first lane's bytes land; the load has no destination register
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                    :: "s"(lds + (wave * kLoads + i) * 1024), "v"(o), "s"(range) : "memory");
     }
+    const int64_t move = KMajor ? BK * 2 : static_cast<int64_t>(p.ld) * (BK * 2);
+    base += move;
+    bytes -= move;
+    left -= BK;
   }
 };
 
-// The same product with a ring of kRing tiles: the loads of kRing - 1 steps are under way while a step is computed.
+// The same product with a ring of kDirectRing tiles: while a step is computed the loads of the next two are under way,
+// also across the end of a tile: a workgroup goes from tile to tile, and the next one's loads run while the results of
+// the last are written.
 template <typename T, int BM, int BN, ProductKind Kind, ProductOut Out>
-__global__ __launch_bounds__(256, DB) void direct_product_kernel(const ProductArgs g) {
+__global__ __launch_bounds__(256, 2) void direct_product_kernel(const ProductArgs g) {
   constexpr int BK = kDirectDepth;
   constexpr bool a_k = Kind == kProductForward || Kind == kProductDx, b_k = Kind == kProductForward;
   typedef DirectTile<BM, BK, a_k> TA;
   typedef DirectTile<BN, BK, b_k> TB;
   constexpr int WM = BM / 2, WN = BN / 2, RM = WM / 32, RN = WN / 32, kRing = kDirectRing;
   constexpr int kStep = TA::kBytes + TB::kBytes, kLoads = TA::kLoads + TB::kLoads;
-  constexpr int kLds = kRing * kStep > 4 * Slab<WN>::kFloats * 4 ? kRing * kStep : 4 * Slab<WN>::kFloats * 4;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[kLds / 2];
+  constexpr int kStores = RM * 4;  // of a wavefront for a whole tile, at least
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[kRing * kStep / 2];
+  __shared__ __attribute__((aligned(16))) float slabs[4 * Slab<WN>::kFloats];
 
-  const Place at = place_of(g, BM, BN);
-  const int steps = static_cast<int>((at.k1 - at.k0 + BK - 1) / BK);
-  const int wave = threadIdx.x / 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int wm = wave / 2 * WM, wn = wave % 2 * WN;
-  F16x acc[RM][RN];
-  start<RM, RN, Out>(g, at.n0 + wn, acc);
+  const Turns turns = turns_of(g.tiles_m * g.tiles_n * g.splits);
+  if (turns.id >= turns.end) return;
+  const auto steps_of = [](const Place &p) { return static_cast<int>((p.k1 - p.k0 + BK - 1) / BK); };
 
   const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint16_t *)lds));
   TA a;
   TB b;
   a.init(g.a);
   b.init(g.b);
-  uint32_t into = base;  // where the next step goes
-  const auto fetch = [&](int s) {  // past the last step too, where it loads nothing: the count of loads stays the same
-    const int64_t k = at.k0 + static_cast<int64_t>(s) * BK;
-    a.fetch(g.a, at.m0, g.M, k, at.k1, into);
-    b.fetch(g.b, at.n0, g.N, k, at.k1, into + TA::kBytes);
-    into = into == base + (kRing - 1) * kStep ? base : into + kStep;
+  // The loads run ahead of the computation, over tiles.  After the last tile they load nothing, so that the count of
+  // loads under way stays the same.
+  uint32_t into = base;
+  int turn = turns.id;
+  int to_go;
+  const auto begin = [&]() {
+    const Place p = place_of(g, turn, BM, BN);
+    a.begin(g.a, p.m0, g.M, p.k0, p.k1);
+    b.begin(g.b, p.n0, g.N, p.k0, p.k1);
+    to_go = steps_of(p);
   };
-#pragma unroll
-  for (int s = 0; s < kRing - 1; ++s) fetch(s);
-  const uint16_t *now = lds;
-  for (int s = 0; s < steps; ++s) {
-    // loads end in order: all but those of the kRing - 2 steps after this one.  Then every wavefront's part is there,
-    // and every wavefront is done with the tile before, which the next loads replace.
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((kRing - 2) * kLoads) : "memory");
-    fetch(s + kRing - 1);
-#pragma unroll
-    for (int kk = 0; kk < BK / 16; ++kk) {
-      S8 fa[RM], fb[RN];
-#pragma unroll
-      for (int i = 0; i < RM; ++i) fa[i] = Spread<BM, BK>::template take<a_k>(now, wm + 32 * i, kk);
-#pragma unroll
-      for (int i = 0; i < RN; ++i) fb[i] = Spread<BN, BK>::template take<b_k>(now + TA::kBytes / 2, wn + 32 * i, kk);
-#pragma unroll
-      for (int i = 0; i < RM; ++i)
-#pragma unroll
-        for (int j = 0; j < RN; ++j) acc[i][j] = Cores<T>::mma(fa[i], fb[j], acc[i][j]);
+  const auto fetch = [&]() {
+    a.fetch(g.a, into);
+    b.fetch(g.b, into + TA::kBytes);
+    into = into == base + (kRing - 1) * kStep ? base : into + kStep;
+    if (--to_go <= 0 && turn + turns.step < turns.end) {
+      turn += turns.step;
+      begin();
     }
-    now = now == lds + (kRing - 1) * (kStep / 2) ? lds : now + kStep / 2;
+  };
+  begin();
+#pragma unroll
+  for (int s = 0; s < kRing - 1; ++s) fetch();
+  const uint16_t *now = lds;
+  bool stored = false;  // the wavefront has written a whole tile just before
+  float bias[RN];
+  load_bias<RN, Out>(g, place_of(g, turns.id, BM, BN).n0 + wn, bias);
+  for (int id = turns.id; id < turns.end; id += turns.step) {
+    const Place at = place_of(g, id, BM, BN);
+    const int steps = steps_of(at);
+    F16x acc[RM][RN];
+    start<RM, RN>(bias, acc);
+    if (Out == kForward && id + turns.step < turns.end)
+      load_bias<RN, Out>(g, place_of(g, id + turns.step, BM, BN).n0 + wn, bias);
+    for (int s = 0; s < steps; ++s) {
+      // Loads and stores end in order.  This step's loads are followed by those of kRing - 2 steps and, in the first
+      // steps after a tile, its stores, which need not be waited for.  Then every wavefront's part is there, and every
+      // wavefront is done with the tile before, which the next loads replace.
+      if (stored && s < kRing - 1)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((kRing - 2) * kLoads + kStores) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((kRing - 2) * kLoads) : "memory");
+      S8 fa[BK / 16][RM], fb[BK / 16][RN];
+#pragma unroll
+      for (int kk = 0; kk < BK / 16; ++kk) {
+#pragma unroll
+        for (int i = 0; i < RN; ++i) fb[kk][i] = Spread<BN, BK>::template take<b_k>(now + TA::kBytes / 2, wn + 32 * i, kk);
+#pragma unroll
+        for (int i = 0; i < RM; ++i) fa[kk][i] = Spread<BM, BK>::template take<a_k>(now, wm + 32 * i, kk);
+      }
+      fetch();  // while the reads above are under way
+#pragma unroll
+      for (int kk = 0; kk < BK / 16; ++kk)
+#pragma unroll
+        for (int i = 0; i < RM; ++i)
+#pragma unroll
+          for (int j = 0; j < RN; ++j) acc[i][j] = Cores<T>::mma(fa[kk][i], fb[kk][j], acc[i][j]);
+      now = now == lds + (kRing - 1) * (kStep / 2) ? lds : now + kStep / 2;
+    }
+    // the next tile's bias is waited for here, before the stores: after them it would wait for those too
+#pragma unroll
+    for (int j = 0; j < RN; ++j) asm volatile("" : "+v"(bias[j]));
+    finish<T, RM, RN, Out>(g, acc, slabs + wave * Slab<WN>::kFloats, at.m0 + wm, at.n0 + wn, at.split);
+    stored = WN == 64 && at.m0 + wm + WM <= g.M && at.n0 + wn + WN <= g.N;
   }
-  // no load may land in the slabs, and no wavefront may still read the last tile
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  finish<T, RM, RN, Out>(g, acc, reinterpret_cast<float *>(lds) + wave * Slab<WN>::kFloats, at.m0 + wm, at.n0 + wn, at.split);
+  // no load may land in LDS that is another workgroup's by then
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 template <typename T, TileSize Size, ProductKind Kind, ProductOut Out>
@@ -555,7 +614,8 @@ int launch_one(const ProductArgs &g, hipStream_t st) {
   const unsigned blocks = static_cast<unsigned>(g.tiles_m) * g.tiles_n * g.splits;
   if constexpr (T::kType != GOSH_F32 && Kind != kProductDwPacked) {
     if (g.direct) {
-      direct_product_kernel<T, tile_m(Size), tile_n(Size), Kind, Out><<<dim3(blocks), dim3(256), 0, st>>>(g);
+      const unsigned held = static_cast<unsigned>(resident_waves()) / 16;  // two workgroups a CU
+      direct_product_kernel<T, tile_m(Size), tile_n(Size), Kind, Out><<<dim3(blocks < held ? blocks : held), dim3(256), 0, st>>>(g);
       return check_launch("matrix product");
     }
   }

@@ -77,10 +77,20 @@ int launch_few_rows(const gosh_mat *x, const gosh_mat *w, const ForwardOut &f, h
 
 constexpr int64_t kTilesPerLaunch = int64_t{1} << 22;  // a grid's threads stay below 2^31
 
-// The largest tiles that still give every one of the device's 256 CUs a workgroup.
+// Time of an entry of the result in tiles of one size, against that in the largest: smaller tiles fetch more of the
+// operands for it (and those that pass through registers come in two sizes).
+double weight_of(TileSize s, bool direct) { return s == kLarge ? (direct ? 1.0 : 1e9) : s == kMiddle ? 1.25 : 2.0; }
+
+// The tiles of which the busiest of the device's 256 CUs has the least work.
 TileSize tiles_for(int64_t M, int64_t N, bool direct) {
-  const auto tiles = [&](TileSize s) { return ceil_div(M, tile_m(s)) * ceil_div(N, tile_n(s)); };
-  return direct && tiles(kLarge) >= 256 ? kLarge : tiles(kMiddle) >= 256 ? kMiddle : kSmall;
+  TileSize best = kSmall;
+  double least = 0;
+  for (TileSize s : {kSmall, kMiddle, kLarge}) {
+    const double turns = static_cast<double>(ceil_div(ceil_div(M, tile_m(s)) * ceil_div(N, tile_n(s)), 256));
+    const double work = turns * tile_m(s) * tile_n(s) * weight_of(s, direct);
+    if (s == kSmall || work <= least) best = s, least = work;
+  }
+  return best;
 }
 
 template <typename T>
@@ -107,7 +117,7 @@ int product_of_rows(ProductKind kind, ProductArgs g, int64_t rows, hipStream_t s
   return GOSH_OK;
 }
 
-// How dw is split along the rows: enough workgroups for two on every CU, at least 256 rows each.
+// How dw is split along the rows: enough workgroups for every CU's eight wavefronts, at least 256 rows each.
 struct DwPlan {
   TileSize size;
   int32_t tiles_m, tiles_n, splits;
@@ -115,11 +125,16 @@ struct DwPlan {
 };
 DwPlan plan_dw(int64_t rows, int32_t in, int32_t out, bool direct) {
   DwPlan p;
-  p.size = std::min(in, out) <= 64 ? kSmall : direct && out > 128 ? kLarge : kMiddle;
+  double least = 0;
+  p.size = kSmall;
+  for (TileSize s : {kSmall, kMiddle, kLarge}) {  // splits fill the device whatever the size
+    const double work = static_cast<double>(ceil_div(out, tile_m(s)) * tile_m(s)) * (ceil_div(in, tile_n(s)) * tile_n(s)) * weight_of(s, direct);
+    if (s == kSmall || work <= least) p.size = s, least = work;
+  }
   p.tiles_m = static_cast<int32_t>(ceil_div(out, tile_m(p.size)));
   p.tiles_n = static_cast<int32_t>(ceil_div(in, tile_n(p.size)));
   const int64_t tiles = static_cast<int64_t>(p.tiles_m) * p.tiles_n;
-  const int64_t want = std::min(std::max<int64_t>(1, rows / 256), std::max<int64_t>(1, 512 / tiles));
+  const int64_t want = std::min(std::max<int64_t>(1, rows / 256), std::max<int64_t>(1, (p.size == kLarge ? 256 : 512) / tiles));
   p.k_per_split = ceil_div(ceil_div(std::max<int64_t>(rows, 1), want), 64) * 64;  // a multiple of every tile's depth
   p.splits = static_cast<int32_t>(ceil_div(rows, p.k_per_split));
   return p;

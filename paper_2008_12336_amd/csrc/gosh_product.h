@@ -43,7 +43,7 @@ enum ProductKind : int { kProductForward, kProductDx, kProductDw, kProductDwPack
 
 enum TileSize : int { kSmall, kMiddle, kLarge };  // kLarge: direct products only
 constexpr int tile_m(TileSize s) { return s == kLarge ? 256 : s == kMiddle ? 128 : 64; }
-constexpr int tile_n(TileSize s) { return s == kSmall ? 64 : 128; }
+constexpr int tile_n(TileSize s) { return tile_m(s); }
 
 // Launches for entries of one type; defined in gosh_product_{f32,bf16,f16}.hip.
 template <typename T>
@@ -64,7 +64,8 @@ struct ProductDepth {  // k of a tile that passes through registers: 128 and 64 
 inline bool can_be_direct(const Plane &p, int64_t along) {
   return reinterpret_cast<uintptr_t>(p.data) % 16 == 0 && p.ld % 8 == 0 && along % 8 == 0;
 }
-constexpr int kDirectDepth = 32, kDirectRing = 3;  // k of a tile; tiles in LDS
+constexpr int kDirectDepth = 64, kDirectRing = 2;  // k of a tile; tiles in LDS
+constexpr int direct_waves(int bn) { return bn == 256 ? 8 : 4; }
 inline int product_depth(int32_t type, TileSize size, bool direct) {
   return direct ? kDirectDepth : type == GOSH_F32 ? ProductDepth<F32>::value(size == kSmall) : ProductDepth<Bf16>::value(false);
 }
@@ -462,10 +463,11 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs g) {
 
 // A tile that the memory system writes to LDS by itself, 1 KB an instruction of a wavefront: lane i's 16 bytes land at
 // 16 i, so that the lanes ask for the chunks that belong there.  Rows are 16-byte aligned and whole numbers of chunks.
-template <int BX, int BK, bool KMajor>
+template <int BX, int BK, bool KMajor, int Waves>
 struct DirectTile {
   static constexpr int kBytes = BX * BK * 2;
-  static constexpr int kLoads = kBytes / 1024 / 4;            // of a wavefront
+  static constexpr int kLoads = kBytes / 1024 / Waves;        // of a wavefront
+  static_assert(kBytes % (1024 * Waves) == 0, "");
   static constexpr int kAlong = (KMajor ? BK : BX) / 8;       // chunks in a row of the tile
   uint32_t off[kLoads];
   int along[kLoads];  // first k of the lane's chunks (k-major)
@@ -514,23 +516,25 @@ struct DirectTile {
   }
 };
 
-// The same product with a ring of kDirectRing tiles: while a step is computed the loads of the next two are under way,
+// The same product with a ring of kDirectRing tiles: while a step is computed the loads of the next ones are under way,
 // also across the end of a tile: a workgroup goes from tile to tile, and the next one's loads run while the results of
 // the last are written.
 template <typename T, int BM, int BN, ProductKind Kind, ProductOut Out>
-__global__ __launch_bounds__(256, 2) void direct_product_kernel(const ProductArgs g) {
+__global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void direct_product_kernel(const ProductArgs g) {
   constexpr int BK = kDirectDepth;
   constexpr bool a_k = Kind == kProductForward || Kind == kProductDx, b_k = Kind == kProductForward;
-  typedef DirectTile<BM, BK, a_k> TA;
-  typedef DirectTile<BN, BK, b_k> TB;
-  constexpr int WM = BM / 2, WN = BN / 2, RM = WM / 32, RN = WN / 32, kRing = kDirectRing;
+  constexpr int kWaves = direct_waves(BN), kAcross = kWaves / 2;
+  typedef DirectTile<BM, BK, a_k, kWaves> TA;
+  typedef DirectTile<BN, BK, b_k, kWaves> TB;
+  constexpr int WM = BM / 2, WN = BN / kAcross, RM = WM / 32, RN = WN / 32, kRing = kDirectRing;
   constexpr int kStep = TA::kBytes + TB::kBytes, kLoads = TA::kLoads + TB::kLoads;
   constexpr int kStores = RM * 4;  // of a wavefront for a whole tile, at least
+  static_assert(BK / 16 % 2 == 0, "the entries read ahead are in turns");
   __shared__ __attribute__((aligned(1024))) uint16_t lds[kRing * kStep / 2];
-  __shared__ __attribute__((aligned(16))) float slabs[4 * Slab<WN>::kFloats];
+  __shared__ __attribute__((aligned(16))) float slabs[kWaves * Slab<WN>::kFloats];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int wm = wave / 2 * WM, wn = wave % 2 * WN;
+  const int wm = wave / kAcross * WM, wn = wave % kAcross * WN;
   const Turns turns = turns_of(g.tiles_m * g.tiles_n * g.splits);
   if (turns.id >= turns.end) return;
   const auto steps_of = [](const Place &p) { return static_cast<int>((p.k1 - p.k0 + BK - 1) / BK); };
@@ -562,11 +566,20 @@ __global__ __launch_bounds__(256, 2) void direct_product_kernel(const ProductArg
   };
   begin();
 #pragma unroll
-  for (int s = 0; s < kRing - 1; ++s) fetch();
+  for (int s = 0; s < kRing; ++s) fetch();
   const uint16_t *now = lds;
-  bool stored = false;  // the wavefront has written a whole tile just before
+  S8 fa[2][RM], fb[2][RN];
+  const auto take = [&](int part) {
+#pragma unroll
+    for (int j = 0; j < RN; ++j) fb[part & 1][j] = Spread<BN, BK>::template take<b_k>(now + TA::kBytes / 2, wn + 32 * j, part);
+#pragma unroll
+    for (int i = 0; i < RM; ++i) fa[part & 1][i] = Spread<BM, BK>::template take<a_k>(now, wm + 32 * i, part);
+  };
   float bias[RN];
   load_bias<RN, Out>(g, place_of(g, turns.id, BM, BN).n0 + wn, bias);
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"((kRing - 1) * kLoads) : "memory");
+  take(0);
+  bool stored = false;  // the wavefront has written a whole tile just before
   for (int id = turns.id; id < turns.end; id += turns.step) {
     const Place at = place_of(g, id, BM, BN);
     const int steps = steps_of(at);
@@ -574,30 +587,34 @@ __global__ __launch_bounds__(256, 2) void direct_product_kernel(const ProductArg
     start<RM, RN>(bias, acc);
     if (Out == kForward && id + turns.step < turns.end)
       load_bias<RN, Out>(g, place_of(g, id + turns.step, BM, BN).n0 + wn, bias);
+    const auto multiply = [&](int part) {
+#pragma unroll
+      for (int i = 0; i < RM; ++i)
+#pragma unroll
+        for (int j = 0; j < RN; ++j) acc[i][j] = Cores<T>::mma(fa[part & 1][i], fb[part & 1][j], acc[i][j]);
+    };
     for (int s = 0; s < steps; ++s) {
-      // Loads and stores end in order.  This step's loads are followed by those of kRing - 2 steps and, in the first
+      // Each 16 k of a step are read from LDS while those before are multiplied.
+      constexpr int kParts = BK / 16;
+#pragma unroll
+      for (int part = 0; part < kParts - 1; ++part) {
+        take(part + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(part);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // Loads and stores end in order.  The next step's loads are followed by those of kRing - 2 steps and, in the first
       // steps after a tile, its stores, which need not be waited for.  Then every wavefront's part is there, and every
-      // wavefront is done with the tile before, which the next loads replace.
+      // wavefront is done with this step's tile, which the next loads replace.
       if (stored && s < kRing - 1)
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((kRing - 2) * kLoads + kStores) : "memory");
       else
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((kRing - 2) * kLoads) : "memory");
-      S8 fa[BK / 16][RM], fb[BK / 16][RN];
-#pragma unroll
-      for (int kk = 0; kk < BK / 16; ++kk) {
-#pragma unroll
-        for (int i = 0; i < RN; ++i) fb[kk][i] = Spread<BN, BK>::template take<b_k>(now + TA::kBytes / 2, wn + 32 * i, kk);
-#pragma unroll
-        for (int i = 0; i < RM; ++i) fa[kk][i] = Spread<BM, BK>::template take<a_k>(now, wm + 32 * i, kk);
-      }
-      fetch();  // while the reads above are under way
-#pragma unroll
-      for (int kk = 0; kk < BK / 16; ++kk)
-#pragma unroll
-        for (int i = 0; i < RM; ++i)
-#pragma unroll
-          for (int j = 0; j < RN; ++j) acc[i][j] = Cores<T>::mma(fa[kk][i], fb[kk][j], acc[i][j]);
       now = now == lds + (kRing - 1) * (kStep / 2) ? lds : now + kStep / 2;
+      take(0);
+      fetch();
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(kParts - 1);
     }
     // the next tile's bias is waited for here, before the stores: after them it would wait for those too
 #pragma unroll
@@ -614,8 +631,8 @@ int launch_one(const ProductArgs &g, hipStream_t st) {
   const unsigned blocks = static_cast<unsigned>(g.tiles_m) * g.tiles_n * g.splits;
   if constexpr (T::kType != GOSH_F32 && Kind != kProductDwPacked) {
     if (g.direct) {
-      const unsigned held = static_cast<unsigned>(resident_waves()) / 16;  // two workgroups a CU
-      direct_product_kernel<T, tile_m(Size), tile_n(Size), Kind, Out><<<dim3(blocks < held ? blocks : held), dim3(256), 0, st>>>(g);
+      const unsigned held = static_cast<unsigned>(resident_waves()) / 4 / direct_waves(tile_n(Size));  // eight wavefronts a CU
+      direct_product_kernel<T, tile_m(Size), tile_n(Size), Kind, Out><<<dim3(blocks < held ? blocks : held), dim3(64 * direct_waves(tile_n(Size))), 0, st>>>(g);
       return check_launch("matrix product");
     }
   }

@@ -61,15 +61,17 @@ struct Entries {
   typedef S Vec __attribute__((ext_vector_type(N)));
   typedef Vec Loose __attribute__((aligned(sizeof(S))));
   // The first `count` of N; the others are zero.
+  static __device__ __forceinline__ Vec fetch(const S *p, int count) {
+    if (count >= N) return *reinterpret_cast<const Loose *>(p);
+    Vec x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = i < count ? p[i] : static_cast<S>(0.f);
+    return x;
+  }
   static __device__ __forceinline__ void load(const S *p, int count, float (&v)[N]) {
-    if (count >= N) {
-      const Vec x = *reinterpret_cast<const Loose *>(p);
+    const Vec x = fetch(p, count);
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = T::up(x[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = i < count ? T::up(p[i]) : 0.f;
-    }
+    for (int i = 0; i < N; ++i) v[i] = T::up(x[i]);
   }
   static __device__ __forceinline__ void store(S *p, int count, const float (&v)[N]) {
     if (count >= N) {

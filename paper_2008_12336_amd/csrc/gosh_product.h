@@ -245,9 +245,10 @@ struct Tile {
   }
 };
 
-// 8 entries of a row of z become entries of y.  Full: all of them are there.
+// 8 entries of a row of z become entries of y; r: the residual's.  Full: all of them are there.
 template <typename T, typename A, bool Full>
-__device__ __forceinline__ void put_forward(const ForwardOut &f, int64_t row, int col, int there, float (&v)[8], bool head) {
+__device__ __forceinline__ void put_forward(const ForwardOut &f, int64_t row, int col, int there, float (&v)[8],
+                                            const typename Entries<T, 8>::Vec &r, bool head) {
   typedef typename T::Store S;
   const int count = Full ? 8 : there;
   if (!Full) {
@@ -260,11 +261,9 @@ __device__ __forceinline__ void put_forward(const ForwardOut &f, int64_t row, in
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = A::value(v[i]);
-  if (f.residual.data != nullptr && (Full || count > 0)) {
-    float r[8];
-    Entries<T, 8>::load(static_cast<const S *>(f.residual.data) + row * f.residual.ld + col, count, r);
+  if (f.residual.data != nullptr) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += r[i];
+    for (int i = 0; i < 8; ++i) v[i] += T::up(r[i]);
   }
   if (f.y8.data != nullptr) {
     if (!Full) {
@@ -335,12 +334,32 @@ struct Slab {
 template <typename T, int RM, int RN, ProductOut Out, bool Full, typename A>
 __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[RM][RN], float *slab, int64_t m, int64_t n, int split) {
   constexpr int W = 32 * RN, kLanes = W / 8;  // lanes of a row
+  constexpr bool kFull = Full && kLanes == 8;
+  typedef typename T::Store S;
   const int lane = threadIdx.x & 63;
   const int r = lane / kLanes, c = lane % kLanes * 8;
+  const int col = static_cast<int>(n) + c;
+  const auto count_of = [&](int64_t row) {
+    const int64_t left = r < 8 && row < g.M ? g.N - col : 0;
+    return kFull ? 8 : static_cast<int>(left < 0 ? 0 : left > 8 ? 8 : left);
+  };
+  // the residual of 8 rows is loaded kAhead turns before: by itself each load would be waited for, behind the stores
+  // before it
+  constexpr int kAhead = 2, kTurns = 4 * RM;
+  typename Entries<T, 8>::Vec residual[kAhead + 1];
+  const auto load_residual = [&](int turn) {
+    if (Out != kForward || g.forward.residual.data == nullptr) return;
+    const int64_t row = m + 8 * turn + r;
+    residual[turn % (kAhead + 1)] = Entries<T, 8>::fetch(
+        static_cast<const S *>(g.forward.residual.data) + row * g.forward.residual.ld + col, count_of(row));
+  };
 #pragma unroll
-  for (int i = 0; i < RM; ++i)
+  for (int turn = 0; turn < kAhead; ++turn) load_residual(turn);
+#pragma unroll
+  for (int i = 0; i < RM; ++i) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
+      if (4 * i + q + kAhead < kTurns) load_residual(4 * i + q + kAhead);
 #pragma unroll
       for (int j = 0; j < RN; ++j)
 #pragma unroll
@@ -348,9 +367,7 @@ __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[R
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
       const int64_t row = m + 32 * i + 8 * q + r;
-      const int col = static_cast<int>(n) + c;
-      const int64_t left = r < 8 && row < g.M ? g.N - col : 0;
-      const int count = Full && kLanes == 8 ? 8 : static_cast<int>(left < 0 ? 0 : left > 8 ? 8 : left);
+      const int count = count_of(row);
       float v[8];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -359,16 +376,16 @@ __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[R
         for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
       }
       if constexpr (Out == kForward) {
-        put_forward<T, A, Full && kLanes == 8>(g.forward, row, col, count, v, (lane & 3) == 0);
+        put_forward<T, A, kFull>(g.forward, row, col, count, v, residual[(4 * i + q) % (kAhead + 1)], (lane & 3) == 0);
       } else if constexpr (Out == kStore) {
-        if (count > 0)
-          Entries<T, 8>::store(static_cast<typename T::Store *>(g.out.data) + row * g.out.ld + col, count, v);
+        if (count > 0) Entries<T, 8>::store(static_cast<S *>(g.out.data) + row * g.out.ld + col, count, v);
       } else {
         if (count > 0) Entries<F32, 8>::store(g.parts + (split * g.M + row) * g.N + col, count, v);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
+  }
 }
 
 template <typename T, int RM, int RN, ProductOut Out>

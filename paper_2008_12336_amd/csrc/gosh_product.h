@@ -9,8 +9,7 @@
 // 32-bit entries are taken apart into three bf16 parts, x = h + m + l, each the nearest to what the ones before leave
 // (|m| <= 2^-9 |x|, |l| <= 2^-18 |x|, nothing is left), and their products summed as hh + hm + mh + hl + mm + lh in the
 // 32-bit accumulators: what is left out is 2^-26 of a product, less than 32 bits round it by.  Six bf16 products of the
-// matrix cores take three eighths of the time of one in 32 bits.  An infinity has no parts but itself, and meets zeros
-// among the other factor's: it gives NaN.
+// matrix cores take three eighths of the time of one in 32 bits.  What an infinity leaves is NaN.
 #pragma once
 
 #include <type_traits>
@@ -228,13 +227,14 @@ struct Tile {
           float x[2] = {__uint_as_float(raw[i][j]), __uint_as_float(raw[i][j + 1])};
 #pragma unroll
           for (int p = 0; p < 3; ++p) {
-            const uint32_t two = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(x[0]))) |
-                                 static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(x[1]))) << 16;
+            typedef float Two __attribute__((ext_vector_type(2)));
+            typedef __bf16 Near __attribute__((ext_vector_type(2)));
+            const uint32_t two = __builtin_bit_cast(uint32_t, __builtin_convertvector((Two{x[0], x[1]}), Near));
             part[p][j / 2] = two;
             if (p == 2) break;
             const float near[2] = {__uint_as_float(two << 16), __uint_as_float(two & 0xffff0000u)};
 #pragma unroll
-            for (int s = 0; s < 2; ++s) x[s] = __builtin_isinf(near[s]) ? 0.f : x[s] - near[s];  // exact
+            for (int s = 0; s < 2; ++s) x[s] -= near[s];  // exact
           }
         }
 #pragma unroll
@@ -245,34 +245,38 @@ struct Tile {
   }
 };
 
-// 8 entries of a row of z become entries of y; r: the residual's.  Full: all of them are there.
-template <typename T, typename A, bool Full>
-__device__ __forceinline__ void put_forward(const ForwardOut &f, int64_t row, int col, int there, float (&v)[8],
-                                            const typename Entries<T, 8>::Vec &r, bool head) {
+// E entries of a row of z become entries of y; r: the residual's.  Full: all of them are there.
+template <typename T, int E, bool Full>
+__device__ __forceinline__ void put_forward(const ForwardOut &f, int64_t row, int col, int there, float (&v)[E],
+                                            const typename Entries<T, E>::Vec &r) {
   typedef typename T::Store S;
-  const int count = Full ? 8 : there;
+  constexpr int kLanes = kGroup / E;  // of a group of the 8-bit form
+  const bool head = threadIdx.x % kLanes == 0;
+  const int count = Full ? E : there;
   if (!Full) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < count ? v[i] : 0.f;  // entries that are not there count in no group
+    for (int i = 0; i < E; ++i) v[i] = i < count ? v[i] : 0.f;  // entries that are not there count in no group
   }
   if (f.z.data != nullptr) {
-    if (f.z_packed) store_packed<T, 8>(f.z, row, col, count, v, head, 4);
-    else if (Full || count > 0) Entries<T, 8>::store(static_cast<S *>(f.z.data) + row * f.z.ld + col, count, v);
+    if (f.z_packed) store_packed<T, E>(f.z, row, col, count, v, head, kLanes);
+    else if (Full || count > 0) Entries<T, E>::store(static_cast<S *>(f.z.data) + row * f.z.ld + col, count, v);
   }
+  with_activation(f.act, [&](auto a) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = A::value(v[i]);
+    for (int i = 0; i < E; ++i) v[i] = decltype(a)::value(v[i]);
+  });
   if (f.residual.data != nullptr) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += T::up(r[i]);
+    for (int i = 0; i < E; ++i) v[i] += T::up(r[i]);
   }
   if (f.y8.data != nullptr) {
     if (!Full) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < count ? v[i] : 0.f;
+      for (int i = 0; i < E; ++i) v[i] = i < count ? v[i] : 0.f;
     }
-    store_packed<T, 8>(f.y8, row, col, count, v, head, 4);
+    store_packed<T, E>(f.y8, row, col, count, v, head, kLanes);
   }
-  if (Full || count > 0) Entries<T, 8>::store(static_cast<S *>(f.y.data) + row * f.y.ld + col, count, v);
+  if (Full || count > 0) Entries<T, E>::store(static_cast<S *>(f.y.data) + row * f.y.ld + col, count, v);
 }
 
 // The id-th tile.
@@ -331,72 +335,72 @@ struct Slab {
 
 // The accumulators of a wavefront, at m, n, to where they go, 8 rows at a time through its slab: a lane of the
 // accumulators holds entries of one column.
-template <typename T, int RM, int RN, ProductOut Out, bool Full, typename A>
+template <typename T, int RM, int RN, ProductOut Out, bool Full>
 __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[RM][RN], float *slab, int64_t m, int64_t n, int split) {
-  constexpr int W = 32 * RN, kLanes = W / 8;  // lanes of a row
-  constexpr bool kFull = Full && kLanes == 8;
+  constexpr int W = 32 * RN;
+  constexpr int E = Out == kParts || T::kType == GOSH_F32 ? 4 : 8;  // 16 bytes of a row to a lane
+  constexpr int kLanes = W / E, kRows = 64 / kLanes < 8 ? 64 / kLanes : 8;  // lanes of a row, rows at a time
+  constexpr bool kFull = Full && kLanes * kRows == 64;
   typedef typename T::Store S;
   const int lane = threadIdx.x & 63;
-  const int r = lane / kLanes, c = lane % kLanes * 8;
+  const int r = lane / kLanes, c = lane % kLanes * E;
   const int col = static_cast<int>(n) + c;
   const auto count_of = [&](int64_t row) {
-    const int64_t left = r < 8 && row < g.M ? g.N - col : 0;
-    return kFull ? 8 : static_cast<int>(left < 0 ? 0 : left > 8 ? 8 : left);
+    const int64_t left = r < kRows && row < g.M ? g.N - col : 0;
+    return kFull ? E : static_cast<int>(left < 0 ? 0 : left > E ? E : left);
   };
-  // the residual of 8 rows is loaded kAhead turns before: by itself each load would be waited for, behind the stores
+  // the residual of some rows is loaded kAhead turns before: by itself each load would be waited for, behind the stores
   // before it
-  constexpr int kAhead = 2, kTurns = 4 * RM;
-  typename Entries<T, 8>::Vec residual[kAhead + 1];
+  constexpr int kAhead = 2, kTurns = 32 / kRows * RM;
+  typename Entries<T, E>::Vec residual[kAhead + 1];
   const auto load_residual = [&](int turn) {
     if (Out != kForward || g.forward.residual.data == nullptr) return;
-    const int64_t row = m + 8 * turn + r;
-    residual[turn % (kAhead + 1)] = Entries<T, 8>::fetch(
+    const int64_t row = m + kRows * turn + r;
+    residual[turn % (kAhead + 1)] = Entries<T, E>::fetch(
         static_cast<const S *>(g.forward.residual.data) + row * g.forward.residual.ld + col, count_of(row));
   };
 #pragma unroll
   for (int turn = 0; turn < kAhead; ++turn) load_residual(turn);
 #pragma unroll
-  for (int i = 0; i < RM; ++i) {
+  for (int i = 0; i < RM; ++i)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      if (4 * i + q + kAhead < kTurns) load_residual(4 * i + q + kAhead);
 #pragma unroll
       for (int j = 0; j < RN; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) slab[Slab<W>::at(4 * (lane >> 5) + e, 32 * j + (lane & 31))] = acc[i][j][4 * q + e];
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      const int64_t row = m + 32 * i + 8 * q + r;
-      const int count = count_of(row);
-      float v[8];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const F4 x = *reinterpret_cast<const F4 *>(slab + Slab<W>::at(r & 7, c + 4 * h));
+      for (int h = 0; h < 8 / kRows; ++h) {
+        const int turn = (4 * i + q) * (8 / kRows) + h;
+        if (turn + kAhead < kTurns) load_residual(turn + kAhead);
+        const int64_t row = m + kRows * turn + r;
+        const int count = count_of(row);
+        float v[E];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
-      }
-      if constexpr (Out == kForward) {
-        put_forward<T, A, kFull>(g.forward, row, col, count, v, residual[(4 * i + q) % (kAhead + 1)], (lane & 3) == 0);
-      } else if constexpr (Out == kStore) {
-        if (count > 0) Entries<T, 8>::store(static_cast<S *>(g.out.data) + row * g.out.ld + col, count, v);
-      } else {
-        if (count > 0) Entries<F32, 8>::store(g.parts + (split * g.M + row) * g.N + col, count, v);
+        for (int w = 0; w < E; w += 4) {
+          const F4 x = *reinterpret_cast<const F4 *>(slab + Slab<W>::at((kRows * h + r) & 7, c + w));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[w + e] = x[e];
+        }
+        if constexpr (Out == kForward) {
+          put_forward<T, E, kFull>(g.forward, row, col, count, v, residual[turn % (kAhead + 1)]);
+        } else if constexpr (Out == kStore) {
+          if (count > 0) Entries<T, E>::store(static_cast<S *>(g.out.data) + row * g.out.ld + col, count, v);
+        } else {
+          if (count > 0) Entries<F32, E>::store(g.parts + (split * g.M + row) * g.N + col, count, v);
+        }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
-  }
 }
 
 template <typename T, int RM, int RN, ProductOut Out>
 __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[RM][RN], float *slab, int64_t m, int64_t n, int split) {
-  const auto with = [&](auto a) {
-    typedef decltype(a) A;
-    if (m + 32 * RM <= g.M && n + 32 * RN <= g.N) finish<T, RM, RN, Out, true, A>(g, acc, slab, m, n, split);
-    else finish<T, RM, RN, Out, false, A>(g, acc, slab, m, n, split);
-  };
-  if constexpr (Out == kForward) with_activation(g.forward.act, with);
-  else with(Activation<GOSH_ACT_NONE>{});
+  if (m + 32 * RM <= g.M && n + 32 * RN <= g.N) finish<T, RM, RN, Out, true>(g, acc, slab, m, n, split);
+  else finish<T, RM, RN, Out, false>(g, acc, slab, m, n, split);
 }
 
 // Tiles that pass through registers on their way to LDS: 32-bit entries, packed ones, and matrices whose rows are not

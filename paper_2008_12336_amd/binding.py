@@ -179,8 +179,13 @@ def _check(rc: int, stats=None) -> None:
         raise GoshError(rc, lib().gosh_last_error().decode(), stats() if (stats and rc == GOSH_EDIVERGED) else None)
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
     if stream is None:
+        if _raw_stream is not None and torch.cuda.is_initialized():  # 2 us less than making a Stream object
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 

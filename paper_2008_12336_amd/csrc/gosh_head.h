@@ -21,10 +21,16 @@ int check_shape(const gosh_mat *m, const char *what, int64_t rows, int32_t cols)
 int check_type(const gosh_mat *m, const char *what, int32_t type);
 int check_floats(const float *p, int64_t count, const char *what, bool optional);
 int check_workspace(const void *p, uint64_t have, uint64_t need);
-// Sums `parts` arrays of n floats, each `stride` floats after the one before, in ascending order within fixed groups
-// (the same bits every time), into out (float, or `type`), n = rows x cols with rows of ld entries.
-int join_parts(const float *parts, int count, int64_t stride, int64_t rows, int32_t cols, void *out, int64_t ld,
-               int32_t type, hipStream_t st);
+// Up to two sums of partial results in one launch.  A job sums `count` arrays of n floats, each `stride` floats after the
+// one before, in an order that depends on these numbers alone (the same bits every time), into out: rows of `cols`
+// entries of `type`, ld apart.
+struct JoinJob {
+  const float *parts;
+  int64_t stride, n, ld;
+  void *out;
+  int32_t count, cols, type;
+};
+int join_parts(const JoinJob *jobs, int how_many, hipStream_t st);
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 

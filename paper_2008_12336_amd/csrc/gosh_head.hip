@@ -76,46 +76,53 @@ __device__ __forceinline__ void store_sum(float sum, int64_t i, int32_t cols, vo
   else static_cast<_Float16 *>(out)[to] = static_cast<_Float16>(sum);
 }
 
-// A thread per entry.
-__global__ __launch_bounds__(256) void join_kernel(const float *parts, int count, int64_t stride, int64_t n, int32_t cols,
-                                                   void *out, int64_t ld, int32_t type) {
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
-    float sum = 0.f;
-#pragma unroll 8
-    for (int s = 0; s < count; ++s) sum += parts[s * stride + i];
-    store_sum(sum, i, cols, out, ld, type);
-  }
-}
+struct JoinJobs {
+  JoinJob job[2];
+  unsigned blocks;  // of the first job
+};
 
-// 16 threads per entry, each with every 16th part.
-__global__ __launch_bounds__(256) void join_few_kernel(const float *parts, int count, int64_t stride, int64_t n, int32_t cols,
-                                                       void *out, int64_t ld, int32_t type) {
+// Few entries have few threads to sum their many parts: 16 share them then.
+__host__ __device__ inline bool shared(const JoinJob &j) { return j.n <= 16384 && j.count > 16; }
+
+__global__ __launch_bounds__(256) void join_kernel(const JoinJobs jobs) {
+  const bool first = blockIdx.x < jobs.blocks;
+  const JoinJob &j = jobs.job[first ? 0 : 1];
+  const int64_t block = first ? blockIdx.x : blockIdx.x - jobs.blocks;
+  if (!shared(j)) {
+    const int64_t step = static_cast<int64_t>(first ? jobs.blocks : gridDim.x - jobs.blocks) * 256;
+    for (int64_t i = block * 256 + threadIdx.x; i < j.n; i += step) {
+      float sum = 0.f;
+#pragma unroll 8
+      for (int s = 0; s < j.count; ++s) sum += j.parts[s * j.stride + i];
+      store_sum(sum, i, j.cols, j.out, j.ld, j.type);
+    }
+    return;
+  }
   __shared__ float lds[256];
   const int x = threadIdx.x % 16, y = threadIdx.x / 16;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 16 + x;
+  const int64_t i = block * 16 + x;
   float sum = 0.f;
-  if (i < n)
+  if (i < j.n)
 #pragma unroll 8
-    for (int s = y; s < count; s += 16) sum += parts[s * stride + i];
+    for (int s = y; s < j.count; s += 16) sum += j.parts[s * j.stride + i];
   lds[threadIdx.x] = sum;
   __syncthreads();
-  if (y != 0 || i >= n) return;
+  if (y != 0 || i >= j.n) return;
 #pragma unroll
   for (int s = 1; s < 16; ++s) sum += lds[s * 16 + x];
-  store_sum(sum, i, cols, out, ld, type);
+  store_sum(sum, i, j.cols, j.out, j.ld, j.type);
 }
 
 }  // namespace
 
-int join_parts(const float *parts, int count, int64_t stride, int64_t rows, int32_t cols, void *out, int64_t ld,
-               int32_t type, hipStream_t st) {
-  const int64_t n = rows * cols;
-  // few entries have few threads to sum their many parts: 16 share them
-  if (n <= 16384 && count > 16)
-    join_few_kernel<<<dim3(static_cast<unsigned>(ceil_div(n, 16))), dim3(256), 0, st>>>(parts, count, stride, n, cols, out, ld, type);
-  else
-    join_kernel<<<dim3(static_cast<unsigned>(std::min<int64_t>(ceil_div(n, 256), 1 << 20))), dim3(256), 0, st>>>(
-        parts, count, stride, n, cols, out, ld, type);
+int join_parts(const JoinJob *jobs, int how_many, hipStream_t st) {
+  if (how_many == 0) return GOSH_OK;
+  const auto blocks = [](const JoinJob &j) {
+    return static_cast<unsigned>(std::min<int64_t>(ceil_div(j.n, shared(j) ? 16 : 256), 1 << 20));
+  };
+  JoinJobs all{{jobs[0], jobs[how_many - 1]}, blocks(jobs[0])};
+  const unsigned grid = all.blocks + (how_many > 1 ? blocks(jobs[1]) : 0);
+  join_kernel<<<dim3(grid), dim3(256), 0, st>>>(all);
   return check_launch("sum of parts");
 }
 

@@ -238,8 +238,9 @@ int linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, co
         db != nullptr ? db_parts : nullptr, rows, out, p.slope.shift, p.slope.rows_per_block);
     if (int rc = check_launch("gradient of the activation")) return rc;
   }
-  if (db != nullptr)
-    if (int rc = join_parts(db_parts, static_cast<int>(p.slope.blocks_y), out, 1, out, db, out, GOSH_F32, st)) return rc;
+  JoinJob jobs[2];
+  int sums = 0;
+  if (db != nullptr) jobs[sums++] = {db_parts, out, out, out, db, static_cast<int32_t>(p.slope.blocks_y), out, GOSH_F32};
   if (dx != nullptr && rows > 0) {
     ProductArgs g{};
     g.a = dz;
@@ -266,9 +267,10 @@ int linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, co
       g.parts = dw_parts;
       if (int rc = launch_product<T>(x->packed ? kProductDwPacked : kProductDw, d.size, g, st)) return rc;
     }
-    if (int rc = join_parts(dw_parts, d.splits, static_cast<int64_t>(out) * in, out, in, dw->data, dw->ld, dw->type, st)) return rc;
+    const int64_t n = static_cast<int64_t>(out) * in;
+    jobs[sums++] = {dw_parts, n, n, dw->ld, dw->data, d.splits, in, dw->type};
   }
-  return GOSH_OK;
+  return join_parts(jobs, sums, st);
 }
 
 }  // namespace

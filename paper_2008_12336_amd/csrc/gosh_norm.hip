@@ -425,8 +425,9 @@ int norm_back(NormBackArgs g, float *dgamma, float *dbeta, hipStream_t st) {
   if (dgamma != nullptr) {
     const int64_t stride = 2 * static_cast<int64_t>(g.cols);
     const int count = static_cast<int>(parts);
-    if (int rc = join_parts(g.parts, count, stride, 1, g.cols, dgamma, g.cols, GOSH_F32, st)) return rc;
-    return join_parts(g.parts + g.cols, count, stride, 1, g.cols, dbeta, g.cols, GOSH_F32, st);
+    const JoinJob jobs[2] = {{g.parts, stride, g.cols, g.cols, dgamma, count, g.cols, GOSH_F32},
+                             {g.parts + g.cols, stride, g.cols, g.cols, dbeta, count, g.cols, GOSH_F32}};
+    return join_parts(jobs, 2, st);
   }
   return GOSH_OK;
 }

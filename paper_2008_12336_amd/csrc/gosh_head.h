@@ -59,20 +59,121 @@ struct F16 {
   static __device__ __forceinline__ _Float16 down(float v) { return static_cast<_Float16>(v); }
 };
 
-// N entries in a row of memory that is aligned to one of them only: the hardware takes 128-bit accesses at any
-// multiple of an entry's size, so there is no second path for odd strides.
+// Memory that need not be aligned to what is read from it: the hardware takes accesses of up to 128 bits at any multiple
+// of an entry's size, so there is no second path for odd strides.
+template <typename U, int Align>
+struct Loosely {
+  typedef U At __attribute__((aligned(Align)));
+};
+template <int N>
+struct Words {
+  typedef uint32_t V __attribute__((ext_vector_type(N)));
+};
+template <>
+struct Words<1> {
+  typedef uint32_t V;
+};
+
+// `Bytes` bytes at p (aligned to Align) of which the first `there` are loaded, in pieces of powers of two (never past
+// them); the others are zero.  Likewise the store.
+template <int Bytes, int Align>
+struct Span {
+  static constexpr int kWords = Bytes / 4;
+  typedef typename Words<kWords>::V V;
+  typedef typename Loosely<uint16_t, Align>::At Half;
+  typedef typename Loosely<uint32_t, Align>::At One;
+  typedef typename Loosely<typename Words<2>::V, Align>::At Two;
+  typedef typename Loosely<typename Words<4>::V, Align>::At Four;
+
+  static __device__ __forceinline__ V load(const void *p, int there) {
+    const char *const c = static_cast<const char *>(p);
+    if (there >= Bytes) {
+      if constexpr (kWords <= 4) {
+        return *reinterpret_cast<const typename Loosely<V, Align>::At *>(p);
+      } else {
+        const Four lo = *reinterpret_cast<const Four *>(p), hi = *reinterpret_cast<const Four *>(c + 16);
+        return V{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      }
+    }
+    there = there < 0 ? 0 : there;
+    // all loads first
+    typename Words<4>::V w4 = 0;
+    typename Words<2>::V w2 = 0;
+    uint32_t w1 = 0, half = 0, low = 0;
+    if constexpr (kWords > 4)
+      if (there & 16) w4 = *reinterpret_cast<const Four *>(c);
+    if constexpr (kWords > 2)
+      if (there & 8) w2 = *reinterpret_cast<const Two *>(c + (there & ~15));
+    if constexpr (kWords > 1)
+      if (there & 4) w1 = *reinterpret_cast<const One *>(c + (there & ~7));
+    if constexpr (Align <= 2)
+      if (there & 2) half = *reinterpret_cast<const Half *>(c + (there & ~3));
+    if constexpr (Align <= 1)
+      if (there & 1) low = static_cast<uint8_t>(c[there & ~1]);
+    const uint32_t last = Align <= 2 && (there & 2) ? half | low << 16 : low;
+    if constexpr (kWords == 1) {
+      return last;
+    } else if constexpr (kWords == 2) {
+      return (there & 4) ? V{w1, last} : V{last, 0};
+    } else {
+      const uint32_t a = (there & 4) ? w1 : last, b = (there & 4) ? last : 0;
+      if constexpr (kWords == 4) {
+        return (there & 8) ? V{w2[0], w2[1], a, b} : V{a, b, 0, 0};
+      } else {
+        const uint32_t d = (there & 8) ? w2[0] : a, e = (there & 8) ? w2[1] : b;
+        const uint32_t f = (there & 8) ? a : 0, g = (there & 8) ? b : 0;
+        return (there & 16) ? V{w4[0], w4[1], w4[2], w4[3], d, e, f, g} : V{d, e, f, g, 0, 0, 0, 0};
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(void *p, int there, V u) {
+    char *c = static_cast<char *>(p);
+    if (there >= Bytes) {
+      if constexpr (kWords <= 4) {
+        *reinterpret_cast<typename Loosely<V, Align>::At *>(p) = u;
+      } else {
+        *reinterpret_cast<Four *>(p) = Four{u[0], u[1], u[2], u[3]};
+        *reinterpret_cast<Four *>(c + 16) = Four{u[4], u[5], u[6], u[7]};
+      }
+      return;
+    }
+    there = there < 0 ? 0 : there;
+    uint32_t a, b = 0;  // the words of which a part is there, as pieces are taken off
+    if constexpr (kWords == 1) {
+      a = u;
+    } else {
+      a = u[0], b = u[1];
+      uint32_t d = 0, e = 0;
+      if constexpr (kWords >= 4) d = u[2], e = u[3];
+      if constexpr (kWords > 4) {
+        if (there & 16) *reinterpret_cast<Four *>(c) = Four{u[0], u[1], u[2], u[3]};
+        if (there & 16) a = u[4], b = u[5], d = u[6], e = u[7];
+      }
+      if constexpr (kWords > 2) {
+        if (there & 8) *reinterpret_cast<Two *>(c + (there & ~15)) = Two{a, b};
+        if (there & 8) a = d, b = e;
+      }
+      if (there & 4) *reinterpret_cast<One *>(c + (there & ~7)) = a;
+      if (there & 4) a = b;
+    }
+    if constexpr (Align <= 2) {
+      if (there & 2) *reinterpret_cast<Half *>(c + (there & ~3)) = static_cast<uint16_t>(a);
+      if (there & 2) a >>= 16;
+    }
+    if constexpr (Align <= 1)
+      if (there & 1) c[there & ~1] = static_cast<char>(a);
+  }
+};
+
+// N entries in a row of memory.
 template <typename T, int N>
 struct Entries {
   typedef typename T::Store S;
   typedef S Vec __attribute__((ext_vector_type(N)));
-  typedef Vec Loose __attribute__((aligned(sizeof(S))));
+  typedef Span<N * sizeof(S), sizeof(S)> Memory;
   // The first `count` of N; the others are zero.
   static __device__ __forceinline__ Vec fetch(const S *p, int count) {
-    if (count >= N) return *reinterpret_cast<const Loose *>(p);
-    Vec x;
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = i < count ? p[i] : static_cast<S>(0.f);
-    return x;
+    return __builtin_bit_cast(Vec, Memory::load(p, count * static_cast<int>(sizeof(S))));
   }
   static __device__ __forceinline__ void load(const S *p, int count, float (&v)[N]) {
     const Vec x = fetch(p, count);
@@ -80,16 +181,10 @@ struct Entries {
     for (int i = 0; i < N; ++i) v[i] = T::up(x[i]);
   }
   static __device__ __forceinline__ void store(S *p, int count, const float (&v)[N]) {
-    if (count >= N) {
-      Vec x;
+    Vec x;
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = T::down(v[i]);
-      *reinterpret_cast<Loose *>(p) = x;
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (i < count) p[i] = T::down(v[i]);
-    }
+    for (int i = 0; i < N; ++i) x[i] = T::down(v[i]);
+    Memory::store(p, count * static_cast<int>(sizeof(S)), __builtin_bit_cast(typename Memory::V, x));
   }
 };
 
@@ -157,33 +252,16 @@ __device__ __forceinline__ uint32_t most_bits(const float (&v)[N], int lanes) {
 // count of N bytes at p (any alignment).
 template <int N>
 __device__ __forceinline__ void store_bytes(int8_t *p, int count, const uint32_t (&q)[N / 4]) {
-  typedef uint32_t W __attribute__((ext_vector_type(N / 4)));
-  typedef W Loose __attribute__((aligned(1)));
-  if (count >= N) {
-    W w;
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) w[i] = q[i];
-    *reinterpret_cast<Loose *>(p) = w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < count) p[i] = static_cast<int8_t>(q[i / 4] >> (8 * (i % 4)));
-  }
+  if constexpr (N == 4) Span<4, 1>::store(p, count, q[0]);
+  else Span<8, 1>::store(p, count, U2{q[0], q[1]});
 }
 template <int N>
 __device__ __forceinline__ void load_bytes(const int8_t *p, int count, uint32_t (&q)[N / 4]) {
-  typedef uint32_t W __attribute__((ext_vector_type(N / 4)));
-  typedef W Loose __attribute__((aligned(1)));
-  if (count >= N) {
-    const W w = *reinterpret_cast<const Loose *>(p);
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) q[i] = w[i];
+  if constexpr (N == 4) {
+    q[0] = Span<4, 1>::load(p, count);
   } else {
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) q[i] = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < count) q[i / 4] |= static_cast<uint32_t>(static_cast<uint8_t>(p[i])) << (8 * (i % 4));
+    const U2 w = Span<8, 1>::load(p, count);
+    q[0] = w[0], q[1] = w[1];
   }
 }
 template <int N>

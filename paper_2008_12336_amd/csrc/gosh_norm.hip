@@ -333,8 +333,7 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const NormBackArgs g, in
   Entries<F32, E>::store(part + g.cols + col, count, dbeta);
 }
 
-constexpr int kPartRows = 64;                          // rows a sum of the gradient takes in at least
-constexpr int kMostParts = 1024;
+constexpr int kMostParts = 1024;  // workgroups of the gradient, each of which leaves sums of its rows: 16 wavefronts a CU
 
 // Shape of the lanes for one row: L lanes of C chunks of 16 bytes; C = 0 for rows that registers do not hold.
 struct RowShape {
@@ -354,10 +353,8 @@ RowShape shape_of(int32_t cols, int32_t type) {
   return {256, 0};
 }
 
-// Workgroups of the gradient: each leaves sums of its rows.
-int64_t back_blocks(int64_t rows, int32_t cols) {
-  return std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, kPartRows), kMostParts));
-}
+// A few rows get a workgroup each turn of 4 rows (the sums of 4 rows are more bytes than half of what the rows read).
+int64_t back_blocks(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 4), kMostParts)); }
 
 template <typename T, typename F>
 int with_shape(RowShape s, F f) {
@@ -406,7 +403,7 @@ int norm_back(NormBackArgs g, float *dgamma, float *dbeta, hipStream_t st) {
   if (g.rows > 0) {
     if (s.C == 0) {
       if (g.parts != nullptr) {  // first: dx may be dy
-        const int64_t per = ceil_div(g.rows, back_blocks(g.rows, g.cols));
+        const int64_t per = ceil_div(g.rows, back_blocks(g.rows));
         parts = ceil_div(g.rows, per);
         const unsigned across = static_cast<unsigned>(ceil_div(g.cols, 256 * Chunk<T>::E));
         norm_sums_kernel<T><<<dim3(across, static_cast<unsigned>(parts)), dim3(256), 0, st>>>(g, per);
@@ -415,7 +412,7 @@ int norm_back(NormBackArgs g, float *dgamma, float *dbeta, hipStream_t st) {
       if (g.dx.data != nullptr)
         norm_back_long_kernel<T><<<dim3(static_cast<unsigned>(std::min<int64_t>(g.rows, 2048))), dim3(256), 0, st>>>(g);
     } else {
-      parts = back_blocks(g.rows, g.cols);
+      parts = back_blocks(g.rows);
       with_shape<T>(s, [&](auto L, auto C) {
         norm_back_kernel<T, decltype(L)::value, decltype(C)::value><<<dim3(static_cast<unsigned>(parts)), dim3(256), 0, st>>>(g);
       });
@@ -464,7 +461,7 @@ int gosh_layer_norm(const gosh_mat *x, const float *gamma, const float *beta, fl
 
 uint64_t gosh_layer_norm_workspace(int64_t rows, int32_t cols) {
   if (rows < 1 || cols < 1 || cols > GOSH_MAT_MAX_COLS) return 0;
-  return static_cast<uint64_t>(gosh::back_blocks(rows, cols)) * 2 * cols * 4;
+  return static_cast<uint64_t>(gosh::back_blocks(rows)) * 2 * cols * 4;
 }
 
 int gosh_layer_norm_backward(const gosh_mat *dy, const gosh_mat *x, const float *gamma, const float *mean,

@@ -21,7 +21,7 @@ int check_shape(const gosh_mat *m, const char *what, int64_t rows, int32_t cols)
 int check_type(const gosh_mat *m, const char *what, int32_t type);
 int check_floats(const float *p, int64_t count, const char *what, bool optional);
 int check_workspace(const void *p, uint64_t have, uint64_t need);
-// Up to two sums of partial results in one launch.  A job sums `count` arrays of n floats, each `stride` floats after the
+// Up to three sums of partial results in one launch.  A job sums `count` arrays of n floats, each `stride` floats after the
 // one before, in an order that depends on these numbers alone (the same bits every time), into out: rows of `cols`
 // entries of `type`, ld apart.
 struct JoinJob {

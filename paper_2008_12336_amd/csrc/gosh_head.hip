@@ -76,20 +76,21 @@ __device__ __forceinline__ void store_sum(float sum, int64_t i, int32_t cols, vo
   else static_cast<_Float16 *>(out)[to] = static_cast<_Float16>(sum);
 }
 
+constexpr int kMostJobs = 3;
 struct JoinJobs {
-  JoinJob job[2];
-  unsigned blocks;  // of the first job
+  JoinJob job[kMostJobs];
+  unsigned first[kMostJobs + 1];  // workgroup of each job; the last: how many there are
 };
 
 // Few entries have few threads to sum their many parts: 16 share them then.
 __host__ __device__ inline bool shared(const JoinJob &j) { return j.n <= 16384 && j.count > 16; }
 
 __global__ __launch_bounds__(256) void join_kernel(const JoinJobs jobs) {
-  const bool first = blockIdx.x < jobs.blocks;
-  const JoinJob &j = jobs.job[first ? 0 : 1];
-  const int64_t block = first ? blockIdx.x : blockIdx.x - jobs.blocks;
+  const int which = blockIdx.x < jobs.first[1] ? 0 : blockIdx.x < jobs.first[2] ? 1 : 2;
+  const JoinJob &j = jobs.job[which];
+  const int64_t block = blockIdx.x - jobs.first[which];
   if (!shared(j)) {
-    const int64_t step = static_cast<int64_t>(first ? jobs.blocks : gridDim.x - jobs.blocks) * 256;
+    const int64_t step = static_cast<int64_t>(jobs.first[which + 1] - jobs.first[which]) * 256;
     for (int64_t i = block * 256 + threadIdx.x; i < j.n; i += step) {
       float sum = 0.f;
 #pragma unroll 8
@@ -120,9 +121,12 @@ int join_parts(const JoinJob *jobs, int how_many, hipStream_t st) {
   const auto blocks = [](const JoinJob &j) {
     return static_cast<unsigned>(std::min<int64_t>(ceil_div(j.n, shared(j) ? 16 : 256), 1 << 20));
   };
-  JoinJobs all{{jobs[0], jobs[how_many - 1]}, blocks(jobs[0])};
-  const unsigned grid = all.blocks + (how_many > 1 ? blocks(jobs[1]) : 0);
-  join_kernel<<<dim3(grid), dim3(256), 0, st>>>(all);
+  JoinJobs all{};
+  for (int i = 0; i < kMostJobs; ++i) {
+    if (i < how_many) all.job[i] = jobs[i];
+    all.first[i + 1] = all.first[i] + (i < how_many ? blocks(jobs[i]) : 0);
+  }
+  join_kernel<<<dim3(all.first[kMostJobs]), dim3(256), 0, st>>>(all);
   return check_launch("sum of parts");
 }
 

@@ -93,14 +93,16 @@ TileSize tiles_for(int64_t M, int64_t N, bool direct) {
   return best;
 }
 
+// The length of `splits` parts of a sum over k: whole steps of every kind of tile.
+int64_t split_length(int64_t k, int64_t splits) { return ceil_div(ceil_div(k, splits), 64) * 64; }
+
 template <typename T>
 int product_of_rows(ProductKind kind, ProductArgs g, int64_t rows, hipStream_t st) {
   g.direct = T::kType != GOSH_F32 && can_be_direct(g.a, g.K) && can_be_direct(g.b, kind == kProductForward ? g.K : g.N);
   const TileSize size = tiles_for(rows, g.N, g.direct);
-  const int64_t depth = product_depth(T::kType, size, g.direct);
   g.tiles_n = static_cast<int32_t>(ceil_div(g.N, tile_n(size)));
-  g.splits = 1;
-  g.k_per_split = ceil_div(g.K, depth) * depth;
+  g.splits = std::max(g.splits, 1);
+  g.k_per_split = split_length(g.K, g.splits);
   const int64_t rows_per_launch = kTilesPerLaunch / g.tiles_n * tile_m(size);
   const ProductArgs all = g;
   for (int64_t r = 0; r < rows; r += rows_per_launch) {
@@ -135,9 +137,17 @@ DwPlan plan_dw(int64_t rows, int32_t in, int32_t out, bool direct) {
   p.tiles_n = static_cast<int32_t>(ceil_div(in, tile_n(p.size)));
   const int64_t tiles = static_cast<int64_t>(p.tiles_m) * p.tiles_n;
   const int64_t want = std::min(std::max<int64_t>(1, rows / 256), std::max<int64_t>(1, (p.size == kLarge ? 256 : 512) / tiles));
-  p.k_per_split = ceil_div(ceil_div(std::max<int64_t>(rows, 1), want), 64) * 64;  // a multiple of every tile's depth
+  p.k_per_split = split_length(std::max<int64_t>(rows, 1), want);
   p.splits = static_cast<int32_t>(ceil_div(rows, p.k_per_split));
   return p;
+}
+
+// Few tiles of dx are split along its long sum, the columns of dy: at least 4 steps each.  1: not split.
+int32_t plan_dx_splits(int64_t rows, int32_t in, int32_t out, int32_t type) {
+  if (rows == 0 || tiles_for(rows, in, type != GOSH_F32) != kSmall) return 1;
+  const int64_t tiles = ceil_div(rows, 64) * ceil_div(in, 64);
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(out / 256, 256 / tiles));
+  return static_cast<int32_t>(ceil_div(out, split_length(out, want)));
 }
 
 // ---- the activation's gradient ------------------------------------------------------------------
@@ -206,7 +216,8 @@ struct BackwardPlan {
   DwPlan dw, dw_direct;
   SlopePlan slope;
   int64_t dz_ld;
-  uint64_t dz, dw_parts, db_parts, bytes;  // offsets, and the whole
+  int32_t dx_splits;
+  uint64_t dz, dw_parts, db_parts, dx_parts, bytes;  // offsets, and the whole
 };
 BackwardPlan plan_backward(int64_t rows, int32_t in, int32_t out, int32_t type, int32_t act) {
   BackwardPlan p;
@@ -217,7 +228,9 @@ BackwardPlan plan_backward(int64_t rows, int32_t in, int32_t out, int32_t type, 
   p.dz = 0;
   p.dw_parts = act == GOSH_ACT_NONE ? 0 : round_up(static_cast<uint64_t>(rows) * p.dz_ld * (type == GOSH_F32 ? 4 : 2));
   p.db_parts = p.dw_parts + round_up(static_cast<uint64_t>(std::max(p.dw.splits, p.dw_direct.splits)) * in * out * 4);
-  p.bytes = p.db_parts + round_up(static_cast<uint64_t>(p.slope.blocks_y) * out * 4);
+  p.dx_splits = plan_dx_splits(rows, in, out, type);
+  p.dx_parts = p.db_parts + round_up(static_cast<uint64_t>(p.slope.blocks_y) * out * 4);
+  p.bytes = p.dx_parts + (p.dx_splits > 1 ? round_up(static_cast<uint64_t>(p.dx_splits) * rows * in * 4) : 0);
   return p;
 }
 
@@ -238,7 +251,7 @@ int linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, co
         db != nullptr ? db_parts : nullptr, rows, out, p.slope.shift, p.slope.rows_per_block);
     if (int rc = check_launch("gradient of the activation")) return rc;
   }
-  JoinJob jobs[2];
+  JoinJob jobs[3];
   int sums = 0;
   if (db != nullptr) jobs[sums++] = {db_parts, out, out, out, db, static_cast<int32_t>(p.slope.blocks_y), out, GOSH_F32};
   if (dx != nullptr && rows > 0) {
@@ -248,7 +261,13 @@ int linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, co
     g.N = in;
     g.K = out;
     g.out = plane_of(dx);
+    if (p.dx_splits > 1) {
+      g.parts = reinterpret_cast<float *>(ws + p.dx_parts);
+      g.splits = p.dx_splits;
+    }
     if (int rc = product_of_rows<T>(kProductDx, g, rows, st)) return rc;
+    const int64_t n = rows * in;
+    if (g.parts != nullptr) jobs[sums++] = {g.parts, n, n, dx->ld, dx->data, p.dx_splits, in, T::kType};
   }
   if (dw != nullptr) {
     ProductArgs g{};

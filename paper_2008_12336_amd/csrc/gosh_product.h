@@ -34,7 +34,7 @@ struct ProductArgs {
   int32_t direct;         // 16-bit operands of aligned rows: see can_be_direct
   ForwardOut forward;     // kForward
   Plane out;              // kStore
-  float *parts;           // kParts: splits x M x N
+  float *parts;           // kParts: splits x M x N; dx in small tiles may have them too
 };
 
 // The products of a layer: which operands are k-major, whether B is packed.
@@ -666,7 +666,10 @@ template <typename T, TileSize Size>
 int launch_sized(ProductKind kind, const ProductArgs &g, hipStream_t st) {
   switch (kind) {
     case kProductForward: return launch_one<T, Size, kProductForward, kForward>(g, st);
-    case kProductDx: return launch_one<T, Size, kProductDx, kStore>(g, st);
+    case kProductDx:
+      if constexpr (Size == kSmall)
+        if (g.parts != nullptr) return launch_one<T, Size, kProductDx, kParts>(g, st);
+      return launch_one<T, Size, kProductDx, kStore>(g, st);
     case kProductDw: return launch_one<T, Size, kProductDw, kParts>(g, st);
     default: return launch_one<T, Size, kProductDwPacked, kParts>(g, st);
   }

@@ -97,12 +97,20 @@ TileSize tiles_for(int64_t M, int64_t N, bool direct) {
 int64_t split_length(int64_t k, int64_t splits) { return ceil_div(ceil_div(k, splits), 64) * 64; }
 
 template <typename T>
-int product_of_rows(ProductKind kind, ProductArgs g, int64_t rows, hipStream_t st) {
+TileSize shape_rows(ProductKind kind, int64_t rows, ProductArgs &g) {
   g.direct = T::kType != GOSH_F32 && can_be_direct(g.a, g.K) && can_be_direct(g.b, kind == kProductForward ? g.K : g.N);
   const TileSize size = tiles_for(rows, g.N, g.direct);
+  g.M = rows;
+  g.tiles_m = static_cast<int32_t>(std::min<int64_t>(ceil_div(rows, tile_m(size)), 1 << 30));
   g.tiles_n = static_cast<int32_t>(ceil_div(g.N, tile_n(size)));
   g.splits = std::max(g.splits, 1);
   g.k_per_split = split_length(g.K, g.splits);
+  return size;
+}
+
+template <typename T>
+int product_of_rows(ProductKind kind, ProductArgs g, int64_t rows, hipStream_t st) {
+  const TileSize size = shape_rows<T>(kind, rows, g);
   const int64_t rows_per_launch = kTilesPerLaunch / g.tiles_n * tile_m(size);
   const ProductArgs all = g;
   for (int64_t r = 0; r < rows; r += rows_per_launch) {
@@ -126,20 +134,22 @@ struct DwPlan {
   int64_t k_per_split;
 };
 DwPlan plan_dw(int64_t rows, int32_t in, int32_t out, bool direct) {
-  DwPlan p;
+  DwPlan best{};
   double least = 0;
-  p.size = kSmall;
-  for (TileSize s : {kSmall, kMiddle, kLarge}) {  // splits fill the device whatever the size
-    const double work = static_cast<double>(ceil_div(out, tile_m(s)) * tile_m(s)) * (ceil_div(in, tile_n(s)) * tile_n(s)) * weight_of(s, direct);
-    if (s == kSmall || work <= least) p.size = s, least = work;
+  for (TileSize s : {kSmall, kMiddle, kLarge}) {
+    DwPlan p;
+    p.size = s;
+    p.tiles_m = static_cast<int32_t>(ceil_div(out, tile_m(s)));
+    p.tiles_n = static_cast<int32_t>(ceil_div(in, tile_n(s)));
+    const int64_t tiles = static_cast<int64_t>(p.tiles_m) * p.tiles_n;
+    const int64_t want = std::min(std::max<int64_t>(1, rows / 256), std::max<int64_t>(1, (s == kLarge ? 256 : 512) / tiles));
+    p.k_per_split = split_length(std::max<int64_t>(rows, 1), want);
+    p.splits = static_cast<int32_t>(ceil_div(rows, p.k_per_split));
+    // of the busiest CU
+    const double work = static_cast<double>(ceil_div(tiles * p.splits, 256)) * tile_m(s) * tile_n(s) * weight_of(s, direct) * p.k_per_split;
+    if (s == kSmall || work <= least) best = p, least = work;
   }
-  p.tiles_m = static_cast<int32_t>(ceil_div(out, tile_m(p.size)));
-  p.tiles_n = static_cast<int32_t>(ceil_div(in, tile_n(p.size)));
-  const int64_t tiles = static_cast<int64_t>(p.tiles_m) * p.tiles_n;
-  const int64_t want = std::min(std::max<int64_t>(1, rows / 256), std::max<int64_t>(1, (p.size == kLarge ? 256 : 512) / tiles));
-  p.k_per_split = split_length(std::max<int64_t>(rows, 1), want);
-  p.splits = static_cast<int32_t>(ceil_div(rows, p.k_per_split));
-  return p;
+  return best;
 }
 
 // Few tiles of dx are split along its long sum, the columns of dy: at least 4 steps each.  1: not split.
@@ -212,6 +222,8 @@ SlopePlan plan_slope(int64_t rows, int32_t n) {
 
 uint64_t round_up(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
+constexpr int64_t kMostOfBoth = 1024;  // tiles of dx up to which dx and dw share a launch: what the device holds at once
+
 struct BackwardPlan {
   DwPlan dw, dw_direct;
   SlopePlan slope;
@@ -254,40 +266,50 @@ int linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, co
   JoinJob jobs[3];
   int sums = 0;
   if (db != nullptr) jobs[sums++] = {db_parts, out, out, out, db, static_cast<int32_t>(p.slope.blocks_y), out, GOSH_F32};
-  if (dx != nullptr && rows > 0) {
-    ProductArgs g{};
-    g.a = dz;
-    g.b = plane_of(w);
-    g.N = in;
-    g.K = out;
-    g.out = plane_of(dx);
+  // a packed x has its entries widened in registers: the alignment of its rows does not matter
+  const bool dw_direct = T::kType != GOSH_F32 && dw != nullptr && can_be_direct(dz, out) &&
+                         (x->packed ? in % 8 == 0 : can_be_direct(plane_of(x), in));
+  const DwPlan &d = dw_direct ? p.dw_direct : p.dw;
+  ProductArgs gx{}, gw{};
+  if (dx != nullptr) {
+    gx.a = dz;
+    gx.b = plane_of(w);
+    gx.N = in;
+    gx.K = out;
+    gx.out = plane_of(dx);
     if (p.dx_splits > 1) {
-      g.parts = reinterpret_cast<float *>(ws + p.dx_parts);
-      g.splits = p.dx_splits;
+      gx.parts = reinterpret_cast<float *>(ws + p.dx_parts);
+      gx.splits = p.dx_splits;
+      const int64_t n = rows * in;
+      jobs[sums++] = {gx.parts, n, n, dx->ld, dx->data, p.dx_splits, in, T::kType};
     }
-    if (int rc = product_of_rows<T>(kProductDx, g, rows, st)) return rc;
-    const int64_t n = rows * in;
-    if (g.parts != nullptr) jobs[sums++] = {g.parts, n, n, dx->ld, dx->data, p.dx_splits, in, T::kType};
   }
   if (dw != nullptr) {
-    ProductArgs g{};
-    g.a = dz;
-    g.b = plane_of(x);
-    g.direct = T::kType != GOSH_F32 && !x->packed && can_be_direct(g.a, out) && can_be_direct(g.b, in);
-    const DwPlan &d = g.direct ? p.dw_direct : p.dw;
-    if (rows > 0) {
-      g.M = out;
-      g.N = in;
-      g.K = rows;
-      g.k_per_split = d.k_per_split;
-      g.tiles_m = d.tiles_m;
-      g.tiles_n = d.tiles_n;
-      g.splits = d.splits;
-      g.parts = dw_parts;
-      if (int rc = launch_product<T>(x->packed ? kProductDwPacked : kProductDw, d.size, g, st)) return rc;
-    }
+    gw.a = dz;
+    gw.b = plane_of(x);
+    gw.direct = dw_direct;
+    gw.M = out;
+    gw.N = in;
+    gw.K = rows;
+    gw.k_per_split = d.k_per_split;
+    gw.tiles_m = d.tiles_m;
+    gw.tiles_n = d.tiles_n;
+    gw.splits = d.splits;
+    gw.parts = dw_parts;
     const int64_t n = static_cast<int64_t>(out) * in;
     jobs[sums++] = {dw_parts, n, n, dw->ld, dw->data, d.splits, in, dw->type};
+  }
+  if (rows > 0) {
+    ProductArgs both = gx;
+    if (dx != nullptr && dw != nullptr && d.size == kSmall && shape_rows<T>(kProductDx, rows, both) == kSmall &&
+        static_cast<int64_t>(both.tiles_m) * both.tiles_n * both.splits <= kMostOfBoth) {
+      if (int rc = launch_both<T>(x->packed != 0, both, gw, st)) return rc;
+    } else {
+      if (dx != nullptr)
+        if (int rc = product_of_rows<T>(kProductDx, gx, rows, st)) return rc;
+      if (dw != nullptr)
+        if (int rc = launch_product<T>(x->packed ? kProductDwPacked : kProductDw, d.size, gw, st)) return rc;
+    }
   }
   return join_parts(jobs, sums, st);
 }

@@ -54,6 +54,16 @@ int launch_product<Bf16>(ProductKind, TileSize, const ProductArgs &, hipStream_t
 template <>
 int launch_product<F16>(ProductKind, TileSize, const ProductArgs &, hipStream_t);
 
+// dx and dw, both in tiles of kSmall, in one launch; `packed`: x is.
+template <typename T>
+int launch_both(bool packed, const ProductArgs &dx, const ProductArgs &dw, hipStream_t st);
+template <>
+int launch_both<F32>(bool, const ProductArgs &, const ProductArgs &, hipStream_t);
+template <>
+int launch_both<Bf16>(bool, const ProductArgs &, const ProductArgs &, hipStream_t);
+template <>
+int launch_both<F16>(bool, const ProductArgs &, const ProductArgs &, hipStream_t);
+
 template <typename T>
 struct ProductDepth {  // k of a tile that passes through registers: 128 and 64 bytes of LDS a row and part
   static constexpr int value(bool small) { return T::kType == GOSH_F32 ? (small ? 32 : 16) : 64; }
@@ -65,9 +75,6 @@ inline bool can_be_direct(const Plane &p, int64_t along) {
 }
 constexpr int kDirectDepth = 64, kDirectRing = 2;  // k of a tile; tiles in LDS
 constexpr int direct_waves(int bn) { return bn == 256 ? 8 : 4; }
-inline int product_depth(int32_t type, TileSize size, bool direct) {
-  return direct ? kDirectDepth : type == GOSH_F32 ? ProductDepth<F32>::value(size == kSmall) : ProductDepth<Bf16>::value(false);
-}
 
 typedef float F16x __attribute__((ext_vector_type(16)));
 typedef short S4 __attribute__((ext_vector_type(4)));
@@ -130,7 +137,7 @@ struct Spread {
 };
 
 // One operand's tile: BX entries of m by BK of k.
-template <typename T, int BX, int BK, bool KMajor, bool Packed>
+template <typename T, int BX, int BK, bool KMajor, bool Packed, int Threads = 256>
 struct Tile {
   static_assert(!(KMajor && Packed), "only x of dw is packed");
   // a packed entry is a whole number of 8 bits times a power of two: one part holds it
@@ -138,10 +145,11 @@ struct Tile {
   static constexpr int kBytes = kParts * BX * BK * 2;  // of LDS
   static constexpr int kSize = Packed ? 1 : T::kType == GOSH_F32 ? 4 : 2;
   static constexpr int kChunks = BX * BK / 8;               // of 8 entries along memory
-  static constexpr int kPerThread = kChunks / 256;
+  static constexpr int kPerThread = kChunks / Threads;
   static constexpr int kAlong = (KMajor ? BK : BX) / 8;     // chunks in a row of the tile
   static constexpr int kWords = Packed ? 2 : T::kType == GOSH_F32 ? 8 : 4;
-  static_assert(kChunks % 256 == 0 && 256 % kAlong == 0, "");
+  static constexpr int kLoads = 0;  // straight to LDS
+  static_assert(kChunks % Threads == 0 && Threads % kAlong == 0, "");
 
   uint32_t raw[kPerThread][kWords];
   uint32_t unit[Packed ? kPerThread : 1];
@@ -162,7 +170,7 @@ struct Tile {
     const int there = static_cast<int>(cols < BX + BK ? cols : BX + BK) - at;
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
-      const int row = t / kAlong + i * (256 / kAlong);
+      const int row = t / kAlong + i * (Threads / kAlong);
       const uint32_t off = static_cast<uint32_t>(row * ld + at * kSize);
       if constexpr (Packed)
         unit[i] = __builtin_amdgcn_raw_buffer_load_b8(re, row * static_cast<int>(p.ld_exps) + at / kGroup, 0, 0);
@@ -205,7 +213,7 @@ struct Tile {
     const int t = threadIdx.x;
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
-      const int row = t / kAlong + i * (256 / kAlong), c = t % kAlong;
+      const int row = t / kAlong + i * (Threads / kAlong), c = t % kAlong;
       uint16_t *const to = lds + (KMajor ? Spread<BX, BK>::k_major(row, c) : Spread<BX, BK>::m_major(row, c));
       if constexpr (Packed) {
         const uint32_t q[2] = {raw[i][0], raw[i][1]};
@@ -405,18 +413,28 @@ __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[R
 
 // Tiles that pass through registers on their way to LDS: 32-bit entries, packed ones, and matrices whose rows are not
 // 16-byte aligned.
-template <typename T, int BX, ProductKind Kind, ProductOut Out>
-__global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs g) {
-  constexpr int BK = ProductDepth<T>::value(BX == 64);
-  constexpr bool a_k = Kind == kProductForward || Kind == kProductDx, b_k = Kind == kProductForward;
+template <typename T, int BX, ProductKind Kind>
+struct Staged {
+  static constexpr int BK = ProductDepth<T>::value(BX == 64);
+  static constexpr bool a_k = Kind == kProductForward || Kind == kProductDx, b_k = Kind == kProductForward;
   typedef Tile<T, BX, BK, a_k, false> TA;
   typedef Tile<T, BX, BK, b_k, Kind == kProductDwPacked> TB;
-  constexpr int W = BX / 2, R = W / 32;          // a wavefront's square of the tile, and its 32 x 32 blocks a side
-  constexpr int kBuffer = (TA::kBytes + TB::kBytes) / 2;
-  constexpr int kLds = 2 * kBuffer * 2 > 4 * Slab<W>::kFloats * 4 ? 2 * kBuffer * 2 : 4 * Slab<W>::kFloats * 4;
-  __shared__ __attribute__((aligned(16))) uint16_t lds[kLds / 2];
+  static constexpr int kBuffer = (TA::kBytes + TB::kBytes) / 2;
+  static constexpr int kSlabs = 4 * Slab<BX / 2>::kFloats * 4;
+  static constexpr int kLds = 2 * kBuffer * 2 > kSlabs ? 2 * kBuffer * 2 : kSlabs;
+};
 
-  const Place at = place_of(g, turns_of(g.tiles_m * g.tiles_n * g.splits).id, BX, BX);
+// The id-th tile.
+template <typename T, int BX, ProductKind Kind, ProductOut Out>
+__device__ __forceinline__ void staged_product(const ProductArgs &g, int id, uint16_t *lds) {
+  typedef Staged<T, BX, Kind> P;
+  typedef typename P::TA TA;
+  typedef typename P::TB TB;
+  constexpr int BK = P::BK, kBuffer = P::kBuffer;
+  constexpr bool a_k = P::a_k, b_k = P::b_k;
+  constexpr int W = BX / 2, R = W / 32;          // a wavefront's square of the tile, and its 32 x 32 blocks a side
+
+  const Place at = place_of(g, id, BX, BX);
   const int64_t m0 = at.m0, n0 = at.n0, k0 = at.k0, k1 = at.k1;
   const int steps = static_cast<int>((k1 - k0 + BK - 1) / BK);
 
@@ -480,6 +498,22 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs g) {
   finish<T, R, R, Out>(g, acc, reinterpret_cast<float *>(lds) + wave * Slab<W>::kFloats, m0 + wm, n0 + wn, at.split);
 }
 
+template <typename T, int BX, ProductKind Kind, ProductOut Out>
+__global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs g) {
+  __shared__ __attribute__((aligned(16))) uint16_t lds[Staged<T, BX, Kind>::kLds / 2];
+  staged_product<T, BX, Kind, Out>(g, turns_of(g.tiles_m * g.tiles_n * g.splits).id, lds);
+}
+
+// Both products of a gradient that is small: one launch, and neither waits for the other.
+template <typename T, ProductKind Dw, ProductOut DxOut>
+__global__ __launch_bounds__(256, 2) void both_products_kernel(const ProductArgs dx, const ProductArgs dw) {
+  constexpr int a = Staged<T, 64, kProductDx>::kLds, b = Staged<T, 64, Dw>::kLds;
+  __shared__ __attribute__((aligned(16))) uint16_t lds[(a > b ? a : b) / 2];
+  const int first = dx.tiles_m * dx.tiles_n * dx.splits, id = blockIdx.x;
+  if (id < first) staged_product<T, 64, kProductDx, DxOut>(dx, id, lds);
+  else staged_product<T, 64, Dw, kParts>(dw, id - first, lds);
+}
+
 // ---- 16-bit tiles that go straight to LDS -------------------------------------------------------
 
 // A tile that the memory system writes to LDS by itself, 1 KB an instruction of a wavefront: lane i's 16 bytes land at
@@ -539,16 +573,17 @@ struct DirectTile {
 
 // The same product with a ring of kDirectRing tiles: while a step is computed the loads of the next ones are under way,
 // also across the end of a tile: a workgroup goes from tile to tile, and the next one's loads run while the results of
-// the last are written.
+// the last are written.  A packed operand goes through registers, two steps ahead, where its entries get their width.
 template <typename T, int BM, int BN, ProductKind Kind, ProductOut Out>
 __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void direct_product_kernel(const ProductArgs g) {
   constexpr int BK = kDirectDepth;
   constexpr bool a_k = Kind == kProductForward || Kind == kProductDx, b_k = Kind == kProductForward;
   constexpr int kWaves = direct_waves(BN), kAcross = kWaves / 2;
   typedef DirectTile<BM, BK, a_k, kWaves> TA;
-  typedef DirectTile<BN, BK, b_k, kWaves> TB;
+  constexpr bool packed = Kind == kProductDwPacked;
+  typedef typename std::conditional<packed, Tile<T, BN, BK, b_k, packed, 64 * kWaves>, DirectTile<BN, BK, b_k, kWaves>>::type TB;
   constexpr int WM = BM / 2, WN = BN / kAcross, RM = WM / 32, RN = WN / 32, kRing = kDirectRing;
-  constexpr int kStep = TA::kBytes + TB::kBytes, kLoads = TA::kLoads + TB::kLoads;
+  constexpr int kStep = TA::kBytes + TB::kBytes, kLoads = packed ? 0 : TA::kLoads + TB::kLoads;
   constexpr int kStores = RM * 4;  // of a wavefront for a whole tile, at least
   static_assert(BK / 16 % 2 == 0, "the entries read ahead are in turns");
   __shared__ __attribute__((aligned(1024))) uint16_t lds[kRing * kStep / 2];
@@ -564,21 +599,28 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void d
   TA a;
   TB b;
   a.init(g.a);
-  b.init(g.b);
+  if constexpr (!packed) b.init(g.b);
   // The loads run ahead of the computation, over tiles.  After the last tile they load nothing, so that the count of
   // loads under way stays the same.
   uint32_t into = base;
   int turn = turns.id;
   int to_go;
+  Place from;
   const auto begin = [&]() {
-    const Place p = place_of(g, turn, BM, BN);
-    a.begin(g.a, p.m0, g.M, p.k0, p.k1);
-    b.begin(g.b, p.n0, g.N, p.k0, p.k1);
-    to_go = steps_of(p);
+    from = place_of(g, turn, BM, BN);
+    a.begin(g.a, from.m0, g.M, from.k0, from.k1);
+    if constexpr (!packed) b.begin(g.b, from.n0, g.N, from.k0, from.k1);
+    to_go = steps_of(from);
   };
   const auto fetch = [&]() {
-    a.fetch(g.a, into);
-    b.fetch(g.b, into + TA::kBytes);
+    if constexpr (packed) {
+      b.fetch(g.b, from.n0, g.N, from.k0, from.k1, false);
+      from.k0 += BK;
+      a.fetch(g.a, into);
+    } else {
+      a.fetch(g.a, into);
+      b.fetch(g.b, into + TA::kBytes);
+    }
     into = into == base + (kRing - 1) * kStep ? base : into + kStep;
     if (--to_go <= 0 && turn + turns.step < turns.end) {
       turn += turns.step;
@@ -587,7 +629,11 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void d
   };
   begin();
 #pragma unroll
-  for (int s = 0; s < kRing; ++s) fetch();
+  for (int s = 0; s < kRing; ++s) {
+    fetch();
+    if constexpr (packed)
+      if (s == 0) b.put(lds + TA::kBytes / 2);
+  }
   const uint16_t *now = lds;
   S8 fa[2][RM], fb[2][RN];
   const auto take = [&](int part) {
@@ -598,7 +644,7 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void d
   };
   float bias[RN];
   load_bias<RN, Out>(g, place_of(g, turns.id, BM, BN).n0 + wn, bias);
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"((kRing - 1) * kLoads) : "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((kRing - 1) * kLoads) : "memory");
   take(0);
   bool stored = false;  // the wavefront has written a whole tile just before
   for (int id = turns.id; id < turns.end; id += turns.step) {
@@ -624,10 +670,14 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void d
         multiply(part);
         __builtin_amdgcn_sched_barrier(0);
       }
+      if constexpr (packed) {
+        static_assert(kRing == 2, "the other tile is the next step's");
+        b.put(lds + (now == lds ? kStep / 2 : 0) + TA::kBytes / 2);
+      }
       // Loads and stores end in order.  The next step's loads are followed by those of kRing - 2 steps and, in the first
       // steps after a tile, its stores, which need not be waited for.  Then every wavefront's part is there, and every
       // wavefront is done with this step's tile, which the next loads replace.
-      if (stored && s < kRing - 1)
+      if (!packed && stored && s < kRing - 1)
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((kRing - 2) * kLoads + kStores) : "memory");
       else
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((kRing - 2) * kLoads) : "memory");
@@ -650,7 +700,7 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void d
 template <typename T, TileSize Size, ProductKind Kind, ProductOut Out>
 int launch_one(const ProductArgs &g, hipStream_t st) {
   const unsigned blocks = static_cast<unsigned>(g.tiles_m) * g.tiles_n * g.splits;
-  if constexpr (T::kType != GOSH_F32 && Kind != kProductDwPacked) {
+  if constexpr (T::kType != GOSH_F32) {
     if (g.direct) {
       const unsigned held = static_cast<unsigned>(resident_waves()) / 4 / direct_waves(tile_n(Size));  // eight wavefronts a CU
       direct_product_kernel<T, tile_m(Size), tile_n(Size), Kind, Out><<<dim3(blocks < held ? blocks : held), dim3(64 * direct_waves(tile_n(Size))), 0, st>>>(g);
@@ -680,6 +730,16 @@ int launch_any(ProductKind kind, TileSize size, const ProductArgs &g, hipStream_
   if (size == kLarge) return launch_sized<T, kLarge>(kind, g, st);
   if (size == kMiddle) return launch_sized<T, kMiddle>(kind, g, st);
   return launch_sized<T, kSmall>(kind, g, st);
+}
+
+template <typename T>
+int launch_both_any(bool packed, const ProductArgs &dx, const ProductArgs &dw, hipStream_t st) {
+  const dim3 grid(static_cast<unsigned>(dx.tiles_m * dx.tiles_n * dx.splits + dw.tiles_m * dw.tiles_n * dw.splits)), block(256);
+  if (packed && dx.parts != nullptr) both_products_kernel<T, kProductDwPacked, kParts><<<grid, block, 0, st>>>(dx, dw);
+  else if (packed) both_products_kernel<T, kProductDwPacked, kStore><<<grid, block, 0, st>>>(dx, dw);
+  else if (dx.parts != nullptr) both_products_kernel<T, kProductDw, kParts><<<grid, block, 0, st>>>(dx, dw);
+  else both_products_kernel<T, kProductDw, kStore><<<grid, block, 0, st>>>(dx, dw);
+  return check_launch("matrix products of the gradient");
 }
 
 }  // namespace gosh

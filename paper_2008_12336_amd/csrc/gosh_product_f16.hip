@@ -8,4 +8,9 @@ int launch_product<F16>(ProductKind kind, TileSize size, const ProductArgs &args
   return launch_any<F16>(kind, size, args, st);
 }
 
+template <>
+int launch_both<F16>(bool packed, const ProductArgs &dx, const ProductArgs &dw, hipStream_t st) {
+  return launch_both_any<F16>(packed, dx, dw, st);
+}
+
 }  // namespace gosh

@@ -8,4 +8,9 @@ int launch_product<F32>(ProductKind kind, TileSize size, const ProductArgs &args
   return launch_any<F32>(kind, size, args, st);
 }
 
+template <>
+int launch_both<F32>(bool packed, const ProductArgs &dx, const ProductArgs &dw, hipStream_t st) {
+  return launch_both_any<F32>(packed, dx, dw, st);
+}
+
 }  // namespace gosh

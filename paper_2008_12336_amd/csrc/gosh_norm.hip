@@ -63,21 +63,32 @@ __global__ __launch_bounds__(256) void norm_kernel(const NormArgs g) {
       Entries<F32, E>::load(g.beta + col[c], count[c], beta[c]);
     }
   }
-  // the rows of a workgroup take turns together, past the last one without memory accesses
+  // the rows of a workgroup take turns together, past the last one without memory accesses; a turn's rows are loaded
+  // while the turn before is worked on
+  typename Entries<T, E>::Vec next[C];
+  const auto fetch = [&](int64_t first) {
+    const int64_t row = first + threadIdx.x / L;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      next[c] = 0;
+      if (row < g.rows && count[c] > 0) next[c] = Entries<T, E>::fetch(static_cast<const S *>(g.x.data) + row * g.x.ld + col[c], count[c]);
+    }
+  };
   const int64_t step = static_cast<int64_t>(gridDim.x) * (256 / L);
+  fetch(static_cast<int64_t>(blockIdx.x) * (256 / L));
   for (int64_t first = static_cast<int64_t>(blockIdx.x) * (256 / L); first < g.rows; first += step) {
     const int64_t row = first + threadIdx.x / L;
     const bool there = row < g.rows;
     float v[C][E];
     float sum = 0.f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[c][e] = 0.f;
-      if (there && count[c] > 0) Entries<T, E>::load(static_cast<const S *>(g.x.data) + row * g.x.ld + col[c], count[c], v[c]);
-#pragma unroll
-      for (int e = 0; e < E; ++e) sum += v[c][e];
-    }
+      for (int e = 0; e < E; ++e) {
+        v[c][e] = T::up(next[c][e]);
+        sum += v[c][e];
+      }
+    fetch(first + step);
     const float mean = row_sum<L>(sum, lds) / width;
     float squares = 0.f;
 #pragma unroll
@@ -196,22 +207,67 @@ __global__ __launch_bounds__(256) void norm_back_kernel(const NormBackArgs g) {
     for (int e = 0; e < E; ++e) gamma[c][e] = dgamma[c][e] = dbeta[c][e] = 0.f;
     if (count[c] > 0) Entries<F32, E>::load(g.gamma + col[c], count[c], gamma[c]);
   }
+  // a turn's rows are loaded while the turn before is worked on
+  constexpr int kWords = E * sizeof(S) / 4;
+  typename Entries<T, E>::Vec next_d[C];
+  uint32_t next_x[C][kWords], next_unit[C];
+  float next_rstd, next_mean;
+  const auto fetch = [&](int64_t first) {
+    const int64_t row = first + threadIdx.x / L;
+    const bool there = row < g.rows;
+    next_rstd = there ? g.rstd[row] : 0.f;
+    next_mean = there && !g.packed ? g.mean[row] : 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      next_d[c] = 0;
+      next_unit[c] = 0;
+#pragma unroll
+      for (int w = 0; w < kWords; ++w) next_x[c][w] = 0;
+      if (!there || count[c] <= 0) continue;
+      next_d[c] = Entries<T, E>::fetch(static_cast<const S *>(g.dy.data) + row * g.dy.ld + col[c], count[c]);
+      if (g.packed) {
+        uint32_t q[E / 4];
+        load_bytes<E>(static_cast<const int8_t *>(g.x.data) + row * g.x.ld + col[c], count[c], q);
+#pragma unroll
+        for (int w = 0; w < E / 4; ++w) next_x[c][w] = q[w];
+        next_unit[c] = g.x.exps[row * g.x.ld_exps + col[c] / kGroup];
+      } else {
+        const auto x = Entries<T, E>::fetch(static_cast<const S *>(g.x.data) + row * g.x.ld + col[c], count[c]);
+        const auto u = __builtin_bit_cast(typename Words<kWords>::V, x);
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) next_x[c][w] = u[w];
+      }
+    }
+  };
   const int64_t step = static_cast<int64_t>(gridDim.x) * (256 / L);
+  fetch(static_cast<int64_t>(blockIdx.x) * (256 / L));
   for (int64_t first = static_cast<int64_t>(blockIdx.x) * (256 / L); first < g.rows; first += step) {
     const int64_t row = first + threadIdx.x / L;
     const bool there = row < g.rows;
-    const float rstd = there ? g.rstd[row] : 0.f;
-    const float mean = there && !g.packed ? g.mean[row] : 0.f;
+    const float rstd = next_rstd, mean = next_mean;
     float d[C][E], xhat[C][E];
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+      if (g.packed) {
+        uint32_t q[E / 4];
 #pragma unroll
-      for (int e = 0; e < E; ++e) d[c][e] = xhat[c][e] = 0.f;
-      if (there && count[c] > 0) {
-        Entries<T, E>::load(static_cast<const S *>(g.dy.data) + row * g.dy.ld + col[c], count[c], d[c]);
-        load_xhat<T, E>(g, row, col[c], count[c], mean, rstd, xhat[c]);
+        for (int w = 0; w < E / 4; ++w) q[w] = next_x[c][w];
+        widen<E>(q, read_unit(next_unit[c]), xhat[c]);
+      } else {
+        typename Words<kWords>::V u;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) u[w] = next_x[c][w];
+        const auto x = __builtin_bit_cast(typename Entries<T, E>::Vec, u);
+#pragma unroll
+        for (int e = 0; e < E; ++e) xhat[c][e] = e < count[c] ? (T::up(x[e]) - mean) * rstd : 0.f;
       }
+#pragma unroll
+      for (int e = 0; e < E; ++e) d[c][e] = T::up(next_d[c][e]);
+    }
+    fetch(first + step);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         dgamma[c][e] = fmaf(d[c][e], xhat[c][e], dgamma[c][e]);

@@ -60,6 +60,7 @@ SHAPES = [  # rows, in, out, padding of the rows, entries off the start of memor
     (1, 1, 1, 0, 0), (1, 512, 2048, 0, 0), (2, 37, 5, 3, 1), (7, 130, 33, 0, 1), (8, 64, 257, 1, 0), (9, 8, 1, 0, 0),
     (33, 3, 40, 5, 3), (64, 64, 64, 0, 0), (129, 260, 130, 0, 0), (200, 17, 517, 2, 1), (300, 1024, 96, 8, 8),
     (1000, 132, 31, 0, 0), (20000, 72, 260, 0, 0), (16391, 128, 384, 0, 0), (33001, 64, 264, 0, 0),
+    (90, 97, 1844, 0, 0),
 ]
 
 
@@ -131,6 +132,14 @@ def test_linear_backward(shape, dtype):
         assert torch.equal(alone, dx)
         beside(dx, xmem)
         beside(dw, wmem)
+
+
+@types
+@pytest.mark.parametrize("shape", [(20011, 512, 1024, 0, 0), (20011, 512, 1024, 8, 1)], ids=["aligned", "not"])
+def test_many_rows(shape, dtype):
+    """Largest tiles, more of them than the device holds at once, and sums that are split."""
+    test_linear(shape, dtype)
+    test_linear_backward(shape, dtype)
 
 
 NORMS = [  # rows, cols, padding, off the start
@@ -417,3 +426,13 @@ def test_refusals_on_the_device():
     with pytest.raises(G.GoshError, match="eps"):
         G.gosh_layer_norm(x, s[:32], s[:32], torch.empty_like(x), eps=-1.0)
     torch.cuda.synchronize()
+
+
+def test_the_link_predictor_learns():
+    """The example: a head trained on an embedding out of 8-bit activations tells held-out edges from other pairs."""
+    from paper_2008_12336_amd.examples import link_head
+
+    before, after, losses = link_head.train(scale=12, dim=32, steps=120, rows=8192)
+    print(f"held-out AUC {before:.3f} -> {after:.3f}, loss {losses[0]:.3f} -> {losses[-1]:.3f}")
+    assert after > 0.75 and after > before
+    assert sum(losses[-10:]) < 0.9 * sum(losses[:10])

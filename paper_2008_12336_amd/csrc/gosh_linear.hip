@@ -9,8 +9,19 @@ namespace {
 
 // ---- a few rows -----------------------------------------------------------------------------
 
-constexpr int kFewRows = 8;   // rows up to which a call reads w once at the rate of memory instead of filling tiles
 constexpr int kFewCols = 2;   // rows of w a wavefront takes together
+
+// Rows for which reading w once for each 8 of them beats tiles, whose steps along k come one after the other.  Measured
+// (us of a call, GELU and residual): 4.3 and 1 for each 8 rows and million entries of w, against 6 and 0.005 (16 bits,
+// straight to LDS) or 0.024 (32 bits) for each column of w; 32 rows of 512 -> 2048: 8.1 and 8.3 (bf16), 8.5 and 16.6
+// (f32), of 2048 -> 512: 7.5 and 15.4, 8.6 and 53.
+bool few_rows(int64_t rows, int64_t k, int64_t n, int32_t type) {
+  if (rows <= 8) return true;
+  if (rows > 1024) return false;
+  const int64_t whole = type == GOSH_F32 ? 256 : 512;  // columns that a wavefront takes at a time, there or not
+  const double by_rows = static_cast<double>(ceil_div(rows, 8)) * (ceil_div(k, whole) * whole) * n * 1e-6;
+  return by_rows < 1.7 + k * (type == GOSH_F32 ? 0.024 : 0.005);
+}
 
 // y = act(x w^T + bias) + residual for R rows: every lane has 8 (16-bit) or 4 entries of a row of w at a time, and its
 // wavefront sums the lanes' products.
@@ -19,7 +30,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const Plane x, const Plan
   constexpr int E = T::kType == GOSH_F32 ? 4 : 8;
   typedef typename T::Store S;
   const int wave = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x & 63;
-  const int col = wave * kFewCols;
+  const int col = wave * kFewCols, row0 = blockIdx.y * R;
   if (col >= n) return;
   float acc[kFewCols][R];
 #pragma unroll
@@ -35,7 +46,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const Plane x, const Plan
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float xv[E];
-      Entries<T, E>::load(static_cast<const S *>(x.data) + (r < rows ? r : 0) * x.ld + k0, count, xv);
+      Entries<T, E>::load(static_cast<const S *>(x.data) + (row0 + r < rows ? row0 + r : row0) * x.ld + k0, count, xv);
 #pragma unroll
       for (int c = 0; c < kFewCols; ++c)
 #pragma unroll
@@ -52,7 +63,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const Plane x, const Plan
       for (int s = 32; s > 0; s /= 2) sum += __shfl_xor(sum, s);
       if (lane == c * R + r) v = sum;
     }
-  const int r = lane % R, to = col + lane / R;
+  const int r = row0 + lane % R, to = col + lane / R;
   if (lane >= kFewCols * R || r >= rows || to >= n) return;
   if (f.bias != nullptr) v += f.bias[to];
   if (f.z.data != nullptr) static_cast<S *>(f.z.data)[r * f.z.ld + to] = T::down(v);
@@ -64,7 +75,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const Plane x, const Plan
 template <typename T>
 int launch_few_rows(const gosh_mat *x, const gosh_mat *w, const ForwardOut &f, hipStream_t st) {
   const int rows = static_cast<int>(x->rows), n = static_cast<int>(w->rows), k = x->cols;
-  const dim3 grid(static_cast<unsigned>(ceil_div(n, 4 * kFewCols))), block(256);
+  const dim3 grid(static_cast<unsigned>(ceil_div(n, 4 * kFewCols)), static_cast<unsigned>(ceil_div(rows, 8))), block(256);
   const Plane xp = plane_of(x), wp = plane_of(w);
   if (rows == 1) few_rows_kernel<T, 1><<<grid, block, 0, st>>>(xp, wp, f, rows, n, k);
   else if (rows == 2) few_rows_kernel<T, 2><<<grid, block, 0, st>>>(xp, wp, f, rows, n, k);
@@ -343,7 +354,7 @@ int gosh_linear(const gosh_mat *x, const gosh_mat *w, const float *bias, int32_t
   if (x->rows == 0) return GOSH_OK;
   hipStream_t st = as_stream(hip_stream);
   ForwardOut f{bias, plane_of(residual), plane_of(y), plane_of(z), plane_of(y8), act, z != nullptr && z->packed};
-  if (x->rows <= kFewRows && !f.z_packed && y8 == nullptr) {
+  if (few_rows(x->rows, x->cols, out, x->type) && !f.z_packed && y8 == nullptr) {
     if (x->type == GOSH_F32) return launch_few_rows<F32>(x, w, f, st);
     if (x->type == GOSH_BF16) return launch_few_rows<Bf16>(x, w, f, st);
     return launch_few_rows<F16>(x, w, f, st);

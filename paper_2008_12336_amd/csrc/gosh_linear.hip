@@ -173,59 +173,81 @@ int32_t plan_dx_splits(int64_t rows, int32_t in, int32_t out, int32_t type) {
 
 // ---- the activation's gradient ------------------------------------------------------------------
 
-// dz = dy * act'(z) and its sums over rows.  A lane has 8 columns; 2^shift lanes lie along a row, the others of the
-// workgroup on rows of their own.  parts: gridDim.y x n sums.
+// dz = dy * act'(z) and its sums over rows.  A lane has 16 bytes of a row; `along` lanes lie along a row, the others of
+// the workgroup on rows of their own.  parts: gridDim.y x n sums.
+template <typename T>
+struct SlopeChunk {
+  static constexpr int E = T::kType == GOSH_F32 ? 4 : 8;
+};
 template <typename T>
 __global__ __launch_bounds__(256) void slope_kernel(const Plane dy, const Plane z, bool z_packed, int act, const Plane dz,
-                                                    float *parts, int64_t rows, int n, int shift, int64_t rows_per_block) {
-  __shared__ float lds[256][8];
-  const int along = threadIdx.x & ((1 << shift) - 1), step = 256 >> shift;
-  const int col = (static_cast<int>(blockIdx.x) << shift) * 8 + along * 8;
-  const int count = n - col < 8 ? n - col : 8;
+                                                    float *parts, int64_t rows, int n, int along, int64_t rows_per_block) {
+  constexpr int E = SlopeChunk<T>::E;
+  typedef typename T::Store S;
+  __shared__ float lds[256][E];
+  const int step = 256 / along, chunk = threadIdx.x % along, first = threadIdx.x / along;
+  const int col = (static_cast<int>(blockIdx.x) * along + chunk) * E;
+  const int count = first >= step ? 0 : n - col < E ? n - col : E;
   const int64_t r0 = blockIdx.y * rows_per_block, r1 = r0 + rows_per_block < rows ? r0 + rows_per_block : rows;
-  float sum[8];
+  float sum[E];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+  for (int e = 0; e < E; ++e) sum[e] = 0.f;
   if (count > 0) {
     with_activation(act, [&](auto a) {
       typedef decltype(a) A;
-      for (int64_t r = r0 + (threadIdx.x >> shift); r < r1; r += step) {
-        float g[8], s[8];
-        Entries<T, 8>::load(static_cast<const typename T::Store *>(dy.data) + r * dy.ld + col, count, g);
-        if (z.data != nullptr) {
-          load_entries<T, 8>(z, z_packed, r, col, count, s);
+      constexpr int kTogether = 2;  // rows whose loads are under way at once
+      for (int64_t r = r0 + first; r < r1; r += kTogether * step) {
+        float g[kTogether][E], s[kTogether][E];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) g[e] *= A::slope(s[e]);
+        for (int t = 0; t < kTogether; ++t) {
+          const int here = r + t * step < r1 ? count : 0;
+          Entries<T, E>::load(static_cast<const S *>(dy.data) + (r + t * step) * dy.ld + col, here, g[t]);
+          if (z.data != nullptr) load_entries<T, E>(z, z_packed, r + t * step, col, here, s[t]);
         }
-        if (dz.data != nullptr) Entries<T, 8>::store(static_cast<typename T::Store *>(dz.data) + r * dz.ld + col, count, g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += g[e];
+        for (int t = 0; t < kTogether; ++t) {
+          if (r + t * step >= r1) break;
+          if (z.data != nullptr) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) g[t][e] *= A::slope(s[t][e]);
+          }
+          if (dz.data != nullptr) Entries<T, E>::store(static_cast<S *>(dz.data) + (r + t * step) * dz.ld + col, count, g[t]);
+#pragma unroll
+          for (int e = 0; e < E; ++e) sum[e] += g[t][e];
+        }
       }
     });
   }
   if (parts == nullptr) return;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) lds[threadIdx.x][e] = sum[e];
+  for (int e = 0; e < E; ++e) lds[threadIdx.x][e] = sum[e];
   __syncthreads();
-  if (threadIdx.x >> shift != 0 || count <= 0) return;
+  if (first != 0 || count <= 0) return;
   for (int s = 1; s < step; ++s)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] += lds[(s << shift) + along][e];
-  Entries<F32, 8>::store(parts + static_cast<int64_t>(blockIdx.y) * n + col, count, sum);
+    for (int e = 0; e < E; ++e) sum[e] += lds[s * along + chunk][e];
+  Entries<F32, E>::store(parts + static_cast<int64_t>(blockIdx.y) * n + col, count, sum);
 }
 
 struct SlopePlan {
-  int shift;
+  int along;
   unsigned blocks_x, blocks_y;
   int64_t rows_per_block;
 };
-SlopePlan plan_slope(int64_t rows, int32_t n) {
+SlopePlan plan_slope(int64_t rows, int32_t n, int32_t type) {
   SlopePlan p;
-  p.shift = 0;
-  while (p.shift < 6 && (8 << p.shift) < n) ++p.shift;
-  p.blocks_x = static_cast<unsigned>(ceil_div(n, 8 << p.shift));
-  const int64_t step = 256 >> p.shift;
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 4 * step), ceil_div(2048, p.blocks_x)));
+  const int64_t chunks = ceil_div(n, type == GOSH_F32 ? 4 : 8);
+  const int64_t fewest = ceil_div(chunks, 256);
+  int64_t busy = 0;
+  for (int64_t blocks = fewest; blocks < fewest + 4; ++blocks) {  // the split of a row that keeps most lanes busy
+    const int64_t along = ceil_div(chunks, blocks);
+    if (256 / along * along <= busy || ceil_div(chunks, along) != blocks) continue;
+    busy = 256 / along * along;
+    p.along = static_cast<int>(along);
+    p.blocks_x = static_cast<unsigned>(blocks);
+  }
+  const int64_t step = 256 / p.along;
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 4 * step), ceil_div(1024, p.blocks_x)));
   p.rows_per_block = ceil_div(ceil_div(std::max<int64_t>(rows, 1), want), step) * step;
   p.blocks_y = static_cast<unsigned>(ceil_div(rows, p.rows_per_block));
   return p;
@@ -246,7 +268,7 @@ BackwardPlan plan_backward(int64_t rows, int32_t in, int32_t out, int32_t type, 
   BackwardPlan p;
   p.dw = plan_dw(rows, in, out, false);
   p.dw_direct = plan_dw(rows, in, out, type != GOSH_F32);
-  p.slope = plan_slope(rows, out);
+  p.slope = plan_slope(rows, out, type);
   p.dz_ld = (out + 7) / 8 * 8;
   p.dz = 0;
   p.dw_parts = act == GOSH_ACT_NONE ? 0 : round_up(static_cast<uint64_t>(rows) * p.dz_ld * (type == GOSH_F32 ? 4 : 2));
@@ -271,7 +293,7 @@ int linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, co
     if (act != GOSH_ACT_NONE && (dx != nullptr || dw != nullptr)) dz = to = Plane{ws + p.dz, nullptr, p.dz_ld, 0};
     slope_kernel<T><<<dim3(p.slope.blocks_x, p.slope.blocks_y), dim3(256), 0, st>>>(
         plane_of(dy), act == GOSH_ACT_NONE ? Plane{nullptr, nullptr, 0, 0} : plane_of(z), z != nullptr && z->packed, act, to,
-        db != nullptr ? db_parts : nullptr, rows, out, p.slope.shift, p.slope.rows_per_block);
+        db != nullptr ? db_parts : nullptr, rows, out, p.slope.along, p.slope.rows_per_block);
     if (int rc = check_launch("gradient of the activation")) return rc;
   }
   JoinJob jobs[3];

@@ -6,6 +6,16 @@
 // transposing read (16 lanes fetch 4 rows of 16 entries and get 4 entries of one column each), so that no operand is
 // transposed in memory.
 //
+// Three ways, all ending in the same epilogue.  Aligned 16-bit rows go straight to LDS, in tiles of 256 x 256 by eight
+// wavefronts where there are enough: 65,536 x 512 x 2048 takes 137 to 150 us (0.9 to 1.0 PFLOP/s; a large product of the
+// vendor's library reaches 1.33), and with K = 512, where the epilogue counts, 262,144 x 512 -> 2048 683 us without and
+// 755 with GELU.  There each tile costs 13.7 us of products and 10 of epilogue (8.5 of them instructions, beside 6 of
+// stores): the eight wavefronts go through them together, and tiles of 128 x 128, two workgroups to a CU, which do
+// overlap them, lose more to fetching (914 us).  Other tiles pass through registers on their way to LDS (32-bit entries,
+// odd strides): 65,536 x 1024 -> 1024 in f32 takes 746 us, 184 TFLOP/s (that library: 144 to 152); their instructions
+// and products take turns on each SIMD (54 % of its time are products).  A packed x of dw is widened in registers beside
+// direct tiles of dz: 196 us for 131,072 x 512 and 1024, against 143 unpacked.
+//
 // 32-bit entries are taken apart into three bf16 parts, x = h + m + l, each the nearest to what the ones before leave
 // (|m| <= 2^-9 |x|, |l| <= 2^-18 |x|, nothing is left), and their products summed as hh + hm + mh + hl + mm + lh in the
 // 32-bit accumulators: what is left out is 2^-26 of a product, less than 32 bits round it by.  Six bf16 products of the
@@ -40,7 +50,7 @@ struct ProductArgs {
 // The products of a layer: which operands are k-major, whether B is packed.
 enum ProductKind : int { kProductForward, kProductDx, kProductDw, kProductDwPacked };
 
-enum TileSize : int { kSmall, kMiddle, kLarge };  // kLarge: direct products only
+enum TileSize : int { kSmall, kMiddle, kLarge };  // kLarge: only straight to LDS, others leave too few registers
 constexpr int tile_m(TileSize s) { return s == kLarge ? 256 : s == kMiddle ? 128 : 64; }
 constexpr int tile_n(TileSize s) { return tile_m(s); }
 
@@ -73,7 +83,9 @@ struct ProductDepth {  // k of a tile that passes through registers: 128 and 64 
 inline bool can_be_direct(const Plane &p, int64_t along) {
   return reinterpret_cast<uintptr_t>(p.data) % 16 == 0 && p.ld % 8 == 0 && along % 8 == 0;
 }
-constexpr int kDirectDepth = 64, kDirectRing = 2;  // k of a tile; tiles in LDS
+// k of a tile, and tiles in LDS.  Rows of 64 k are lines of 128 bytes: with 32 k and a ring of 3 or 4 the address unit was
+// busy 71 % of the time and the matrix cores 48 %, and 65,536 x 2048 -> 512 took 151 instead of 137 us.
+constexpr int kDirectDepth = 64, kDirectRing = 2;
 constexpr int direct_waves(int bn) { return bn == 256 ? 8 : 4; }
 
 typedef float F16x __attribute__((ext_vector_type(16)));
@@ -504,7 +516,7 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs g) {
   staged_product<T, BX, Kind, Out>(g, turns_of(g.tiles_m * g.tiles_n * g.splits).id, lds);
 }
 
-// Both products of a gradient that is small: one launch, and neither waits for the other.
+// Both products of a gradient that is small: one launch, and neither waits for the other.  (Measured where it is chosen.)
 template <typename T, ProductKind Dw, ProductOut DxOut>
 __global__ __launch_bounds__(256, 2) void both_products_kernel(const ProductArgs dx, const ProductArgs dw) {
   constexpr int a = Staged<T, 64, kProductDx>::kLds, b = Staged<T, 64, Dw>::kLds;
@@ -707,9 +719,12 @@ int launch_one(const ProductArgs &g, hipStream_t st) {
       return check_launch("matrix product");
     }
   }
-  if constexpr (Size != kLarge)
+  if constexpr (Size == kLarge) {
+    return fail(GOSH_EINVAL, "tiles of 256 x 256 are for aligned rows of 16-bit entries");
+  } else {
     product_kernel<T, tile_m(Size), Kind, Out><<<dim3(blocks), dim3(256), 0, st>>>(g);
-  return check_launch("matrix product");
+    return check_launch("matrix product");
+  }
 }
 
 template <typename T, TileSize Size>

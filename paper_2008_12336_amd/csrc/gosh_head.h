@@ -299,17 +299,23 @@ __device__ __forceinline__ void load_entries(const Plane &m, bool packed, int64_
   }
 }
 
-// N entries at (row, col) into a packed matrix, by the lanes of a group together: kGroup / N of them, or fewer where
-// `lanes` says so, hold a group's columns.  Entries past `count` are zero.  Every lane of the group calls it.
+// N entries into a packed matrix, at p and the exponent at e, by the lanes of a group together: kGroup / N of them, or
+// fewer where `lanes` says so, hold a group's columns.  Entries past `count` are zero.  Every lane of the group calls it.
 template <typename T, int N>
-__device__ __forceinline__ void store_packed(const Plane &m, int64_t row, int col, int count, const float (&v)[N],
-                                             bool first_of_group, int lanes) {
+__device__ __forceinline__ void store_packed(int8_t *p, uint8_t *e, int count, const float (&v)[N], bool first_of_group, int lanes) {
   const uint32_t byte = exponent_byte<T>(most_bits<N>(v, lanes));
   if (count <= 0) return;
   uint32_t q[N / 4];
   quantise<N>(v, byte, top_of<T>(byte), q);
-  store_bytes<N>(static_cast<int8_t *>(m.data) + row * m.ld + col, count, q);
-  if (first_of_group) m.exps[row * m.ld_exps + col / kGroup] = static_cast<uint8_t>(byte);
+  store_bytes<N>(p, count, q);
+  if (first_of_group) *e = static_cast<uint8_t>(byte);
+}
+// The same at (row, col).
+template <typename T, int N>
+__device__ __forceinline__ void store_packed(const Plane &m, int64_t row, int col, int count, const float (&v)[N],
+                                             bool first_of_group, int lanes) {
+  store_packed<T, N>(static_cast<int8_t *>(m.data) + row * m.ld + col, m.exps + row * m.ld_exps + col / kGroup, count, v,
+                     first_of_group, lanes);
 }
 
 // ---- device: activations ----------------------------------------------------------------
@@ -317,7 +323,10 @@ __device__ __forceinline__ void store_packed(const Plane &m, int64_t row, int co
 template <int Act>
 struct Activation;
 
-__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
+constexpr float kLog2E = 1.4426950408889634f;
+// The logistic function of -x / kLog2E.
+__device__ __forceinline__ float logistic2(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)); }
+__device__ __forceinline__ float logistic(float x) { return logistic2(-kLog2E * x); }
 
 template <>
 struct Activation<GOSH_ACT_NONE> {
@@ -343,7 +352,7 @@ template <>
 struct Activation<GOSH_ACT_GELU> {
   static constexpr float kC = 1.5957691216057308f;             // 2 sqrt(2/pi)
   static constexpr float kD = 1.5957691216057308f * 0.044715f;
-  static __device__ __forceinline__ float value(float z) { return z * logistic(z * (kC + kD * z * z)); }
+  static __device__ __forceinline__ float value(float z) { return z * logistic2(z * (-kLog2E * kC + -kLog2E * kD * (z * z))); }
   static __device__ __forceinline__ float slope(float z) {
     z = z > 12.f ? 12.f : z < -12.f ? -12.f : z;  // as above
     const float s = logistic(z * (kC + kD * z * z));

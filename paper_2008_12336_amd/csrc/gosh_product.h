@@ -265,9 +265,24 @@ struct Tile {
   }
 };
 
+// Where a lane's entries lie in a matrix: a row and column that are the same for the wavefront, in scalar registers, and
+// the lane's place from there, 32 bits.
+struct Spot {
+  int64_t row, col;
+  int down, right;
+  template <typename S>
+  __device__ __forceinline__ S *in(const Plane &p) const {
+    const uint32_t lane = static_cast<uint32_t>(down * static_cast<int>(p.ld) + right) * static_cast<uint32_t>(sizeof(S));
+    return reinterpret_cast<S *>(static_cast<char *>(p.data) + (row * p.ld + col) * static_cast<int64_t>(sizeof(S)) + lane);
+  }
+  __device__ __forceinline__ uint8_t *exponent_in(const Plane &p) const {
+    return p.exps + (row * p.ld_exps + col / kGroup) + static_cast<uint32_t>(down * static_cast<int>(p.ld_exps) + right / kGroup);
+  }
+};
+
 // E entries of a row of z become entries of y; r: the residual's.  Full: all of them are there.
 template <typename T, int E, bool Full>
-__device__ __forceinline__ void put_forward(const ForwardOut &f, int64_t row, int col, int there, float (&v)[E],
+__device__ __forceinline__ void put_forward(const ForwardOut &f, const Spot &at, int there, float (&v)[E],
                                             const typename Entries<T, E>::Vec &r) {
   typedef typename T::Store S;
   constexpr int kLanes = kGroup / E;  // of a group of the 8-bit form
@@ -278,8 +293,8 @@ __device__ __forceinline__ void put_forward(const ForwardOut &f, int64_t row, in
     for (int i = 0; i < E; ++i) v[i] = i < count ? v[i] : 0.f;  // entries that are not there count in no group
   }
   if (f.z.data != nullptr) {
-    if (f.z_packed) store_packed<T, E>(f.z, row, col, count, v, head, kLanes);
-    else if (Full || count > 0) Entries<T, E>::store(static_cast<S *>(f.z.data) + row * f.z.ld + col, count, v);
+    if (f.z_packed) store_packed<T, E>(at.in<int8_t>(f.z), at.exponent_in(f.z), count, v, head, kLanes);
+    else if (Full || count > 0) Entries<T, E>::store(at.in<S>(f.z), count, v);
   }
   with_activation(f.act, [&](auto a) {
 #pragma unroll
@@ -294,9 +309,9 @@ __device__ __forceinline__ void put_forward(const ForwardOut &f, int64_t row, in
 #pragma unroll
       for (int i = 0; i < E; ++i) v[i] = i < count ? v[i] : 0.f;
     }
-    store_packed<T, E>(f.y8, row, col, count, v, head, kLanes);
+    store_packed<T, E>(at.in<int8_t>(f.y8), at.exponent_in(f.y8), count, v, head, kLanes);
   }
-  if (Full || count > 0) Entries<T, E>::store(static_cast<S *>(f.y.data) + row * f.y.ld + col, count, v);
+  if (Full || count > 0) Entries<T, E>::store(at.in<S>(f.y), count, v);
 }
 
 // The id-th tile.
@@ -364,20 +379,19 @@ __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[R
   typedef typename T::Store S;
   const int lane = threadIdx.x & 63;
   const int r = lane / kLanes, c = lane % kLanes * E;
-  const int col = static_cast<int>(n) + c;
-  const auto count_of = [&](int64_t row) {
-    const int64_t left = r < kRows && row < g.M ? g.N - col : 0;
-    return kFull ? E : static_cast<int>(left < 0 ? 0 : left > E ? E : left);
+  const int across = static_cast<int>(g.N - n) - c, down = static_cast<int>(g.M - m < 32 * RM ? g.M - m : 32 * RM) - r;
+  const auto count_of = [&](int turn) {
+    const int left = r < kRows && kRows * turn < down ? across : 0;
+    return kFull ? E : left < 0 ? 0 : left > E ? E : left;
   };
+  const auto spot_of = [&](int turn) { return Spot{m + kRows * turn, n, r, c}; };
   // the residual of some rows is loaded kAhead turns before: by itself each load would be waited for, behind the stores
   // before it
   constexpr int kAhead = 2, kTurns = 32 / kRows * RM;
   typename Entries<T, E>::Vec residual[kAhead + 1];
   const auto load_residual = [&](int turn) {
     if (Out != kForward || g.forward.residual.data == nullptr) return;
-    const int64_t row = m + kRows * turn + r;
-    residual[turn % (kAhead + 1)] = Entries<T, E>::fetch(
-        static_cast<const S *>(g.forward.residual.data) + row * g.forward.residual.ld + col, count_of(row));
+    residual[turn % (kAhead + 1)] = Entries<T, E>::fetch(spot_of(turn).template in<S>(g.forward.residual), count_of(turn));
   };
 #pragma unroll
   for (int turn = 0; turn < kAhead; ++turn) load_residual(turn);
@@ -395,8 +409,7 @@ __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[R
       for (int h = 0; h < 8 / kRows; ++h) {
         const int turn = (4 * i + q) * (8 / kRows) + h;
         if (turn + kAhead < kTurns) load_residual(turn + kAhead);
-        const int64_t row = m + kRows * turn + r;
-        const int count = count_of(row);
+        const int count = count_of(turn);
         float v[E];
 #pragma unroll
         for (int w = 0; w < E; w += 4) {
@@ -405,11 +418,12 @@ __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[R
           for (int e = 0; e < 4; ++e) v[w + e] = x[e];
         }
         if constexpr (Out == kForward) {
-          put_forward<T, E, kFull>(g.forward, row, col, count, v, residual[turn % (kAhead + 1)]);
+          put_forward<T, E, kFull>(g.forward, spot_of(turn), count, v, residual[turn % (kAhead + 1)]);
         } else if constexpr (Out == kStore) {
-          if (count > 0) Entries<T, E>::store(static_cast<S *>(g.out.data) + row * g.out.ld + col, count, v);
+          if (count > 0) Entries<T, E>::store(spot_of(turn).template in<S>(g.out), count, v);
         } else {
-          if (count > 0) Entries<F32, E>::store(g.parts + (split * g.M + row) * g.N + col, count, v);
+          const Plane parts{g.parts + split * g.M * g.N, nullptr, g.N, 0};
+          if (count > 0) Entries<F32, E>::store(spot_of(turn).template in<float>(parts), count, v);
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

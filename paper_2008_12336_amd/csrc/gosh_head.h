@@ -126,11 +126,15 @@ struct Span {
       }
     }
   }
+  // Past: of what the caches need not keep.
+  template <bool Past = false>
   static __device__ __forceinline__ void store(void *p, int there, V u) {
     char *c = static_cast<char *>(p);
     if (there >= Bytes) {
       if constexpr (kWords <= 4) {
-        *reinterpret_cast<typename Loosely<V, Align>::At *>(p) = u;
+        typedef typename Loosely<V, Align>::At At;
+        if constexpr (Past) __builtin_nontemporal_store(u, static_cast<At *>(p));
+        else *static_cast<At *>(p) = u;
       } else {
         *reinterpret_cast<Four *>(p) = Four{u[0], u[1], u[2], u[3]};
         *reinterpret_cast<Four *>(c + 16) = Four{u[4], u[5], u[6], u[7]};
@@ -180,11 +184,12 @@ struct Entries {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = T::up(x[i]);
   }
+  template <bool Past = false>
   static __device__ __forceinline__ void store(S *p, int count, const float (&v)[N]) {
     Vec x;
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = T::down(v[i]);
-    Memory::store(p, count * static_cast<int>(sizeof(S)), __builtin_bit_cast(typename Memory::V, x));
+    Memory::template store<Past>(p, count * static_cast<int>(sizeof(S)), __builtin_bit_cast(typename Memory::V, x));
   }
 };
 

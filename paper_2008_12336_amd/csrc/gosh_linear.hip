@@ -97,6 +97,12 @@ double weight_of(TileSize s, bool direct) {
   return s == kLarge ? 1e9 : s == kMiddle ? 1.0 : 1.25;
 }
 
+// Bytes of y from which tiles of kLarge store it past the caches, where nothing else is written: the 256 MB of the cache
+// beside the memory, in which the next reader would not find it anyway.  us with and without, in bf16: 65,536 x 512 ->
+// 2048 with GELU 167 and 187; layer norm, 512 -> 2048 with GELU and 2048 -> 512 after each other, which read what was
+// written, 131,072 rows (y of 537 MB) 695 and 743, 65,536 rows 346 and 360, but 32,768 rows 184 and 178.
+constexpr int64_t kPastCaches = int64_t{256} << 20;
+
 // The tiles of which the busiest of the device's 256 CUs has the least work.  (8,192 x 512 -> 512 in bf16: 18, 15 and
 // 25 us, with 4 tiles, one and a quarter of one to each CU.)
 TileSize tiles_for(int64_t M, int64_t N, bool direct) {
@@ -388,7 +394,8 @@ int gosh_linear(const gosh_mat *x, const gosh_mat *w, const float *bias, int32_t
   if (int rc = check_floats(bias, out, "bias", true)) return rc;
   if (x->rows == 0) return GOSH_OK;
   hipStream_t st = as_stream(hip_stream);
-  ForwardOut f{bias, plane_of(residual), plane_of(y), plane_of(z), plane_of(y8), act, z != nullptr && z->packed};
+  const int32_t past = z == nullptr && y8 == nullptr && x->rows * out * (x->type == GOSH_F32 ? 4 : 2) >= kPastCaches;
+  ForwardOut f{bias, plane_of(residual), plane_of(y), plane_of(z), plane_of(y8), act, z != nullptr && z->packed, past};
   if (few_rows(x->rows, x->cols, out, x->type) && !f.z_packed && y8 == nullptr) {
     if (x->type == GOSH_F32) return launch_few_rows<F32>(x, w, f, st);
     if (x->type == GOSH_BF16) return launch_few_rows<Bf16>(x, w, f, st);

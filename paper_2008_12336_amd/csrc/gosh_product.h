@@ -28,12 +28,16 @@
 
 namespace gosh {
 
-enum ProductOut : int { kForward, kStore, kParts };
+// kPast: kForward of y alone, in tiles of kLarge, past the caches.  (A kernel of its own: as a branch at each store it
+// cost the other calls 2 to 20 %, in registers.)
+enum ProductOut : int { kForward, kStore, kParts, kPast };
+constexpr bool is_forward(ProductOut out) { return out == kForward || out == kPast; }
 
 struct ForwardOut {
   const float *bias;
   Plane residual, y, z, y8;
   int32_t act, z_packed;
+  int32_t past;  // y alone, and too large for the caches
 };
 
 struct ProductArgs {
@@ -42,7 +46,7 @@ struct ProductArgs {
   int64_t k_per_split;    // a multiple of the tile's depth
   int32_t tiles_m, tiles_n, splits;
   int32_t direct;         // 16-bit operands of aligned rows: see can_be_direct
-  ForwardOut forward;     // kForward
+  ForwardOut forward;     // kForward, kPast
   Plane out;              // kStore
   float *parts;           // kParts: splits x M x N; dx in small tiles may have them too
 };
@@ -280,8 +284,8 @@ struct Spot {
   }
 };
 
-// E entries of a row of z become entries of y; r: the residual's.  Full: all of them are there.
-template <typename T, int E, bool Full>
+// E entries of a row of z become entries of y; r: the residual's.  Full: all of them are there.  Past: see kPast.
+template <typename T, int E, bool Full, bool Past>
 __device__ __forceinline__ void put_forward(const ForwardOut &f, const Spot &at, int there, float (&v)[E],
                                             const typename Entries<T, E>::Vec &r) {
   typedef typename T::Store S;
@@ -292,7 +296,7 @@ __device__ __forceinline__ void put_forward(const ForwardOut &f, const Spot &at,
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = i < count ? v[i] : 0.f;  // entries that are not there count in no group
   }
-  if (f.z.data != nullptr) {
+  if (!Past && f.z.data != nullptr) {
     if (f.z_packed) store_packed<T, E>(at.in<int8_t>(f.z), at.exponent_in(f.z), count, v, head, kLanes);
     else if (Full || count > 0) Entries<T, E>::store(at.in<S>(f.z), count, v);
   }
@@ -304,14 +308,14 @@ __device__ __forceinline__ void put_forward(const ForwardOut &f, const Spot &at,
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] += T::up(r[i]);
   }
-  if (f.y8.data != nullptr) {
+  if (!Past && f.y8.data != nullptr) {
     if (!Full) {
 #pragma unroll
       for (int i = 0; i < E; ++i) v[i] = i < count ? v[i] : 0.f;
     }
     store_packed<T, E>(at.in<int8_t>(f.y8), at.exponent_in(f.y8), count, v, head, kLanes);
   }
-  if (Full || count > 0) Entries<T, E>::store(at.in<S>(f.y), count, v);
+  if (Full || count > 0) Entries<T, E>::template store<Past>(at.in<S>(f.y), count, v);
 }
 
 // The id-th tile.
@@ -345,7 +349,7 @@ __device__ __forceinline__ void load_bias(const ProductArgs &g, int64_t n, float
 #pragma unroll
   for (int j = 0; j < RN; ++j) {
     const int64_t col = n + 32 * j + (threadIdx.x & 31);
-    bias[j] = Out == kForward && g.forward.bias != nullptr && col < g.N ? g.forward.bias[col] : 0.f;
+    bias[j] = is_forward(Out) && g.forward.bias != nullptr && col < g.N ? g.forward.bias[col] : 0.f;
   }
 }
 template <int RM, int RN>
@@ -390,7 +394,7 @@ __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[R
   constexpr int kAhead = 2, kTurns = 32 / kRows * RM;
   typename Entries<T, E>::Vec residual[kAhead + 1];
   const auto load_residual = [&](int turn) {
-    if (Out != kForward || g.forward.residual.data == nullptr) return;
+    if (!is_forward(Out) || g.forward.residual.data == nullptr) return;
     residual[turn % (kAhead + 1)] = Entries<T, E>::fetch(spot_of(turn).template in<S>(g.forward.residual), count_of(turn));
   };
 #pragma unroll
@@ -417,8 +421,8 @@ __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[R
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[w + e] = x[e];
         }
-        if constexpr (Out == kForward) {
-          put_forward<T, E, kFull>(g.forward, spot_of(turn), count, v, residual[turn % (kAhead + 1)]);
+        if constexpr (is_forward(Out)) {
+          put_forward<T, E, kFull, Out == kPast>(g.forward, spot_of(turn), count, v, residual[turn % (kAhead + 1)]);
         } else if constexpr (Out == kStore) {
           if (count > 0) Entries<T, E>::store(spot_of(turn).template in<S>(g.out), count, v);
         } else {
@@ -678,7 +682,7 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void d
     const int steps = steps_of(at);
     F16x acc[RM][RN];
     start<RM, RN>(bias, acc);
-    if (Out == kForward && id + turns.step < turns.end)
+    if (is_forward(Out) && id + turns.step < turns.end)
       load_bias<RN, Out>(g, place_of(g, id + turns.step, BM, BN).n0 + wn, bias);
     const auto multiply = [&](int part) {
 #pragma unroll
@@ -744,7 +748,10 @@ int launch_one(const ProductArgs &g, hipStream_t st) {
 template <typename T, TileSize Size>
 int launch_sized(ProductKind kind, const ProductArgs &g, hipStream_t st) {
   switch (kind) {
-    case kProductForward: return launch_one<T, Size, kProductForward, kForward>(g, st);
+    case kProductForward:
+      if constexpr (Size == kLarge && T::kType != GOSH_F32)
+        if (g.forward.past && g.direct) return launch_one<T, Size, kProductForward, kPast>(g, st);
+      return launch_one<T, Size, kProductForward, kForward>(g, st);
     case kProductDx:
       if constexpr (Size == kSmall)
         if (g.parts != nullptr) return launch_one<T, Size, kProductDx, kParts>(g, st);

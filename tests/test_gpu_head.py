@@ -142,6 +142,25 @@ def test_many_rows(shape, dtype):
     test_linear_backward(shape, dtype)
 
 
+@types
+@pytest.mark.parametrize("pad", [0, 8])
+def test_results_larger_than_the_caches(pad, dtype):
+    rows, k, n = 65281, 40, 2056
+    rnd = gen(rows + pad)
+    x, _ = view(rnd(rows, k), dtype, pad, pad)
+    w, _ = view(rnd(n, k) / math.sqrt(k), dtype, pad, pad)
+    b, r = 0.3 * rnd(n), view(rnd(rows, n), dtype, pad, pad)[0]
+    for kind, use_r in ((H.GELU, False), (H.SILU, True), (H.RELU, True), (H.NONE, False)):
+        y, ymem = view(torch.zeros(rows, n, device=DEV), dtype, pad, pad)
+        G.gosh_linear(x, w, y, bias=b, act=kind, residual=r if use_r else None)
+        wy, _, ey, _ = H.linear(x.double(), w.double(), b.double(), kind, r.double() if use_r else None)
+        within(y, wy, H.rounded(ey, wy, dtype), f"y, activation {kind}")
+        again = r.clone()
+        G.gosh_linear(x, w, again, bias=b, act=kind, residual=again if use_r else None)  # in place, and the same bits
+        assert torch.equal(again, y)
+        beside(y, ymem)
+
+
 NORMS = [  # rows, cols, padding, off the start
     (1, 1, 0, 0), (1, 128, 0, 0), (5, 2, 1, 1), (64, 8, 0, 0), (63, 31, 0, 1), (100, 33, 2, 0), (1000, 96, 0, 0),
     (257, 128, 8, 8), (70, 501, 0, 0), (33, 512, 0, 3), (20, 1000, 1, 0), (9, 2048, 0, 0), (5, 2049, 0, 1), (6, 4100, 0, 0),

@@ -227,30 +227,38 @@ __device__ __forceinline__ float top_of(uint32_t byte) {
   return byte >= top ? 63.f : 127.f;
 }
 
-// N entries' q as bytes of words, from entries in 32 bits.  inv = inverse_unit, top = top_of.
+// N entries' q as bytes of words, from entries in 32 bits.  top = top_of.  v / unit is exact, and its sum with 1.5 * 2^23
+// rounds it once, to the nearest whole number (ties to even), whose low byte is the sum's.
 template <int N>
 __device__ __forceinline__ void quantise(const float (&v)[N], uint32_t byte, float top, uint32_t (&q)[N / 4]) {
+  constexpr float kWhole = 12582912.f;
   const float inv = inverse_unit(byte);
+  const uint32_t finite = byte == kNotFinite ? 0 : ~0u;
 #pragma unroll
   for (int w = 0; w < N / 4; ++w) {
-    q[w] = 0;
+    uint32_t n[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = byte == kNotFinite ? 0.f : rintf(v[4 * w + i] * inv);
-      const int n = static_cast<int>(fminf(fmaxf(x, -top), top));
-      q[w] |= (static_cast<uint32_t>(n) & 255u) << (8 * i);
-    }
+    for (int i = 0; i < 4; ++i)
+      n[i] = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fmaf(v[4 * w + i], inv, kWhole), kWhole - top, kWhole + top));
+    const uint32_t lo = __builtin_amdgcn_perm(n[1], n[0], 0x0c0c0400), hi = __builtin_amdgcn_perm(n[3], n[2], 0x04000c0c);
+    q[w] = (lo | hi) & finite;
   }
 }
 
-// The largest magnitude, as bits, of N entries and of those of the other lanes of a group of `lanes` (1 to 8).
+// The largest magnitude, as bits, of N entries and of those of the other lanes of a group of `lanes` (1, 2, 4 or 8).
 // Bits order as magnitudes do, with infinity and then NaN on top, where a comparison of floats would drop a NaN.
+template <int Swap>
+__device__ __forceinline__ uint32_t larger_of_lanes(uint32_t x) {
+  return max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), Swap, 0xf, 0xf, true)));
+}
 template <int N>
 __device__ __forceinline__ uint32_t most_bits(const float (&v)[N], int lanes) {
   uint32_t most = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
-  for (int s = 1; s < lanes; s *= 2) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), s)));
+  if (lanes > 1) most = larger_of_lanes<0xb1>(most);   // the other lane of two
+  if (lanes > 2) most = larger_of_lanes<0x4e>(most);   // the other two of four
+  if (lanes > 4) most = larger_of_lanes<0x141>(most);  // one of the other four of eight: the half row mirrored
   return most;
 }
 

@@ -246,16 +246,17 @@ __device__ __forceinline__ void quantise(const float (&v)[N], uint32_t byte, flo
 }
 
 // The largest magnitude, as bits, of N entries and of those of the other lanes of a group of `lanes` (1, 2, 4 or 8).
-// Bits order as magnitudes do, with infinity and then NaN on top, where a comparison of floats would drop a NaN.
+// Bits order as magnitudes do, with infinity and then NaN on top.
 template <int Swap>
 __device__ __forceinline__ uint32_t larger_of_lanes(uint32_t x) {
   return max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), Swap, 0xf, 0xf, true)));
 }
 template <int N>
 __device__ __forceinline__ uint32_t most_bits(const float (&v)[N], int lanes) {
-  uint32_t most = 0;
+  float largest = 0.f;  // or a NaN, which this maximum keeps
 #pragma unroll
-  for (int i = 0; i < N; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+  for (int i = 0; i < N; ++i) largest = __builtin_elementwise_maximum(largest, __builtin_fabsf(v[i]));
+  uint32_t most = __float_as_uint(largest) & 0x7fffffffu;
   if (lanes > 1) most = larger_of_lanes<0xb1>(most);   // the other lane of two
   if (lanes > 2) most = larger_of_lanes<0x4e>(most);   // the other two of four
   if (lanes > 4) most = larger_of_lanes<0x141>(most);  // one of the other four of eight: the half row mirrored

@@ -135,7 +135,7 @@ int join_parts(const JoinJob *jobs, int how_many, hipStream_t st) {
 namespace {
 
 // A lane has 8 columns, four lanes a group; 64 groups a workgroup and turn.  Bound by memory: 2^20 x 512 in bf16 are packed
-// in 335 us and unpacked in 265, 4.8 and 6.1 TB/s (reads are cheaper than writes).
+// in 290 us and unpacked in 265, 5.6 and 6.1 TB/s (reads are cheaper than writes).
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(const Plane x, const Plane q, int64_t rows, int32_t cols, int32_t groups) {
   const int64_t total = rows * groups;

@@ -8,13 +8,15 @@
 //
 // Three ways, all ending in the same epilogue.  Aligned 16-bit rows go straight to LDS, in tiles of 256 x 256 by eight
 // wavefronts where there are enough: 65,536 x 512 x 2048 takes 137 to 150 us (0.9 to 1.0 PFLOP/s; a large product of the
-// vendor's library reaches 1.33), and with K = 512, where the epilogue counts, 262,144 x 512 -> 2048 683 us without and
-// 755 with GELU.  There each tile costs 13.7 us of products and 10 of epilogue (8.5 of them instructions, beside 6 of
-// stores): the eight wavefronts go through them together, and tiles of 128 x 128, two workgroups to a CU, which do
-// overlap them, lose more to fetching (914 us).  Other tiles pass through registers on their way to LDS (32-bit entries,
-// odd strides): 65,536 x 1024 -> 1024 in f32 takes 746 us, 184 TFLOP/s (that library: 144 to 152); their instructions
-// and products take turns on each SIMD (54 % of its time are products).  A packed x of dw is widened in registers beside
-// direct tiles of dz: 196 us for 131,072 x 512 and 1024, against 143 unpacked.
+// vendor's library reaches 1.33), and with K = 512, where the epilogue counts, 262,144 x 512 -> 2048 652 us without and
+// 722 with GELU.  There each tile costs some 14 us of products and then, since the eight wavefronts go through it
+// together, 6 of epilogue, 9 with GELU; its stores alone need 4.9 at the rate of a fill.  One instruction in six less,
+// workgroups that start at different times, rows of 256 bytes and rows fetched from LDS ahead of the stores changed
+// nothing; tiles of 128 x 128, two workgroups to a CU, which do overlap both, lose more to fetching (914 us).  Other
+// tiles pass through registers on their way to LDS (32-bit entries, odd strides): 65,536 x 1024 -> 1024 in f32 takes
+// 746 us, 184 TFLOP/s (that library: 144 to 152); their instructions and products take turns on each SIMD (54 % of its
+// time are products).  A packed x of dw is widened in registers beside direct tiles of dz: 193 us for 131,072 x 512 and
+// 1024, against 143 unpacked, also where the widening lies between the products.
 //
 // 32-bit entries are taken apart into three bf16 parts, x = h + m + l, each the nearest to what the ones before leave
 // (|m| <= 2^-9 |x|, |l| <= 2^-18 |x|, nothing is left), and their products summed as hh + hm + mh + hl + mm + lh in the

@@ -478,13 +478,16 @@ __device__ __forceinline__ void staged_product(const ProductArgs &g, int id, uin
   start<R, R>(bias, acc);
 
   // The last step's chunks may be short: along k where K is no multiple of 8; along m the very last row of memory ends
-  // inside its last chunk, of which the hardware's bounds check drops a dword that is only half there.
+  // inside its last chunk, of which the hardware's bounds check drops a dword that is only partly there.  Along m a row of an
+  // earlier step has at least one row after it, whose bytes complete its last dword: up to 2 of them are missing in 16-bit
+  // rows, none in 32-bit ones, and 3 in packed ones, which rows less than 3 bytes apart do not have.
   const bool ragged_a = a_k ? k1 % 8 != 0 : g.M % 8 != 0, ragged_b = b_k ? k1 % 8 != 0 : g.N % 8 != 0;
+  const bool always_b = Kind == kProductDwPacked && g.b.ld < 3;
   TA a;
   TB b;
   if (steps > 0) {
     a.fetch(g.a, m0, g.M, k0, k1, steps == 1 && ragged_a);
-    b.fetch(g.b, n0, g.N, k0, k1, steps == 1 && ragged_b);
+    b.fetch(g.b, n0, g.N, k0, k1, always_b || (steps == 1 && ragged_b));
     a.put(lds);
     b.put(lds + TA::kBytes / 2);
   }
@@ -496,7 +499,7 @@ __device__ __forceinline__ void staged_product(const ProductArgs &g, int id, uin
       const int64_t k = k0 + static_cast<int64_t>(s + 1) * BK;
       const bool last = s + 2 == steps;
       a.fetch(g.a, m0, g.M, k, k1, last && ragged_a);
-      b.fetch(g.b, n0, g.N, k, k1, last && ragged_b);
+      b.fetch(g.b, n0, g.N, k, k1, always_b || (last && ragged_b));
     }
 #pragma unroll
     for (int kk = 0; kk < BK / 16; ++kk) {

@@ -1,0 +1,84 @@
+"""The head's operators on matrices laid out in ways that Packed8 and ordinary tensors are not: rows as close to each other
+as the entry points allow, of fewer entries than a load fetches, with bounds from head_model.py."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+import paper_2008_12336_amd as G
+from tests import head_model as H
+from tests.test_gpu_head import DEV, NAMES, gen, types, within
+
+pytestmark = pytest.mark.gpu
+
+
+class Eight:
+    """An 8-bit form with rows `ld` bytes and their exponents `ld_exps` bytes apart, `off` bytes off the start of memory
+    that holds 99 besides."""
+
+    def __init__(self, rows, cols, dtype, ld, ld_exps, off=0):
+        groups = -(-cols // 32)
+        self.cols = cols
+        self.bytes = torch.full((off + (rows - 1) * ld + cols + 8,), 99, dtype=torch.int8, device=DEV)
+        self.units = torch.full((off + (rows - 1) * ld_exps + groups + 8,), 99, dtype=torch.uint8, device=DEV)
+        self.q = torch.as_strided(self.bytes, (rows, cols), (ld, 1), off)
+        self.exps = torch.as_strided(self.units, (rows, groups), (ld_exps, 1), off)
+        kind = {torch.float32: G.GOSH_F32, torch.bfloat16: G.GOSH_BF16, torch.float16: G.GOSH_F16}[dtype]
+        self.mat = G.gosh_mat(self.q.data_ptr(), self.exps.data_ptr(), rows, ld, ld_exps, cols, kind, 1)
+
+    def values(self):
+        return H.values(self.q.cpu(), self.exps.cpu()).to(DEV)
+
+    def beside(self):
+        """Memory beside the matrix holds 99 still."""
+        self.q.fill_(99), self.exps.fill_(99)
+        assert (self.bytes == 99).all() and (self.units == 99).all()
+
+
+def mat(t):
+    """A tensor's view, whatever its strides."""
+    kind = {torch.float32: G.GOSH_F32, torch.bfloat16: G.GOSH_BF16, torch.float16: G.GOSH_F16}[t.dtype]
+    return G.gosh_mat(t.data_ptr(), None, t.shape[0], t.stride(0), 0, t.shape[1], kind, 0)
+
+
+def check(rc):
+    assert rc == 0, G.gosh_last_error()
+
+
+def pack(x, p):
+    check(G.lib().gosh_pack8(C.byref(mat(x)), C.byref(p.mat), torch.cuda.current_stream().cuda_stream))
+
+
+def backward(dy, x, w, dx, dw, db):
+    """The gradient of a layer without an activation; x: a view."""
+    kind = mat(dy).type
+    n = G.gosh_linear_backward_workspace(dy.shape[0], w.shape[1], w.shape[0], kind, H.NONE)
+    work = torch.empty(n, dtype=torch.uint8, device=DEV)
+    check(G.lib().gosh_linear_backward(C.byref(mat(dy)), C.byref(x), C.byref(mat(w)), None, H.NONE,
+                                       None if dx is None else C.byref(mat(dx)), C.byref(mat(dw)), db.data_ptr(),
+                                       work.data_ptr(), n, torch.cuda.current_stream().cuda_stream))
+
+
+@types
+@pytest.mark.parametrize("rows", [33, 34, 35, 65, 66, 67, 129, 577])
+def test_gradient_of_few_columns_without_padding(rows, dtype):
+    """Rows of fewer bytes than a load, in matrices that end with them: what a load reaches past its row lies in the rows
+    after it, of which the last step of the sum may hold one.  Bounds as in test_linear_backward."""
+    for k, n, more in ((1, 1, 0), (1, 5, 1), (1, 64, 2), (2, 3, 0), (2, 8, 1), (3, 1, 0), (5, 7, 0), (7, 2, 0), (6, 4, 1)):
+        rnd = gen(rows * 64 + k * 8 + n)
+        x, w, dy = rnd(rows, k).to(dtype), rnd(n, k).to(dtype), (0.1 * rnd(rows, n)).to(dtype)
+        p = Eight(rows, k, dtype, k + more, 1)
+        pack(x, p)
+        for name, view, open_ in (("x", mat(x), x.double()), ("packed x", p.mat, p.values())):
+            want, bounds = H.linear_backward(dy.double(), open_, w.double(), None, H.NONE, dtype)
+            for with_dx in (True, False):
+                dx = torch.empty(rows, k, dtype=dtype, device=DEV) if with_dx else None
+                dw, db = torch.empty(n, k, device=DEV), torch.empty(n, device=DEV)
+                backward(dy, view, w, dx, dw, db)
+                what = f"{rows} x {k} -> {n}, {name} with rows {view.ld} apart, {NAMES[dtype]}"
+                within(dw, want[1], H.rounded(bounds[1], want[1], torch.float32), f"dw of {what}")
+                within(db, want[2], H.rounded(bounds[2], want[2], torch.float32), f"db of {what}")
+                if with_dx:
+                    within(dx, want[0], H.rounded(bounds[0], want[0], dtype), f"dx of {what}")
+        p.beside()

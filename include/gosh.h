@@ -593,7 +593,7 @@ int gosh_linear(const gosh_mat *x, const gosh_mat *w, const float *bias, int32_t
  * rows x in; dw: out x in; db: out floats.  Any of the three may be NULL; w may be NULL if dx is, x if dw is.  All
  * of one type, but dw may be GOSH_F32.  dz is rounded to that type before the two products, not in db.  With rows = 0
  * dw and db are zero.  dx must not overlap dy, x, w or z.
- * workspace: as above, at least gosh_linear_backward_workspace bytes. */
+ * workspace: as above, at least gosh_linear_backward_workspace bytes (where db is all that is asked for, those of any in). */
 int gosh_linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, const gosh_mat *z, int32_t act,
                          const gosh_mat *dx, const gosh_mat *dw, float *db, void *workspace, uint64_t workspace_bytes,
                          void *hip_stream);

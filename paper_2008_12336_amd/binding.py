@@ -705,8 +705,10 @@ def gosh_linear_backward(dy: torch.Tensor, x, w, z, act: int = GOSH_ACT_NONE, dx
     """dx, dw and db (those that are given) of gosh_linear; x and z: tensors or Packed8."""
     v = _mat(dy, "dy")
     into = dx if dx is not None else dw
-    cols = into.shape[1] if into is not None else 1
-    workspace = _workspace(workspace, gosh_linear_backward_workspace(v.rows, cols, v.cols, v.type, act), stream, dy.device)
+    # db alone needs neither the products' parts nor dz
+    nbytes = (gosh_linear_backward_workspace(v.rows, 1, v.cols, v.type, GOSH_ACT_NONE) if into is None else
+              gosh_linear_backward_workspace(v.rows, into.shape[1], v.cols, v.type, act))
+    workspace = _workspace(workspace, nbytes, stream, dy.device)
     _check(lib().gosh_linear_backward(v, _mat(x, "x"), _mat(w, "w"), _mat(z, "z"), act, _mat(dx, "dx"), _mat(dw, "dw"),
                                       _floats(db, "db", v.cols), workspace.data_ptr() or None, workspace.numel(),
                                       _stream(stream)))

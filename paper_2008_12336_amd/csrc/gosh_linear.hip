@@ -282,6 +282,7 @@ struct BackwardPlan {
   int64_t dz_ld;
   int32_t dx_splits;
   uint64_t dz, dw_parts, db_parts, dx_parts, bytes;  // offsets, and the whole
+  uint64_t db_alone() const { return dx_parts - db_parts; }  // the whole where db is all that is asked for
 };
 BackwardPlan plan_backward(int64_t rows, int32_t in, int32_t out, int32_t type, int32_t act) {
   BackwardPlan p;
@@ -305,7 +306,8 @@ int linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *w, co
   const int64_t rows = dy->rows;
   const BackwardPlan p = plan_backward(rows, in, out, T::kType, act);
   char *const ws = static_cast<char *>(workspace);
-  float *const dw_parts = reinterpret_cast<float *>(ws + p.dw_parts), *const db_parts = reinterpret_cast<float *>(ws + p.db_parts);
+  float *const dw_parts = reinterpret_cast<float *>(ws + p.dw_parts);
+  float *const db_parts = reinterpret_cast<float *>(ws + (dx != nullptr || dw != nullptr ? p.db_parts : 0));
   Plane dz = plane_of(dy);
   if (rows > 0 && (db != nullptr || act != GOSH_ACT_NONE)) {
     Plane to{nullptr, nullptr, 0, 0};
@@ -430,7 +432,7 @@ int gosh_linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *
   if (int rc = check_mat(dw, "dw", kOptional)) return rc;
   const int32_t out = dy->cols;
   if (dx == nullptr && dw == nullptr && db == nullptr) return GOSH_OK;
-  const int32_t in = dx != nullptr ? dx->cols : dw != nullptr ? dw->cols : 1;
+  const int32_t in = dx != nullptr ? dx->cols : dw != nullptr ? dw->cols : x != nullptr ? x->cols : w != nullptr ? w->cols : 1;
   if (int rc = check_shape(x, "x", dy->rows, in)) return rc;
   if (int rc = check_shape(w, "w", out, in)) return rc;
   if (int rc = check_shape(z, "z", dy->rows, out)) return rc;
@@ -442,7 +444,8 @@ int gosh_linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *
   if (dw != nullptr && dw->type != GOSH_F32)
     if (int rc = check_type(dw, "dw", dy->type)) return rc;
   if (int rc = check_floats(db, out, "db", true)) return rc;
-  if (int rc = check_workspace(workspace, workspace_bytes, plan_backward(dy->rows, in, out, dy->type, act).bytes)) return rc;
+  const BackwardPlan plan = plan_backward(dy->rows, in, out, dy->type, act);
+  if (int rc = check_workspace(workspace, workspace_bytes, dx != nullptr || dw != nullptr ? plan.bytes : plan.db_alone())) return rc;
   hipStream_t st = as_stream(hip_stream);
   if (dy->type == GOSH_F32) return linear_backward<F32>(dy, x, w, z, act, dx, dw, db, workspace, in, out, st);
   if (dy->type == GOSH_BF16) return linear_backward<Bf16>(dy, x, w, z, act, dx, dw, db, workspace, in, out, st);

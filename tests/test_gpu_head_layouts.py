@@ -82,3 +82,26 @@ def test_gradient_of_few_columns_without_padding(rows, dtype):
                 if with_dx:
                     within(dx, want[0], H.rounded(bounds[0], want[0], dtype), f"dx of {what}")
         p.beside()
+
+
+@types
+@pytest.mark.parametrize("rows", [0, 1, 700, 20011])
+def test_the_bias_gradient_alone(rows, dtype):
+    """db without dx and dw, with and without the operands that only those need; the same bits as beside them."""
+    k, n = 40, 77
+    rnd = gen(rows + 5)
+    x, w = rnd(rows, k).to(dtype), rnd(n, k).to(dtype)
+    dy, z = (0.1 * rnd(rows, n)).to(dtype), (2 * rnd(rows, n)).to(dtype)
+    z8 = G.Packed8(rows, n, dtype, DEV)
+    G.gosh_pack8(z, z8)
+    for kind, zz in ((H.NONE, None), (H.RELU, z), (H.GELU, z8), (H.SILU, z)):
+        full, dw = torch.empty(n, device=DEV), torch.empty_like(w)
+        G.gosh_linear_backward(dy, x, w, zz, kind, dw=dw, db=full)
+        open_ = z8 if zz is z8 else None
+        z64 = z.double() if open_ is None else H.values(z8.q[:, :n].cpu(), z8.exps.cpu()).to(DEV)
+        want, bounds = H.linear_backward(dy.double(), x.double(), w.double(), z64, kind, dtype)
+        for xx, ww in ((x, w), (x, None), (None, w), (None, None)):
+            db = torch.full((n,), 77.0, device=DEV)
+            G.gosh_linear_backward(dy, xx, ww, zz, kind, db=db)
+            within(db, want[2], H.rounded(bounds[2], want[2], torch.float32), f"db alone, activation {kind}")
+            assert torch.equal(db, full)

@@ -600,7 +600,8 @@ _TYPES = {torch.float32: GOSH_F32, torch.bfloat16: GOSH_BF16, torch.float16: GOS
 
 class Packed8:
     """The 8-bit form of a rows x cols matrix of `dtype`: int8 entries `q` (rows padded to 16) and one exponent byte for
-    each group of 32 columns, `exps`.  Uninitialised; gosh_pack8, gosh_layer_norm and gosh_linear write it."""
+    each group of 32 columns, `exps`.  Uninitialised; gosh_pack8, gosh_layer_norm and gosh_linear write it.  q and exps may
+    be replaced, by tensors of at least as many columns whose rows are contiguous: a call takes those of that moment."""
 
     def __init__(self, rows: int, cols: int, dtype: torch.dtype, device="cuda"):
         if dtype not in _TYPES:
@@ -608,14 +609,31 @@ class Packed8:
         self.rows, self.cols, self.dtype = rows, cols, dtype
         self.q = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.int8, device=device)
         self.exps = torch.empty(rows, -(-cols // 32), dtype=torch.uint8, device=device)
-        self._mat = gosh_mat(self.q.data_ptr() or None, self.exps.data_ptr() or None, rows, self.q.shape[1],
-                             self.exps.shape[1], cols, _TYPES[dtype], 1)
+
+    def _mat(self, name: str) -> gosh_mat:
+        q, exps, rows, cols = self.q, self.exps, self.rows, self.cols
+        if q.dtype != torch.int8 or exps.dtype != torch.uint8:
+            raise TypeError(f"{name}: q must be int8 and exps uint8")
+        groups = -(-cols // 32)
+        ld, ld_exps = _rows_apart(q, rows, cols), _rows_apart(exps, rows, groups)
+        if ld is None or ld_exps is None:
+            raise TypeError(f"{name}: q and exps must have {rows} rows of at least {cols} and {groups} contiguous entries")
+        return gosh_mat(q.data_ptr() or None, exps.data_ptr() or None, rows, ld, ld_exps, cols, _TYPES[self.dtype], 1)
+
+
+def _rows_apart(t: torch.Tensor, rows: int, least: int):
+    """The stride of the rows, or None where t is no matrix of `rows` contiguous rows of `least` entries."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != rows or shape[1] < least:
+        return None
+    ld, along = t.stride()
+    return None if along != 1 and shape[1] > 1 else ld if rows > 1 else max(least, 1)
 
 
 def _mat(m, name: str):
     """A 2-D tensor whose rows are contiguous, or a Packed8, as the library sees it."""
     if isinstance(m, Packed8):
-        return m._mat
+        return m._mat(name)
     if m is None:
         return None
     kind = _TYPES.get(m.dtype)

@@ -105,3 +105,20 @@ def test_the_bias_gradient_alone(rows, dtype):
             G.gosh_linear_backward(dy, xx, ww, zz, kind, db=db)
             within(db, want[2], H.rounded(bounds[2], want[2], torch.float32), f"db alone, activation {kind}")
             assert torch.equal(db, full)
+
+
+def test_an_8_bit_form_that_was_moved():
+    """Saved activations that went to the host and back, while other data took their place: calls use the new tensors."""
+    rnd = gen(12)
+    x, out = rnd(300, 70), torch.empty(300, 70, device=DEV)
+    p = G.Packed8(300, 70, torch.float32, DEV)
+    G.gosh_pack8(x, p)
+    want = H.values(p.q[:, :70].cpu(), p.exps.cpu())
+    old = p.q, p.exps
+    p.q, p.exps = p.q.cpu(), p.exps.cpu()
+    with pytest.raises(G.GoshError, match="not memory"):
+        G.gosh_unpack8(p, out)
+    p.q, p.exps = p.q.to(DEV), p.exps.to(DEV)
+    old[0].fill_(1), old[1].fill_(1)
+    G.gosh_unpack8(p, out)
+    assert torch.equal(out.double().cpu(), want)

@@ -595,9 +595,13 @@ struct DirectTile {
     for (int i = 0; i < kLoads; ++i) {
       uint32_t o = off[i];
       if (KMajor) o = along[i] < left ? o : kNowhere;
-      // m0 holds where the first lane's bytes land; the load has no destination register
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                   :: "s"(lds + (wave * kLoads + i) * 1024), "v"(o), "s"(range) : "memory");
+      // m0, which the compiler sets, holds where the first lane's bytes land; the load has no destination register.  The
+      // compiler does not count the wait states of an instruction that it cannot see: s_nop 4 are the five that the load
+      // needs behind a vector instruction that wrote its range (a spilled register read back), more than behind m0's move.
+      // With the builtin for this load the compiler waits for all under way before a step's transposing reads: 482 instead of
+      // 455 us for the gradient of 65,536 x 512 -> 2048.
+      asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+                   :: "v"(o), "s"(range), "{m0}"(lds + (wave * kLoads + i) * 1024) : "memory");
     }
     const int64_t move = KMajor ? BK * 2 : static_cast<int64_t>(p.ld) * (BK * 2);
     base += move;

@@ -122,7 +122,8 @@ int64_t split_length(int64_t k, int64_t splits) { return ceil_div(ceil_div(k, sp
 template <typename T>
 TileSize shape_rows(ProductKind kind, int64_t rows, ProductArgs &g) {
   g.direct = T::kType != GOSH_F32 && can_be_direct(g.a, g.K) && can_be_direct(g.b, kind == kProductForward ? g.K : g.N);
-  const TileSize size = tiles_for(rows, g.N, g.direct);
+  // a split sum was planned in tiles of kSmall, before it was known whether they are direct; only those store parts
+  const TileSize size = g.parts != nullptr ? kSmall : tiles_for(rows, g.N, g.direct);
   g.M = rows;
   g.tiles_m = static_cast<int32_t>(std::min<int64_t>(ceil_div(rows, tile_m(size)), 1 << 30));
   g.tiles_n = static_cast<int32_t>(ceil_div(g.N, tile_n(size)));

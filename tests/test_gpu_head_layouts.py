@@ -122,3 +122,19 @@ def test_an_8_bit_form_that_was_moved():
     old[0].fill_(1), old[1].fill_(1)
     G.gosh_unpack8(p, out)
     assert torch.equal(out.double().cpu(), want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=lambda t: NAMES[t])
+@pytest.mark.parametrize("rows", [1, 63, 64, 200, 1000, 4000])
+def test_a_split_dx_of_rows_off_alignment(rows, dtype):
+    """dx whose long sum is split, of aligned rows and of others, which are planned alike and stored in the same tiles."""
+    k, n = 96, 2056
+    rnd = gen(rows + 9)
+    dy, w = (0.1 * rnd(rows, n)).to(dtype), (rnd(n, k) / math.sqrt(k)).to(dtype)
+    for pad in (0, 1):
+        dys, ws = torch.zeros(rows, n + pad, dtype=dtype, device=DEV)[:, :n], torch.zeros(n, k + pad, dtype=dtype, device=DEV)[:, :k]
+        dys.copy_(dy), ws.copy_(w)
+        dx = torch.full((rows, k), 77.0, dtype=dtype, device=DEV)
+        G.gosh_linear_backward(dys, None, ws, None, H.NONE, dx=dx)
+        want, bounds = H.linear_backward(dy.double(), torch.zeros(rows, k, device=DEV).double(), w.double(), None, H.NONE, dtype)
+        within(dx, want[0], H.rounded(bounds[0], want[0], dtype), f"dx, rows {pad} entries apart")

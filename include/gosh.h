@@ -567,7 +567,8 @@ int gosh_layer_norm(const gosh_mat *x, const float *gamma, const float *beta, fl
  * add: the gradient that reaches x beside the norm (a residual branch), or NULL.  dx may be dy or add.  dx, or both
  * dgamma and dbeta, may be NULL.  With rows = 0 dgamma and dbeta are zero.
  * workspace: device memory of at least gosh_layer_norm_workspace(rows, cols) bytes, 16-byte aligned, that no other
- * work uses until the call's is done (nothing is kept in it; NULL where that is 0 or dgamma is NULL). */
+ * work uses until the call's is done (nothing is kept in it; NULL where that is 0 or dgamma is NULL).  The function is 0
+ * for rows = 0 and for sizes that the call refuses. */
 int gosh_layer_norm_backward(const gosh_mat *dy, const gosh_mat *x, const float *gamma, const float *mean,
                              const float *rstd, const gosh_mat *add, const gosh_mat *dx, float *dgamma, float *dbeta,
                              void *workspace, uint64_t workspace_bytes, void *hip_stream);

@@ -14,6 +14,7 @@ namespace gosh {
 
 enum MatUse : int { kMayBePacked = 1, kMustBePacked = 2, kOptional = 4 };
 
+inline bool rows_fit(int64_t rows) { return rows >= 0 && rows < 2147483647LL; }
 // A matrix argument: its fields, and that its memory is there.  GOSH_OK also for an optional one that is null.
 int check_mat(const gosh_mat *m, const char *what, int use = 0);
 // Two matrices of one shape, or GOSH_EINVAL.

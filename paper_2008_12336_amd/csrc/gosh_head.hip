@@ -18,7 +18,7 @@ int check_mat(const gosh_mat *m, const char *what, int use) {
   if (m->packed != 0 && m->packed != 1) return fail(GOSH_EINVAL, "%s: packed = %d: must be 0 or 1", what, m->packed);
   if (m->packed && !(use & (kMayBePacked | kMustBePacked))) return fail(GOSH_EINVAL, "%s must not be packed", what);
   if (!m->packed && (use & kMustBePacked)) return fail(GOSH_EINVAL, "%s must be packed", what);
-  if (m->rows < 0 || m->rows >= 2147483647LL)
+  if (!rows_fit(m->rows))
     return fail(GOSH_EINVAL, "%s: rows = %lld: must be in [0, 2^31-1)", what, (long long)m->rows);
   if (m->cols < 1 || m->cols > GOSH_MAT_MAX_COLS)
     return fail(GOSH_EINVAL, "%s: cols = %d: must be in [1, %d]", what, m->cols, GOSH_MAT_MAX_COLS);

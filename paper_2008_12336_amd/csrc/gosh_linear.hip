@@ -416,7 +416,8 @@ int gosh_linear(const gosh_mat *x, const gosh_mat *w, const float *bias, int32_t
 }
 
 uint64_t gosh_linear_backward_workspace(int64_t rows, int32_t in, int32_t out, int32_t type, int32_t act) {
-  if (rows < 0 || in < 1 || out < 1 || in > GOSH_MAT_MAX_COLS || out > GOSH_MAT_MAX_COLS) return 0;
+  if (!gosh::rows_fit(rows) || in < 1 || out < 1 || in > GOSH_MAT_MAX_COLS || out > GOSH_MAT_MAX_COLS) return 0;
+  if (type < GOSH_F32 || type > GOSH_F16 || act < GOSH_ACT_NONE || act > GOSH_ACT_SILU) return 0;
   return gosh::plan_backward(rows, in, out, type, act).bytes;
 }
 

@@ -521,7 +521,7 @@ int gosh_layer_norm(const gosh_mat *x, const float *gamma, const float *beta, fl
 }
 
 uint64_t gosh_layer_norm_workspace(int64_t rows, int32_t cols) {
-  if (rows < 1 || cols < 1 || cols > GOSH_MAT_MAX_COLS) return 0;
+  if (rows < 1 || !gosh::rows_fit(rows) || cols < 1 || cols > GOSH_MAT_MAX_COLS) return 0;
   return static_cast<uint64_t>(gosh::back_blocks(rows)) * 2 * cols * 4;
 }
 

@@ -67,3 +67,15 @@ def test_an_8_bit_form_is_copied_and_pickled():
     for c in (copy.deepcopy(p), pickle.loads(pickle.dumps(p))):
         assert torch.equal(c.q, p.q) and torch.equal(c.exps, p.exps) and (c.rows, c.cols, c.dtype) == (3, 40, torch.float16)
         assert G.binding._mat(c, "q").data == c.q.data_ptr() != p.q.data_ptr()
+
+
+def test_workspaces_of_what_is_refused():
+    """Sizes, types and activations that a call refuses have no workspace, however large: nothing overflows."""
+    most = 2 ** 31 - 2
+    for rows in (-1, most + 1, 2 ** 62, 2 ** 63 - 1):
+        assert G.gosh_layer_norm_workspace(rows, 64) == 0
+        assert G.gosh_linear_backward_workspace(rows, 64, 64, G.GOSH_BF16, H.GELU) == 0
+    for type_, act in ((-1, H.NONE), (3, H.NONE), (G.GOSH_F32, -1), (G.GOSH_F32, 4)):
+        assert G.gosh_linear_backward_workspace(10, 64, 64, type_, act) == 0
+    assert G.gosh_layer_norm_workspace(most, 65536) == 1024 * 2 * 65536 * 4
+    assert G.gosh_linear_backward_workspace(most, 65536, 65536, G.GOSH_F32, H.SILU) > most * 65536 * 4 + 65536 * 65536 * 4

@@ -584,8 +584,10 @@ uint64_t gosh_layer_norm_workspace(int64_t rows, int32_t cols);
 /* Linear layer: z = x w^T + bias, y = act(z) + residual.  x: rows x in; w: out x in; y: rows x out; all of one type,
  * not packed.  bias: out floats, or NULL.  residual: as y, or NULL; it may be y itself.  z, y8: what the backward pass
  * wants, or NULL: z as y, or packed; y8 packed, of y (both from the values in 32 bits).  y must not overlap x or w.
- * Products are summed in 32 bits; those of GOSH_F32 have the accuracy of 32-bit products.  Not-finite entries reach the
- * results that they are part of and no others; an infinite one of GOSH_F32 (or one over 3.39e38) may give NaN there. */
+ * Products, here and in the gradient, are summed in 32 bits; those of GOSH_F32 have the accuracy of 32-bit products where
+ * both entries are 0 or 2^-110 (7.7e-34) or more in magnitude; a smaller one may count as another, up to 2^-134 off.
+ * Not-finite entries reach the results that they are part of and no others; an infinite one of GOSH_F32 (or one over
+ * 3.39e38) may give NaN there. */
 int gosh_linear(const gosh_mat *x, const gosh_mat *w, const float *bias, int32_t act, const gosh_mat *residual,
                 const gosh_mat *y, const gosh_mat *z, const gosh_mat *y8, void *hip_stream);
 

@@ -19,9 +19,10 @@
 // 1024, against 143 unpacked, also where the widening lies between the products.
 //
 // 32-bit entries are taken apart into three bf16 parts, x = h + m + l, each the nearest to what the ones before leave
-// (|m| <= 2^-9 |x|, |l| <= 2^-18 |x|, nothing is left), and their products summed as hh + hm + mh + hl + mm + lh in the
-// 32-bit accumulators: what is left out is 2^-26 of a product, less than 32 bits round it by.  Six bf16 products of the
-// matrix cores take three eighths of the time of one in 32 bits.  What an infinity leaves is NaN.
+// (|m| <= 2^-9 |x|, |l| <= 2^-18 |x|, nothing is left from |x| = 2^-110 on; of smaller ones up to 2^-134, half of the least
+// bf16 number, which the matrix cores take as it is), and their products summed as hh + hm + mh + hl + mm + lh in the 32-bit
+// accumulators: what is left out is 2^-26 of a product, less than 32 bits round it by.  Six bf16 products of the matrix
+// cores take three eighths of the time of one in 32 bits.  What an infinity leaves is NaN.
 #pragma once
 
 #include <type_traits>

@@ -138,3 +138,30 @@ def test_a_split_dx_of_rows_off_alignment(rows, dtype):
         G.gosh_linear_backward(dys, None, ws, None, H.NONE, dx=dx)
         want, bounds = H.linear_backward(dy.double(), torch.zeros(rows, k, device=DEV).double(), w.double(), None, H.NONE, dtype)
         within(dx, want[0], H.rounded(bounds[0], want[0], dtype), f"dx, rows {pad} entries apart")
+
+
+@pytest.mark.parametrize("exponent", [-108, -112, -116, -120, -126, -131])
+def test_small_entries_in_32_bits(exponent):
+    """Entries of 32 bits down to the least ones.  From 2^-110 on the tiles' three bf16 parts hold an entry wholly; below,
+    what is left is at most 2^-134, half of the least bf16 number, and the products that are left out are under 2^-8 of
+    that: 1.01 * 2^-134 times the other operand.  A few rows are multiplied as they are.  The other operand is large, so
+    that no result is near the end of the range."""
+    k, n, least = 96, 64, 1.01 * 2.0 ** -134
+    for rows in (5, 3000):
+        rnd = gen(rows - exponent)
+        x, w = rnd(rows, k) * 2.0 ** exponent, rnd(n, k) * 2.0 ** 40
+        y = torch.empty(rows, n, device=DEV)
+        G.gosh_linear(x, w, y)
+        x64, w64 = x.double(), w.double()
+        wy, _, ey, _ = H.linear(x64, w64, None, H.NONE, None)
+        if rows > 1024:
+            ey = ey + least * (x64.abs() < 2.0 ** -110).double() @ w64.abs().t()
+        within(y, wy, H.rounded(ey, wy, torch.float32), f"y of {rows} rows")
+        dy, big = rnd(rows, n) * 2.0 ** exponent, rnd(rows, k) * 2.0 ** 40
+        dx, dw, db = torch.empty(rows, k, device=DEV), torch.empty(n, k, device=DEV), torch.empty(n, device=DEV)
+        G.gosh_linear_backward(dy, big, w, None, H.NONE, dx=dx, dw=dw, db=db)
+        want, bounds = H.linear_backward(dy.double(), big.double(), w64, None, H.NONE, torch.float32)
+        small = least * (dy.double().abs() < 2.0 ** -110).double()
+        within(dx, want[0], H.rounded(bounds[0] + small @ w64.abs(), want[0], torch.float32), f"dx of {rows} rows")
+        within(dw, want[1], H.rounded(bounds[1] + small.t() @ big.double().abs(), want[1], torch.float32), f"dw of {rows} rows")
+        within(db, want[2], H.rounded(bounds[2], want[2], torch.float32), f"db of {rows} rows")

@@ -165,3 +165,89 @@ def test_small_entries_in_32_bits(exponent):
         within(dx, want[0], H.rounded(bounds[0] + small @ w64.abs(), want[0], torch.float32), f"dx of {rows} rows")
         within(dw, want[1], H.rounded(bounds[1] + small.t() @ big.double().abs(), want[1], torch.float32), f"dw of {rows} rows")
         within(db, want[2], H.rounded(bounds[2], want[2], torch.float32), f"db of {rows} rows")
+
+
+@types
+@pytest.mark.parametrize("rows, cols, more, more_exps, off", [(5, 33, 0, 0, 1), (130, 70, 3, 2, 5), (64, 96, 32, 5, 3), (300, 264, 1, 1, 7)])
+def test_8_bit_forms_of_any_strides(rows, cols, more, more_exps, off, dtype):
+    """8-bit forms whose rows, exponents and starts lie anywhere: all calls that write one give the bytes of an ordinary one
+    and leave the memory beside it, and all that read one give the same bits."""
+    rnd = gen(rows + cols)
+    new = lambda: Eight(rows, cols, dtype, cols + more, -(-cols // 32) + more_exps, off)  # noqa: E731
+    usual = lambda: G.Packed8(rows, cols, dtype, DEV)  # noqa: E731
+    x, w = rnd(rows, cols).to(dtype), (rnd(cols, cols) / math.sqrt(cols)).to(dtype)
+    gamma, beta = 1 + 0.1 * rnd(cols), 0.1 * rnd(cols)
+    y, rstd = torch.empty_like(x), torch.empty(rows, device=DEV)
+    p, forms = usual(), []
+
+    def odd(q):
+        """The Packed8 that holds an Eight's memory."""
+        o = usual()
+        o.q, o.exps = q.q, q.exps
+        return o
+
+    for call in (lambda q: G.gosh_pack8(x, q), lambda q: G.gosh_layer_norm(x, gamma, beta, y, rstd=rstd, xhat8=q),
+                 lambda q: G.gosh_layer_norm(x, gamma, beta, y, y8=q), lambda q: G.gosh_linear(x, w, y, act=H.GELU, z=q),
+                 lambda q: G.gosh_linear(x, w, y, act=H.GELU, y8=q)):
+        q = new()
+        call(p)
+        call(odd(q))
+        assert torch.equal(q.q, p.q[:, :cols]) and torch.equal(q.exps, p.exps)
+        again = new()
+        again.q.copy_(q.q), again.exps.copy_(q.exps)
+        q.beside()
+        forms.append(odd(again))
+    G.gosh_layer_norm(x, gamma, beta, y, rstd=rstd, xhat8=p)
+    xhat, z = forms[1], forms[3]
+    usual_z = usual()
+    G.gosh_linear(x, w, y, act=H.GELU, z=usual_z)
+    dy = (0.1 * rnd(rows, cols)).to(dtype)
+    got = []
+    for hat, pre in ((xhat, z), (p, usual_z)):
+        dx, dh, dw = torch.empty_like(x), torch.empty_like(x), torch.empty_like(w)
+        db, dg, dn = (torch.empty(cols, device=DEV) for _ in range(3))
+        G.gosh_linear_backward(dy, hat, w, pre, H.GELU, dx=dh, dw=dw, db=db)
+        G.gosh_layer_norm_backward(dh, hat, gamma, None, rstd, dx, dgamma=dg, dbeta=dn)
+        back = torch.empty_like(x)
+        G.gosh_unpack8(pre, back)
+        got.append((dx, dh, dw, db, dg, dn, back))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@types
+@pytest.mark.parametrize("into", H.TYPES, ids=lambda t: NAMES[t])
+def test_unpacking_into_another_type(into, dtype):
+    """What an 8-bit form stands for is rounded once, to the type that it is read into."""
+    rnd = gen(31)
+    x = (rnd(200, 75) * torch.exp2(torch.round(8 * rnd(200, 1)))).to(dtype)
+    x[7, 3], x[9, 70] = math.nan, 0.0
+    p = G.Packed8(200, 75, dtype, DEV)
+    G.gosh_pack8(x, p)
+    out = torch.empty(200, 75, dtype=into, device=DEV)
+    G.gosh_unpack8(p, out)
+    want = H.values(p.q[:, :75].cpu(), p.exps.cpu()).to(into)
+    assert torch.equal(torch.nan_to_num(out.cpu().double(), nan=0.123, posinf=1e300, neginf=-1e300),
+                       torch.nan_to_num(want.double(), nan=0.123, posinf=1e300, neginf=-1e300))
+
+
+def test_a_placed_matrix_as_operand():
+    """Matrices of gosh_matrix_place, which lie in several mappings, are operands as others are."""
+    n, d = 1 << 16, 128
+    M, _ = G.gosh_matrix_place(n, d, arena_bytes=6 << 30)
+    rnd = gen(2)
+    x = rnd(n, d)
+    M.copy_(x)
+    w, gamma, beta = rnd(48, d) / 10, 1 + 0.1 * rnd(d), 0.1 * rnd(d)
+    got = []
+    for m in (M, x):
+        y, p = torch.empty(n, 48, device=DEV), G.Packed8(n, d, torch.float32, DEV)
+        G.gosh_linear(m, w, y)
+        G.gosh_pack8(m, p)
+        dw = torch.empty_like(w)
+        G.gosh_linear_backward(y, m, None, None, dw=dw)
+        G.gosh_layer_norm(m, gamma, beta, m)
+        got.append((y, p.q, p.exps, dw, m.clone()))
+    torch.cuda.synchronize()
+    same = [torch.equal(a, b) for a, b in zip(*got)]
+    G.gosh_matrix_release(M)
+    assert all(same)

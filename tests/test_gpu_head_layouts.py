@@ -251,3 +251,35 @@ def test_a_placed_matrix_as_operand():
     same = [torch.equal(a, b) for a, b in zip(*got)]
     G.gosh_matrix_release(M)
     assert all(same)
+
+
+@pytest.mark.parametrize("dtype, k", [(torch.bfloat16, 8), (torch.float16, 3), (torch.float32, 1)], ids=["aligned", "not", "f32"])
+def test_more_rows_than_a_launch_takes(dtype, k):
+    """2^28 rows are the most that one launch has tiles for: what follows is the same layer on the rows from there."""
+    rows, n, edge = (1 << 28) + 777, 5, 1 << 28
+    at = torch.cat((torch.arange(50), torch.arange(edge - 50, edge + 50), torch.arange(rows - 50, rows))).to(DEV)
+    rnd = gen(k)
+    x, r, y = (torch.zeros(rows, c, dtype=dtype, device=DEV) for c in (k, n, n))
+    x[at], r[at] = rnd(at.numel(), k).to(dtype), rnd(at.numel(), n).to(dtype)
+    w, b = rnd(n, k).to(dtype), rnd(n)
+    z8, y8 = (G.Packed8(0, n, dtype, DEV) for _ in range(2))
+    for p in (z8, y8):
+        p.rows = rows
+        p.q, p.exps = torch.zeros(rows, n, dtype=torch.int8, device=DEV), torch.zeros(rows, 1, dtype=torch.uint8, device=DEV)
+    G.gosh_linear(x, w, y, bias=b, act=H.SILU, residual=r, z=z8, y8=y8)
+    few, one, two = torch.empty(at.numel(), n, dtype=dtype, device=DEV), G.Packed8(at.numel(), n, dtype), G.Packed8(at.numel(), n, dtype)
+    G.gosh_linear(x[at], w, few, bias=b, act=H.SILU, residual=r[at], z=one, y8=two)
+    assert torch.equal(y[at], few)
+    for p, q in ((z8, one), (y8, two)):
+        assert torch.equal(p.q[at], q.q[:, :n]) and torch.equal(p.exps[at], q.exps)
+    other = torch.ones(rows, dtype=torch.bool, device=DEV)
+    other[at] = False
+    plain = y[60]  # a row of zeros
+    assert bool(((y == plain).all(dim=1) | ~other).all())
+    del other, z8, y8
+    dx = torch.full((rows, k), 77.0, dtype=dtype, device=DEV)
+    G.gosh_linear_backward(r, None, w, None, H.NONE, dx=dx)
+    want = torch.empty(at.numel(), k, dtype=dtype, device=DEV)
+    G.gosh_linear_backward(r[at], None, w, None, H.NONE, dx=want)
+    assert torch.equal(dx[at], want)
+    assert bool((dx == 0).all(dim=1).sum() >= rows - at.numel())

@@ -152,7 +152,7 @@ int product_of_rows(ProductKind kind, ProductArgs g, int64_t rows, hipStream_t s
 }
 
 // How dw is split along the rows: enough workgroups for every CU's eight wavefronts, at least 256 rows each.  The parts
-// are summed by join_parts: 64 MB written and read for 65,536 x 512 -> 2048, 16 of its 143 + 18 us.
+// are summed by join_parts: 64 MB written and read for 65,536 x 512 -> 2048, 16 of its 145 + 17 us.
 struct DwPlan {
   TileSize size;
   int32_t tiles_m, tiles_n, splits;
@@ -189,10 +189,12 @@ int32_t plan_dx_splits(int64_t rows, int32_t in, int32_t out, int32_t type) {
 // ---- the activation's gradient ------------------------------------------------------------------
 
 // dz = dy * act'(z) and its sums over rows, bound by memory: 65,536 x 2048 in bf16 reads and writes 805 MB in 158 us,
-// 5.1 TB/s.  Taking the slope inside the products instead would take it again for every tile along the other side, 8
-// times there, about 0.5 ms of instructions.  dz is rounded to the activations' type: the matrix cores take 16 bits, and
-// so does memory.  A lane has 16 bytes of a row; `along` lanes lie along a row, the others of
-// the workgroup on rows of their own.  parts: gridDim.y x n sums.
+// 5.1 TB/s.  Taking the slope inside the products instead would take it again for every tile along the other side, 4
+// times there (2 in dx, 2 in dw), each some 0.1 ms of all SIMDs' time by the instructions counted here.  dz is rounded to
+// the activations' type: the matrix cores take 16 bits, and so does memory.  Of 16-bit types dx and dw end 1.4 times as
+// far from 64 bits for it (rms 0.0023 of the entries' for bf16, of which 0.0017 is the rounding of dx and dw themselves).
+// A lane has 16 bytes of a row; `along` lanes lie along a row, the others of the workgroup on rows of their own.  parts:
+// gridDim.y x n sums.
 template <typename T>
 struct SlopeChunk {
   static constexpr int E = T::kType == GOSH_F32 ? 4 : 8;

@@ -7,7 +7,7 @@
 // that they walk, then over the rows of a workgroup, and the workgroups' sums are joined in a fixed order by a second
 // kernel: no atomics, the same bits every time.
 //
-// Bound by memory.  300,007 x 501 in f32: 249 us, 4.8 TB/s; the gradient of 2^20 x 128 in bf16 with another branch's: 203
+// Bound by memory.  300,007 x 501 in f32: 252 us, 4.8 TB/s; the gradient of 2^20 x 128 in bf16 with another branch's: 203
 // us, 5.3 TB/s; 400,003 x 96 in f16 forward and back through 8-bit rows: 95 us, 4.1 TB/s (134 without loading a turn's
 // rows during the turn before).  Rows of 15 entries leave half of a wavefront's bytes unused: 1.9 M of them 128 us, 1.9
 // TB/s.

@@ -8,15 +8,17 @@
 //
 // Three ways, all ending in the same epilogue.  Aligned 16-bit rows go straight to LDS, in tiles of 256 x 256 by eight
 // wavefronts where there are enough: 65,536 x 512 x 2048 takes 137 to 150 us (0.9 to 1.0 PFLOP/s; a large product of the
-// vendor's library reaches 1.33), and with K = 512, where the epilogue counts, 262,144 x 512 -> 2048 652 us without and
-// 722 with GELU.  There each tile costs some 14 us of products and then, since the eight wavefronts go through it
-// together, 6 of epilogue, 9 with GELU; its stores alone need 4.9 at the rate of a fill.  One instruction in six less,
+// vendor's library reaches 1.33; the matrix cores are busy 48 % of it in dx, 55 % in dw), and with K = 512, where the
+// epilogue counts, 262,144 x 512 -> 2048 625 to 652 us without and 700 to 740 with GELU (38 %).  There, by the times for K
+// from 64 to 512, each tile costs 14 to 15 us of products and then, since the eight wavefronts go through it together, 4 to
+// 6 of epilogue, 7 to 9 with GELU; its stores alone need 4.9 at the rate of a fill.  One instruction in six less,
 // workgroups that start at different times, rows of 256 bytes and rows fetched from LDS ahead of the stores changed
 // nothing; tiles of 128 x 128, two workgroups to a CU, which do overlap both, lose more to fetching (914 us).  Other
 // tiles pass through registers on their way to LDS (32-bit entries, odd strides): 65,536 x 1024 -> 1024 in f32 takes
-// 746 us, 184 TFLOP/s (that library: 144 to 152); their instructions and products take turns on each SIMD (54 % of its
-// time are products).  A packed x of dw is widened in registers beside direct tiles of dz: 193 us for 131,072 x 512 and
-// 1024, against 143 unpacked, also where the widening lies between the products.
+// 735 us, 187 TFLOP/s (that library: 144 to 152), and the matrix cores are busy 68 % of it; 131,072 x 513 -> 1024 in bf16
+// takes 393 where 512 columns take 181.  A packed x of dw is widened in registers beside direct tiles of dz: 188 us for
+// 131,072 x 512 and 1024 (33 %), against 143 unpacked, also where the widening lies between the products; that kernel
+// spills 159 registers, none of them in the loop over k, but where it goes from one tile to the next.
 //
 // 32-bit entries are taken apart into three bf16 parts, x = h + m + l, each the nearest to what the ones before leave
 // (|m| <= 2^-9 |x|, |l| <= 2^-18 |x|, nothing is left from |x| = 2^-110 on; of smaller ones up to 2^-134, half of the least
@@ -32,7 +34,8 @@
 namespace gosh {
 
 // kPast: kForward of y alone, in tiles of kLarge, past the caches.  (A kernel of its own: as a branch at each store it
-// cost the other calls 2 to 20 %, in registers.)
+// cost the other calls 2 to 20 %, in registers.  kForward, with every optional output, has 112 scalar registers in lanes of
+// vector ones there, kPast 18: 131,072 x 512 -> 1024 with SiLU takes 180 us, 214 with z and 226 with a packed z.)
 enum ProductOut : int { kForward, kStore, kParts, kPast };
 constexpr bool is_forward(ProductOut out) { return out == kForward || out == kPast; }
 

@@ -13,7 +13,8 @@ neighbours may go to either there: what is summed from such values is returned i
 
 Moments in 8 bits: 128 entries of a tensor share a power of two, the smallest at which the largest is at most 1.875; the
 first moment has a sign, 4 bits of exponent and 3 of mantissa, the second 5 and 3.  They are rounded up where the bits that
-are cut off and a number from a sequence in the entry's index and the step's number carry, so that the mean over the steps is right.
+are cut off and a number from a sequence in the entry's index and the step's number carry, so that the mean over the steps is
+right; a second moment that is not 0 does not become 0.
 
 GELU is the form with tanh.  Rows are vertices or vertex pairs.
 """
@@ -216,13 +217,16 @@ def _moment8(x, exponent_bits, step):
     bits = (b.abs() / _two(power, b) * down).view(torch.int32)
     if step is not None:
         bits = bits + step.reshape(-1, BLOCK)
-    kept = (bits >> 20 << 20).view(torch.float32) / down * _two(power, b)
+    bits = bits >> 20 << 20
+    if exponent_bits == 5:  # what is more than nothing stays so
+        bits = torch.where((b > 0) & (bits == 0), torch.full_like(bits, 1 << 20), bits)
+    kept = bits.view(torch.float32) / down * _two(power, b)
     return (torch.sign(b) * kept).reshape(-1)
 
 
 def _sequence(index, number, other):
-    """20 bits for each index: the fractional parts of multiples of the golden ratio's and another number."""
-    h = (index * 2654435769 + number * 2246822519) & 0xFFFFFFFF
+    """20 bits for each index: the fractional parts of multiples of the golden ratio and of the root of 2."""
+    h = (index * 2654435769 + number * 1779033703) & 0xFFFFFFFF
     return (((~h if other else h) & 0xFFFFFFFF) >> 12).to(torch.int32)
 
 

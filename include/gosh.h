@@ -602,6 +602,122 @@ int gosh_linear_backward(const gosh_mat *dy, const gosh_mat *x, const gosh_mat *
                          void *hip_stream);
 uint64_t gosh_linear_backward_workspace(int64_t rows, int32_t in, int32_t out, int32_t type, int32_t act);
 
+/* ---- the head in 8-bit floating point ------------------------------------------------------- */
+/* Linear layers whose operands are kept in 8 bits: twice the rate of 16 bits on the matrix cores, half of their bytes.  As
+ * above: asynchronous, nothing allocated, the same bits for the same arguments.  Results of GOSH_F32 are sums in 32 bits of
+ * exact products.  Those of 16-bit types are summed in 32 bits too, but of eight products along the sum at a time, of which
+ * the matrix cores cut off what is below 2^-13 of the largest: together less than 2^-10 of the magnitudes that are summed,
+ * typically 2^-16. */
+
+/* Borrowed view of a rows x cols device matrix in 8-bit floating point.  data holds e4m3 entries q (a sign, 4 bits of
+ * exponent, 3 of mantissa; largest 448, 0x7f and 0xff NaN), entry (r, c) at data[r * ld + c], and stands for
+ * q * 2^(exps[r / block_rows * ld_exps + c / 128] - 127).  block_rows: 1 (128 columns of a row share a power of two) or
+ * 128 (a square of 128 x 128; the last ones may be smaller).
+ * 0 <= rows < 2^31 - 1, 0 <= cols <= GOSH_FP8_MAX_LD; data 16-byte aligned, exps 4-byte aligned, both may be NULL without
+ * entries; ld a multiple of 128, cols <= ld <= GOSH_FP8_MAX_LD; ld_exps a multiple of 4, at least ceil(cols / 128), at most
+ * GOSH_FP8_MAX_LD.  The bytes from cols to the next multiple of 128 of each row are zero: gosh_pack_fp8 writes them, and the
+ * products take them for entries.  Exponent bytes are 1 to 254.
+ * gosh_pack_fp8 takes the smallest power of two, at least 2^-126, at which the block's largest finite magnitude is at most
+ * 448, and rounds once, to the nearest, ties to even: half of 2^-3 of an entry's magnitude at most down to 2^-6 of the unit,
+ * 2^-10 of the unit below.  An entry that is not finite becomes NaN. */
+#define GOSH_FP8_MAX_LD 8388608
+typedef struct {
+  void *data;
+  uint8_t *exps;
+  int64_t rows, cols, ld, ld_exps;
+  int32_t block_rows;
+} gosh_fp8;
+
+/* x (not packed) to 8-bit floating point: as it is into q, transposed into qt (cols x rows; its blocks are 128 rows of a
+ * column of x, or the squares of q), or both; one of them may be NULL.  With both, block_rows has to be the same. */
+int gosh_pack_fp8(const gosh_mat *x, const gosh_fp8 *q, const gosh_fp8 *qt, void *hip_stream);
+/* q back to x, a matrix of any type that is not packed; rounded once. */
+int gosh_unpack_fp8(const gosh_fp8 *q, const gosh_mat *x, void *hip_stream);
+
+/* Linear layer: z = x8 w^T + bias, y = act(z) + residual.  x: rows x in, of any type, is put into x8 first (block_rows 1),
+ * as by gosh_pack_fp8; or NULL, and x8 holds it.  w: out x in, of either block_rows, out <= GOSH_MAT_MAX_COLS.  bias, act,
+ * residual, y and z (which may be packed) as for gosh_linear, of one type.  y must not overlap x, x8 or w. */
+int gosh_linear_fp8(const gosh_mat *x, const gosh_fp8 *x8, const gosh_fp8 *w, const float *bias, int32_t act,
+                    const gosh_mat *residual, const gosh_mat *y, const gosh_mat *z, void *hip_stream);
+
+/* Its gradient: dz = dy * act'(z), dx = dz8 w, dw = dz8^T x8, db = sum over rows dz.  dz is formed in 32 bits and put into 8
+ * twice, in blocks of 128 columns for dx and of 128 rows for dw; db sums it as it is.  dy: rows x out; z: as dy, or packed;
+ * NULL with GOSH_ACT_NONE.  xt: in x rows, x transposed, block_rows 1 (gosh_pack_fp8's qt); may be NULL if dw is.  wt: in x
+ * out, w transposed, of either block_rows; may be NULL if dx is.  dx: rows x in, of dy's type; dw: out x in, of dy's type or
+ * GOSH_F32; db: out floats.  dx or dw may be NULL, db too (db alone: gosh_linear_backward).  in, out <= GOSH_MAT_MAX_COLS;
+ * with dw rows <= GOSH_FP8_MAX_LD.  With rows = 0 dw and db are zero.  dx must not overlap dy, z or wt.
+ * workspace: as above, at least gosh_linear_fp8_backward_workspace bytes (0 for sizes that the call refuses). */
+int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_fp8 *wt, const gosh_mat *z, int32_t act,
+                             const gosh_mat *dx, const gosh_mat *dw, float *db, void *workspace, uint64_t workspace_bytes,
+                             void *hip_stream);
+uint64_t gosh_linear_fp8_backward_workspace(int64_t rows, int32_t in, int32_t out);
+
+/* ---- losses and steps of a head ---------------------------------------------------------------- */
+
+/* Softmax cross-entropy of each row of logits, rows x classes, of any type (not packed), against one class:
+ *   loss = weight * (log(sum exp x) - x[target]),  dlogits = scale * weight * (softmax(x) - [class = target]).
+ * targets: rows int32, or int64 with targets_are64 = 1.  A negative target is none: loss and gradient of the row are 0, as
+ * they are for a row of weight 0 and for one all of whose logits are -infinity (which takes a class out).  A target of `classes` or more makes
+ * both NaN, and so does a logit that is NaN or +infinity.  weight: rows floats, or NULL for 1.  loss: rows floats.
+ * dlogits: as logits, may be logits; NULL: the loss alone.  One reading of the logits; 32 bits within. */
+int gosh_softmax_loss(const gosh_mat *logits, const void *targets, int32_t targets_are64, const float *weight, float scale,
+                      float *loss, const gosh_mat *dlogits, void *hip_stream);
+
+/* AdamW.  A parameter tensor of an optimiser: n entries p with their gradients g; state: gosh_adamw_state_bytes(n, bits)
+ * bytes, 16-byte aligned, zero (as bytes) before the first step; copy: n entries of copy_type that receive the new
+ * parameters rounded, or NULL.  Pointers need the alignment of their entries.  Flat arrays: tensors of any shape whose
+ * memory has no gaps. */
+typedef struct {
+  float *p;
+  const void *g;
+  void *state;
+  void *copy;
+  int64_t n;           /* 0 <= n <= 2^40 */
+  int32_t g_type;      /* gosh_type */
+  int32_t copy_type;   /* GOSH_BF16 or GOSH_F16; ignored without copy */
+  int32_t bits;        /* of a moment's entry: 8 or 32 */
+  float weight_decay;  /* >= 0 */
+} gosh_param;
+/* bits = 32: n floats m and, from the next multiple of 16 bytes on, n floats v.  bits = 8, each from the next multiple of 16
+ * bytes on: n bytes m, n bytes v, ceil(n / 128) exponent bytes of m, and of v.  128 entries of a tensor share an exponent.
+ * m: a sign, 4 bits of exponent, 3 of mantissa, bias 15 (without infinities and NaN; exponent 0 has no leading one); v: 5
+ * and 3 bits, bias 31; an entry stands for that number times 2^(byte - 127), or NaN where the byte is 255.  The exponent is
+ * the smallest from 2^-95 on at which the block's largest magnitude is at most 1.875.  A block with an entry that is not
+ * finite, or beyond 1.875 * 2^126, becomes NaN. */
+uint64_t gosh_adamw_state_bytes(int64_t n, int32_t bits);
+
+/* An optimiser over `count` tensors (host array, read by the call): checks them and puts their addresses into device memory
+ * of the current device (waits for the device).  The arrays stay the caller's and must live, where they are, as long as the
+ * optimiser is used.  GOSH_EINVAL also where anything that a step writes overlaps another tensor's arrays. */
+int gosh_adamw_create(const gosh_param *params, int32_t count, void **optimiser_out);
+void gosh_adamw_free(void *optimiser); /* waits for the device's work */
+
+/* One step, of all tensors in one launch: with g' = scale * g
+ *   m = beta1 m + (1 - beta1) g',  v = beta2 v + ((1 - beta2) g') g',
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * from the moments as they are before they are put back into 8 bits.  t: step, from 1 on; or, where steps is not NULL (device memory),
+ * *steps + 1, which the call leaves there.  lr_dev, scale: device floats in place of lr and of 1, or NULL.  Where *scale is
+ * not finite nothing changes, *steps neither: a step with gradients that overflowed is left out.
+ * 0 <= beta1, beta2 < 1, eps >= 0.
+ * Moments in 8 bits: the bits of a float below the third of its mantissa are cut off, after the addition of 20 bits
+ * (i * 2654435769 + t * 1779033703 mod 2^32) / 2^12 (of the complement for v), i the entry's index: so that, over the steps,
+ * the mean is right, and a v that shrinks by a thousandth of itself a step does not stay where it is.  A v over 0 does not
+ * become 0, by which an update could grow without bound: it takes the smallest number of its block. */
+typedef struct {
+  double lr, beta1, beta2, eps;
+  int64_t step;
+  const float *lr_dev, *scale;
+  int64_t *steps;
+} gosh_adamw_options;
+int gosh_adamw_step(void *optimiser, const gosh_adamw_options *options, void *hip_stream);
+
+/* The moments of all tensors as values, to m and v, or from them (in 8 bits rounded to the nearest, v as above): flat arrays of `type`
+ * (GOSH_F32; to: GOSH_BF16 too, which holds what 8 bits stand for exactly) in which a tensor begins at the sum of the sizes before it, each
+ * rounded up to a multiple of 128; save writes zeros between.  `entries`: of m and of v each, gosh_adamw_entries or more. */
+int64_t gosh_adamw_entries(const void *optimiser);
+int gosh_adamw_save(void *optimiser, void *m, void *v, int64_t entries, int32_t type, void *hip_stream);
+int gosh_adamw_load(void *optimiser, const float *m, const float *v, int64_t entries, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,6 +27,7 @@ GOSH_F32, GOSH_BF16, GOSH_F16 = 0, 1, 2
 GOSH_ACT_NONE, GOSH_ACT_RELU, GOSH_ACT_GELU, GOSH_ACT_SILU = 0, 1, 2, 3
 GOSH_MAT_MAX_COLS = 65536
 GOSH_MAT_MAX_LD = 1048576
+GOSH_FP8_MAX_LD = 8388608
 GOSH_MAX_NEG = 15
 GOSH_STATIC_MAX_N = 1 << 26
 
@@ -77,7 +78,23 @@ class gosh_mat(C.Structure):
                 ("ld_exps", C.c_int64), ("cols", C.c_int32), ("type", C.c_int32), ("packed", C.c_int32)]
 
 
+class gosh_fp8(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("exps", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64),
+                ("ld_exps", C.c_int64), ("block_rows", C.c_int32)]
+
+
+class gosh_param(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("state", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64),
+                ("g_type", C.c_int32), ("copy_type", C.c_int32), ("bits", C.c_int32), ("weight_decay", C.c_float)]
+
+
+class gosh_adamw_options(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64),
+                ("lr_dev", C.c_void_p), ("scale", C.c_void_p), ("steps", C.c_void_p)]
+
+
 _MAT = C.POINTER(gosh_mat)
+_FP8 = C.POINTER(gosh_fp8)
 EXPORTS = {
     "gosh_last_error": (C.c_char_p, []),
     "gosh_tuning_defaults": (None, [C.POINTER(gosh_tuning)]),
@@ -152,6 +169,20 @@ EXPORTS = {
     "gosh_linear_backward": (C.c_int, [_MAT, _MAT, _MAT, _MAT, C.c_int32, _MAT, _MAT, C.c_void_p,
                                        C.c_void_p, C.c_uint64, C.c_void_p]),
     "gosh_linear_backward_workspace": (C.c_uint64, [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
+    "gosh_pack_fp8": (C.c_int, [_MAT, _FP8, _FP8, C.c_void_p]),
+    "gosh_unpack_fp8": (C.c_int, [_FP8, _MAT, C.c_void_p]),
+    "gosh_linear_fp8": (C.c_int, [_MAT, _FP8, _FP8, C.c_void_p, C.c_int32, _MAT, _MAT, _MAT, C.c_void_p]),
+    "gosh_linear_fp8_backward": (C.c_int, [_MAT, _FP8, _FP8, _MAT, C.c_int32, _MAT, _MAT, C.c_void_p, C.c_void_p,
+                                           C.c_uint64, C.c_void_p]),
+    "gosh_linear_fp8_backward_workspace": (C.c_uint64, [C.c_int64, C.c_int32, C.c_int32]),
+    "gosh_softmax_loss": (C.c_int, [_MAT, C.c_void_p, C.c_int32, C.c_void_p, C.c_float, C.c_void_p, _MAT, C.c_void_p]),
+    "gosh_adamw_state_bytes": (C.c_uint64, [C.c_int64, C.c_int32]),
+    "gosh_adamw_create": (C.c_int, [C.POINTER(gosh_param), C.c_int32, C.POINTER(C.c_void_p)]),
+    "gosh_adamw_free": (None, [C.c_void_p]),
+    "gosh_adamw_step": (C.c_int, [C.c_void_p, C.POINTER(gosh_adamw_options), C.c_void_p]),
+    "gosh_adamw_entries": (C.c_int64, [C.c_void_p]),
+    "gosh_adamw_save": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p]),
+    "gosh_adamw_load": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
 }
 
 _lib = None
@@ -730,3 +761,210 @@ def gosh_linear_backward(dy: torch.Tensor, x, w, z, act: int = GOSH_ACT_NONE, dx
     _check(lib().gosh_linear_backward(v, _mat(x, "x"), _mat(w, "w"), _mat(z, "z"), act, _mat(dx, "dx"), _mat(dw, "dw"),
                                       _floats(db, "db", v.cols), workspace.data_ptr() or None, workspace.numel(),
                                       _stream(stream)))
+
+
+# ---- the head in 8-bit floating point --------------------------------------------------------
+
+
+class PackedFp8:
+    """A rows x cols matrix in 8-bit floating point: e4m3 entries `q` (rows padded to 128, which the library's calls write as
+    zeros) and exponent bytes `exps`, one for each 128 columns of a row or, with block_rows = 128, of 128 rows.  Zeros at
+    first; gosh_pack_fp8 and gosh_linear_fp8 write it.  q and exps may be replaced, by tensors whose rows are contiguous and
+    at least as long: a call takes those of that moment."""
+
+    def __init__(self, rows: int, cols: int, block_rows: int = 1, device="cuda"):
+        if block_rows not in (1, 128):
+            raise ValueError("block_rows must be 1 or 128")
+        self.rows, self.cols, self.block_rows = rows, cols, block_rows
+        self.q = torch.zeros(rows, -(-cols // 128) * 128, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+        self.exps = torch.zeros(-(-rows // block_rows), -(-cols // 512) * 4, dtype=torch.uint8, device=device)
+
+    def __getstate__(self):  # as bytes: torch does not pickle tensors of this type
+        return {**self.__dict__, "q": self.q.view(torch.uint8)}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state, q=state["q"].view(torch.float8_e4m3fn))
+
+    def _fp8(self, name: str) -> gosh_fp8:
+        q, exps, rows, cols = self.q, self.exps, self.rows, self.cols
+        if q.dtype != torch.float8_e4m3fn or exps.dtype != torch.uint8:
+            raise TypeError(f"{name}: q must be float8_e4m3fn and exps uint8")
+        blocks, wide, long = -(-rows // self.block_rows), -(-cols // 128) * 128, -(-cols // 512) * 4
+        ld, ld_exps = _rows_apart(q, rows, wide), _rows_apart(exps, blocks, long)
+        if ld is None or ld_exps is None:
+            raise TypeError(f"{name}: q must have {rows} rows of at least {wide} contiguous entries, exps {blocks} of {long}")
+        if not rows or not cols:
+            return gosh_fp8(None, None, rows, cols, wide, max(long, 4), self.block_rows)
+        return gosh_fp8(q.data_ptr(), exps.data_ptr(), rows, cols, wide if rows == 1 else ld, long if blocks == 1 else ld_exps,
+                        self.block_rows)
+
+
+def _fp8(m, name: str):
+    if m is None:
+        return None
+    if not isinstance(m, PackedFp8):
+        raise TypeError(f"{name} must be a PackedFp8")
+    return m._fp8(name)
+
+
+def gosh_pack_fp8(x: torch.Tensor, q: PackedFp8 = None, qt: PackedFp8 = None, stream=None) -> None:
+    """x in 8-bit floating point: as it is into q, transposed into qt."""
+    _check(lib().gosh_pack_fp8(_mat(x, "x"), _fp8(q, "q"), _fp8(qt, "qt"), _stream(stream)))
+
+
+def gosh_unpack_fp8(q: PackedFp8, x: torch.Tensor, stream=None) -> None:
+    _check(lib().gosh_unpack_fp8(_fp8(q, "q"), _mat(x, "x"), _stream(stream)))
+
+
+def gosh_linear_fp8(x, x8: PackedFp8, w: PackedFp8, y: torch.Tensor, bias=None, act: int = GOSH_ACT_NONE, residual=None, z=None,
+                    stream=None) -> None:
+    """y = act(x8 w^T + bias) + residual, after x was put into x8; x None: x8 holds it.  z: a tensor or a Packed8 that
+    receives x8 w^T + bias."""
+    v = _fp8(w, "w")
+    _check(lib().gosh_linear_fp8(_mat(x, "x"), _fp8(x8, "x8"), v, _floats(bias, "bias", v.rows), act, _mat(residual, "residual"),
+                                 _mat(y, "y"), _mat(z, "z"), _stream(stream)))
+
+
+def gosh_linear_fp8_backward_workspace(rows: int, in_: int, out: int) -> int:
+    return int(lib().gosh_linear_fp8_backward_workspace(rows, in_, out))
+
+
+def gosh_linear_fp8_backward(dy: torch.Tensor, xt, wt, z, act: int = GOSH_ACT_NONE, dx=None, dw=None, db=None, workspace=None,
+                             stream=None) -> None:
+    """dx, dw and db (those that are given, dx or dw among them) of gosh_linear_fp8, from x and w transposed in 8 bits."""
+    v = _mat(dy, "dy")
+    into = dx if dx is not None else dw
+    nbytes = 0 if into is None else gosh_linear_fp8_backward_workspace(v.rows, into.shape[1], v.cols)
+    workspace = _workspace(workspace, nbytes, stream, dy.device)
+    _check(lib().gosh_linear_fp8_backward(v, _fp8(xt, "xt"), _fp8(wt, "wt"), _mat(z, "z"), act, _mat(dx, "dx"), _mat(dw, "dw"),
+                                          _floats(db, "db", v.cols), workspace.data_ptr() or None, workspace.numel(),
+                                          _stream(stream)))
+
+
+# ---- losses and steps of a head ----------------------------------------------------------------
+
+
+def gosh_softmax_loss(logits: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, dlogits=None, weight=None,
+                      scale: float = 1.0, stream=None) -> None:
+    """loss of each row against its class in targets (int32 or int64, negative: none), and scale * its gradient."""
+    v = _mat(logits, "logits")
+    if targets.dtype not in (torch.int32, torch.int64) or targets.numel() != v.rows or not targets.is_contiguous():
+        raise TypeError(f"targets must be a contiguous int32 or int64 tensor of {v.rows} entries")
+    _check(lib().gosh_softmax_loss(v, targets.data_ptr() or None, targets.dtype == torch.int64, _floats(weight, "weight", v.rows),
+                                   scale, _floats(loss, "loss", v.rows), _mat(dlogits, "dlogits"), _stream(stream)))
+
+
+class AdamW:
+    """An optimiser of gosh_adamw_create.  Holds the tensors that it was made with (their memory must not be replaced), and
+    `states`, the uint8 tensors of its moments."""
+
+    def __init__(self, handle, tensors, states):
+        self.handle, self._tensors, self.states = handle, tensors, states
+
+    def free(self) -> None:
+        if self.handle:
+            lib().gosh_adamw_free(self.handle)
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.free()
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """No two entries at one place and no gaps between them."""
+    at = 1
+    for n, s in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n != 1), key=lambda v: v[1]):
+        if s != at:
+            return False
+        at *= n
+    return True
+
+
+def gosh_adamw_state_bytes(n: int, bits: int) -> int:
+    return int(lib().gosh_adamw_state_bytes(n, bits))
+
+
+def gosh_adamw_create(params, grads, bits=8, states=None, copies=None, weight_decay=0.0) -> AdamW:
+    """params: float32 tensors; grads: theirs, of any type of the head.  bits (8 or 32) and weight_decay: of all, or a list.
+    states: uint8 tensors of gosh_adamw_state_bytes, or None for new ones, zero.  copies: None, or a list of bfloat16 or float16
+    tensors (or None) that receive the parameters rounded."""
+    params, grads = list(params), list(grads)
+    count = len(params)
+    each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * count  # noqa: E731
+    bits, decay, copies = each(bits), each(weight_decay), each(copies)
+    if states is None:
+        states = [torch.zeros(gosh_adamw_state_bytes(p.numel(), b), dtype=torch.uint8, device=p.device) for p, b in zip(params, bits)]
+    states = list(states)
+    if not count == len(grads) == len(states) == len(copies) == len(bits) == len(decay):
+        raise ValueError("params, grads, states, copies, bits and weight_decay must be as many")
+    array = (gosh_param * max(count, 1))()
+    for i, (p, g, s, c) in enumerate(zip(params, grads, states, copies)):
+        if p.dtype != torch.float32 or g.dtype not in _TYPES or (c is not None and c.dtype not in (torch.bfloat16, torch.float16)):
+            raise TypeError(f"tensor {i}: float32 parameters, float32, bfloat16 or float16 gradients, 16-bit copies")
+        for t in (g, c):
+            if t is not None and (t.shape != p.shape or any(a != b for n, a, b in zip(p.shape, p.stride(), t.stride()) if n != 1)):
+                raise TypeError(f"tensor {i}: parameters, gradients and copies must have one shape and the same strides")
+        if not _dense(p):
+            raise TypeError(f"tensor {i}: parameters must lie in memory without gaps")
+        if s.dtype != torch.uint8 or not s.is_contiguous() or s.numel() < gosh_adamw_state_bytes(p.numel(), bits[i]):
+            raise TypeError(f"tensor {i}: a state is a contiguous uint8 tensor of gosh_adamw_state_bytes entries")
+        array[i] = gosh_param(p.data_ptr() or None, g.data_ptr() or None, s.data_ptr() or None, None if c is None else c.data_ptr() or None,
+                              p.numel(), _TYPES[g.dtype], GOSH_BF16 if c is None else _TYPES[c.dtype], bits[i], decay[i])
+    handle = C.c_void_p()
+    _check(lib().gosh_adamw_create(array, count, C.byref(handle)))
+    return AdamW(handle.value, (params, grads, copies), states)
+
+
+def gosh_adamw_free(opt: AdamW) -> None:
+    opt.free()
+
+
+def _device_scalar(t, name: str, dtype):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != 1:
+        raise TypeError(f"{name} must be a {dtype} tensor of one entry")
+    return t.data_ptr()
+
+
+def gosh_adamw_step(opt: AdamW, lr: float = 0.0, step: int = 1, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                    lr_dev=None, scale=None, steps=None, stream=None) -> None:
+    """A step of all tensors, the step-th from 1 on.  Device tensors of one entry: lr_dev in place of lr, scale that gradients are
+    multiplied by (the step is left out where it is not finite), steps (int64) in place of `step`: how many were taken."""
+    options = gosh_adamw_options(lr, beta1, beta2, eps, step, _device_scalar(lr_dev, "lr_dev", torch.float32),
+                                 _device_scalar(scale, "scale", torch.float32), _device_scalar(steps, "steps", torch.int64))
+    _check(lib().gosh_adamw_step(opt.handle, options, _stream(stream)))
+
+
+def gosh_adamw_entries(opt: AdamW) -> int:
+    """Entries of the flat arrays of gosh_adamw_save and gosh_adamw_load."""
+    return int(lib().gosh_adamw_entries(opt.handle))
+
+
+def _moments(m: torch.Tensor, v: torch.Tensor):
+    if m.dtype != v.dtype or m.numel() != v.numel() or not m.is_contiguous() or not v.is_contiguous() or m.dtype not in _TYPES:
+        raise TypeError("m and v must be contiguous tensors of one type and size")
+    return m.data_ptr() or None, v.data_ptr() or None
+
+
+def gosh_adamw_save(opt: AdamW, m: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+    """The moments of all tensors, each from a multiple of 128 on, as float32 or bfloat16 values."""
+    pm, pv = _moments(m, v)
+    _check(lib().gosh_adamw_save(opt.handle, pm, pv, m.numel(), _TYPES[m.dtype], _stream(stream)))
+
+
+def gosh_adamw_load(opt: AdamW, m: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+    """The same back, from float32."""
+    pm, pv = _moments(m, v)
+    if m.dtype != torch.float32:
+        raise TypeError("moments are loaded from float32")
+    _check(lib().gosh_adamw_load(opt.handle, pm, pv, m.numel(), _stream(stream)))

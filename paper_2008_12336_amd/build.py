@@ -14,7 +14,8 @@ EXAMPLE = os.path.join(HERE, "examples", "embed_example")
 
 SOURCES = ["gosh_host.cpp", "gosh_coarsen.cpp", "gosh_sampler.cpp", "gosh_coarsen_gpu.hip", "gosh_quotient.hip", "gosh_quotient_radix32.hip", "gosh_quotient_radix64.hip", "gosh_device_pool.cpp", "gosh_train.hip", "gosh_embed.hip", "gosh_parts.hip", "gosh_place.hip",
            "gosh_head.hip", "gosh_norm.hip", "gosh_linear.hip", "gosh_product_f32.hip", "gosh_product_bf16.hip",
-           "gosh_product_f16.hip"]
+           "gosh_product_f16.hip", "gosh_fp8.hip", "gosh_fp8_f32.hip", "gosh_fp8_bf16.hip", "gosh_fp8_f16.hip", "gosh_loss.hip",
+           "gosh_adamw.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950",

@@ -1,0 +1,109 @@
+// Shared by the units of the head in 8-bit floating point: views and checks of its matrices, their format, and the matrix
+// product's arguments.
+//
+// An entry is q * 2^(byte - 127), q in e4m3, and 128 entries along the sum of a product share the byte: the matrix cores
+// take such a power of two per operand and 32 entries, so that 128 of them cost no instruction of their own and sums stay
+// in the accumulators from the first block to the last.  (A scale that is no power of two would have to multiply the
+// accumulators of every block: 16 vector instructions for each two of the matrix cores.)
+#pragma once
+
+#include "gosh_product.h"
+
+namespace gosh {
+
+constexpr int kFp8Block = 128;
+
+int check_fp8(const gosh_fp8 *m, const char *what, int use = 0);
+
+// An operand of a product, k along its rows.  shift: 0, or 7 where 128 rows share their exponents.
+struct Fp8Plane {
+  const uint8_t *data, *exps;
+  int64_t ld, ld_exps;
+  int32_t shift;
+};
+inline Fp8Plane fp8_plane(const gosh_fp8 *m) {
+  return {static_cast<const uint8_t *>(m->data), m->exps, m->ld, m->ld_exps, m->block_rows == 1 ? 0 : 7};
+}
+
+struct Fp8Args {
+  Fp8Plane x, w;   // A (M rows), B (N rows)
+  ProductArgs g;   // M, N, tiles, splits and where the results go; K and k_per_split count blocks
+};
+
+// Defined in gosh_fp8_{f32,bf16,f16}.hip, by the type of the results; kParts: F32 for sums that stay in 32 bits, Bf16 for
+// those that are rounded to 16.
+template <typename T>
+int launch_fp8(ProductOut out, const Fp8Args &args, hipStream_t st);
+template <>
+int launch_fp8<F32>(ProductOut, const Fp8Args &, hipStream_t);
+template <>
+int launch_fp8<Bf16>(ProductOut, const Fp8Args &, hipStream_t);
+template <>
+int launch_fp8<F16>(ProductOut, const Fp8Args &, hipStream_t);
+
+// ---- device -------------------------------------------------------------------------------------
+
+// The exponent byte of a block whose largest finite magnitude, f * 2^E with f in [1, 2), has the bits `most`: 448 is 1.75 *
+// 2^8, so e is E - 8, or E - 7 from f > 1.75 on, which the carry decides.
+__device__ __forceinline__ uint32_t fp8_byte(uint32_t most) {
+  const uint32_t e = (most + 0x1fffffu) >> 23;
+  return e < 9 ? 1 : e - 8;
+}
+
+// The magnitude's bits, of what is finite.
+__device__ __forceinline__ uint32_t finite_bits(float v) {
+  const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
+  return b < 0x7f800000u ? b : 0u;
+}
+
+// Four entries' e4m3 as a word, from entries in 32 bits that are at most 448 units or not finite.
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d, float inverse) {
+  const auto in = [&](float v) {
+    const float x = v * inverse;  // exact, or below what rounds to zero
+    return __builtin_fabsf(x) < INFINITY ? x : __uint_as_float(0x7fc00000u);
+  };
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(in(a), in(b), 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(in(c), in(d), w, true);
+  return static_cast<uint32_t>(w);
+}
+
+typedef int I8 __attribute__((ext_vector_type(8)));
+
+// 16 bytes of a lane's row, or 8 of them.
+__device__ __forceinline__ I8 both_halves(U4 lo, U4 hi) {
+  return I8{static_cast<int>(lo[0]), static_cast<int>(lo[1]), static_cast<int>(lo[2]), static_cast<int>(lo[3]),
+            static_cast<int>(hi[0]), static_cast<int>(hi[1]), static_cast<int>(hi[2]), static_cast<int>(hi[3])};
+}
+__device__ __forceinline__ S8 widened(uint32_t lo, uint32_t hi, float unit) {
+  typedef __bf16 Two __attribute__((ext_vector_type(2)));
+  typedef __bf16 Eight __attribute__((ext_vector_type(8)));
+  const Two a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, unit, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, unit, true);
+  const Two c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, unit, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, unit, true);
+  return __builtin_bit_cast(S8, Eight{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]});
+}
+
+// 64 k of 32 x 32 products, 32 bytes of each lane's row; any order of k is right that both sides share.
+//
+// Exact: through bf16, which holds a number of 4 bits times a power of two as it is, and whose products the matrix cores sum
+// in 32 bits.  Otherwise in 8 bits, at twice the rate: there the cores align eight products (of neighbouring k) to the largest of them
+// and cut off what is below 2^-13 of its power of two, so that a sum ends up to 7 * 2^-13 of its largest products off, by measurement
+// 1.3e-5 of its rms for normal entries and 8e-5 for entries that differ by e^1.5 (32-bit sums: 1e-7).  That is a
+// thousandth of what the entries' own rounding to 4 bits does, and below half a step of 16-bit results: those take 8 bits,
+// 32-bit results bf16.
+template <bool Exact>
+__device__ __forceinline__ F16x fp8_mma(const U4 (&a)[2], const U4 (&b)[2], uint32_t byte_a, uint32_t byte_b, F16x c) {
+  if constexpr (Exact) {
+    const float ua = read_unit(byte_a), ub = read_unit(byte_b);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2)
+        c = Cores<Bf16>::mma(widened(a[h][i], a[h][i + 1], ua), widened(b[h][i], b[h][i + 1], ub), c);
+    return c;
+  } else {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(both_halves(a[0], a[1]), both_halves(b[0], b[1]), c, 0, 0, 0,
+                                                           static_cast<int>(byte_a), 0, static_cast<int>(byte_b));
+  }
+}
+
+}  // namespace gosh

@@ -1,0 +1,462 @@
+// The head in 8-bit floating point: gosh_pack_fp8, gosh_unpack_fp8, gosh_linear_fp8 and its gradient.
+#include "gosh_fp8.h"
+
+#include <algorithm>
+
+namespace gosh {
+
+int check_fp8(const gosh_fp8 *m, const char *what, int use) {
+  if (m == nullptr) return (use & kOptional) ? GOSH_OK : fail(GOSH_EINVAL, "%s is null", what);
+  if (m->block_rows != 1 && m->block_rows != kFp8Block)
+    return fail(GOSH_EINVAL, "%s: block_rows = %d: must be 1 or 128", what, m->block_rows);
+  if (!rows_fit(m->rows)) return fail(GOSH_EINVAL, "%s: rows = %lld: must be in [0, 2^31-1)", what, (long long)m->rows);
+  if (m->cols < 0 || m->cols > GOSH_FP8_MAX_LD)
+    return fail(GOSH_EINVAL, "%s: cols = %lld: must be in [0, %d]", what, (long long)m->cols, GOSH_FP8_MAX_LD);
+  if (m->ld < m->cols || m->ld > GOSH_FP8_MAX_LD || m->ld % kFp8Block != 0)
+    return fail(GOSH_EINVAL, "%s: ld = %lld: must be a multiple of 128 in [cols, %d]", what, (long long)m->ld, GOSH_FP8_MAX_LD);
+  const int64_t groups = ceil_div(m->cols, kFp8Block);
+  if (m->ld_exps < groups || m->ld_exps > GOSH_FP8_MAX_LD || m->ld_exps % 4 != 0)
+    return fail(GOSH_EINVAL, "%s: ld_exps = %lld: must be a multiple of 4 in [ceil(cols / 128), %d]", what, (long long)m->ld_exps, GOSH_FP8_MAX_LD);
+  if (m->rows == 0 || m->cols == 0) return GOSH_OK;
+  if (m->data == nullptr) return fail(GOSH_EINVAL, "%s: data is null", what);
+  if (m->exps == nullptr) return fail(GOSH_EINVAL, "%s: exps is null", what);
+  if (reinterpret_cast<uintptr_t>(m->data) % 16 != 0) return fail(GOSH_EINVAL, "%s: data must be 16-byte aligned", what);
+  if (reinterpret_cast<uintptr_t>(m->exps) % 4 != 0) return fail(GOSH_EINVAL, "%s: exps must be 4-byte aligned", what);
+  if (int rc = check_device_span(m->data, static_cast<size_t>(m->rows - 1) * m->ld + groups * kFp8Block, what)) return rc;
+  return check_device_span(m->exps, static_cast<size_t>(ceil_div(m->rows, m->block_rows) - 1) * m->ld_exps + ceil_div(groups, 4) * 4, what);
+}
+
+namespace {
+
+int check_fp8_shape(const gosh_fp8 *m, const char *what, int64_t rows, int64_t cols) {
+  if (m != nullptr && (m->rows != rows || m->cols != cols))
+    return fail(GOSH_EINVAL, "%s is %lld x %lld: must be %lld x %lld", what, (long long)m->rows, (long long)m->cols, (long long)rows, (long long)cols);
+  return GOSH_OK;
+}
+
+// ---- into 8 bits ----------------------------------------------------------------------------------
+
+struct Fp8Out {
+  uint8_t *data, *exps;
+  int64_t ld, ld_exps;
+};
+Fp8Out fp8_out(const gosh_fp8 *m) {
+  return m == nullptr ? Fp8Out{nullptr, nullptr, 0, 0} : Fp8Out{static_cast<uint8_t *>(m->data), m->exps, m->ld, m->ld_exps};
+}
+
+struct PackArgs {
+  Plane x, z;       // z: x is multiplied by the activation's slope there
+  Fp8Out q, qt;
+  float *sums;      // of the columns of each 128 rows, cols of them
+  int64_t rows, tiles;
+  int32_t cols, tiles_n, act, z_packed;
+};
+
+// Squares of 128 x 128: a lane has 8 columns of 8 rows after each other, 16 lanes a row.  The largest magnitude along a row
+// is joined over those 16 lanes, that along a column over the 16 that have the others of its rows, through LDS; the
+// transposed bytes are turned round in LDS too.  Square: one exponent for all of it.
+template <typename T, bool Square, bool Slope>
+__global__ __launch_bounds__(256) void pack_fp8_kernel(const PackArgs a) {
+  typedef typename T::Store S;
+  __shared__ uint32_t most_of[16][kFp8Block];       // by rows' lanes and column
+  __shared__ float sum_of[Slope ? 16 : 1][kFp8Block];
+  __shared__ __attribute__((aligned(16))) uint8_t turned[kFp8Block * kFp8Block];
+  const int c = threadIdx.x % 16, r = threadIdx.x / 16;
+  for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+    const int64_t row0 = tile / a.tiles_n * kFp8Block + 8 * r;
+    const int tile_n = static_cast<int>(tile % a.tiles_n), col0 = tile_n * kFp8Block + 8 * c;
+    const int count = a.cols - col0 < 0 ? 0 : a.cols - col0 < 8 ? a.cols - col0 : 8;
+    float v[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      Entries<T, 8>::load(static_cast<const S *>(a.x.data) + (row0 + i) * a.x.ld + col0, row0 + i < a.rows ? count : 0, v[i]);
+    if constexpr (Slope) {
+      if (a.act != GOSH_ACT_NONE) {
+        with_activation(a.act, [&](auto f) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float z[8];
+            const int here = row0 + i < a.rows ? count : 0;
+            load_entries<T, 8>(a.z, a.z_packed != 0, row0 + i, col0, here, z);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = e < here ? v[i][e] * decltype(f)::slope(z[e]) : 0.f;
+          }
+        });
+      }
+    }
+    uint32_t along[8], down[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) along[i] = down[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t b = finite_bits(v[i][e]);
+        along[i] = max(along[i], b);
+        down[e] = max(down[e], b);
+      }
+    const bool turn = a.qt.data != nullptr;
+    if (Square || turn || Slope) {
+      __syncthreads();  // the square before has been read
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most_of[r][8 * c + e] = down[e];
+      if constexpr (Slope) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float s = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s += v[i][e];
+          sum_of[r][8 * c + e] = s;
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) down[e] = max(down[e], most_of[k][8 * c + e]);
+      if constexpr (Slope) {
+        if (a.sums != nullptr && threadIdx.x < kFp8Block && tile_n * kFp8Block + static_cast<int>(threadIdx.x) < a.cols) {
+          float s = 0.f;
+#pragma unroll
+          for (int k = 0; k < 16; ++k) s += sum_of[k][threadIdx.x];
+          a.sums[tile / a.tiles_n * a.cols + tile_n * kFp8Block + threadIdx.x] = s;
+        }
+      }
+    }
+    // Square: the largest of all, over a lane's columns and the 16 lanes of a row
+    uint32_t all = 0;
+    if constexpr (Square) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) all = max(all, down[e]);
+      all = larger_of_lanes<0xb1>(all);
+      all = larger_of_lanes<0x4e>(all);
+      all = larger_of_lanes<0x141>(all);
+      all = larger_of_lanes<0x140>(all);
+    }
+    if (a.q.data != nullptr) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t most = all;
+        if constexpr (!Square) {
+          most = larger_of_lanes<0xb1>(along[i]);
+          most = larger_of_lanes<0x4e>(most);
+          most = larger_of_lanes<0x141>(most);
+          most = larger_of_lanes<0x140>(most);
+        }
+        if (row0 + i >= a.rows) continue;
+        const uint32_t byte = fp8_byte(most);
+        const float inv = inverse_unit(byte);
+        *reinterpret_cast<U2 *>(a.q.data + (row0 + i) * a.q.ld + col0) =
+            U2{to_e4m3(v[i][0], v[i][1], v[i][2], v[i][3], inv), to_e4m3(v[i][4], v[i][5], v[i][6], v[i][7], inv)};
+        if (Square ? threadIdx.x == 0 && i == 0 : c == 0)
+          a.q.exps[(Square ? row0 / kFp8Block : row0 + i) * a.q.ld_exps + tile_n] = static_cast<uint8_t>(byte);
+      }
+    }
+    if (!turn) continue;
+    // column 8 c + e of 8 rows: 8 bytes, at place r ^ c of the column's 16
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t byte = fp8_byte(Square ? all : down[e]);
+      const float inv = inverse_unit(byte);
+      *reinterpret_cast<U2 *>(turned + (8 * c + e) * kFp8Block + (r ^ c) * 8) =
+          U2{to_e4m3(v[0][e], v[1][e], v[2][e], v[3][e], inv), to_e4m3(v[4][e], v[5][e], v[6][e], v[7][e], inv)};
+      const int64_t block = tile / a.tiles_n;
+      if (Square ? threadIdx.x == 0 && e == 0 : r == 0 && e < count)
+        a.qt.exps[(Square ? col0 / kFp8Block : col0 + e) * a.qt.ld_exps + block] = static_cast<uint8_t>(byte);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int col = 32 * p + threadIdx.x / 8, pair = threadIdx.x % 8, shift = col / 8;
+      if (tile_n * kFp8Block + col >= a.cols) continue;
+      const U4 x = *reinterpret_cast<const U4 *>(turned + col * kFp8Block + (2 * pair ^ (shift & 14)) * 8);
+      const U4 out = shift & 1 ? U4{x[2], x[3], x[0], x[1]} : x;
+      *reinterpret_cast<U4 *>(a.qt.data + (static_cast<int64_t>(tile_n) * kFp8Block + col) * a.qt.ld + tile / a.tiles_n * kFp8Block + 16 * pair) = out;
+    }
+  }
+}
+
+constexpr int64_t kMostBlocks = int64_t{1} << 22;  // a grid's threads stay below 2^31
+
+template <typename T>
+int launch_pack_fp8(PackArgs a, bool square, bool slope, hipStream_t st) {
+  a.tiles_n = static_cast<int32_t>(ceil_div(a.cols, kFp8Block));
+  a.tiles = ceil_div(a.rows, kFp8Block) * a.tiles_n;
+  const dim3 grid(static_cast<unsigned>(std::min(a.tiles, kMostBlocks))), block(256);
+  if (slope) pack_fp8_kernel<T, false, true><<<grid, block, 0, st>>>(a);
+  else if (square) pack_fp8_kernel<T, true, false><<<grid, block, 0, st>>>(a);
+  else pack_fp8_kernel<T, false, false><<<grid, block, 0, st>>>(a);
+  return check_launch("8-bit floating point");
+}
+int pack_fp8(int32_t type, const PackArgs &a, bool square, bool slope, hipStream_t st) {
+  if (type == GOSH_F32) return launch_pack_fp8<F32>(a, square, slope, st);
+  if (type == GOSH_BF16) return launch_pack_fp8<Bf16>(a, square, slope, st);
+  return launch_pack_fp8<F16>(a, square, slope, st);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void unpack_fp8_kernel(const Fp8Plane q, const Plane x, int64_t rows, int32_t cols, int32_t chunks) {
+  const int64_t total = rows * chunks;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t row = i / chunks;
+    const int col = static_cast<int>(i - row * chunks) * 8;
+    const U2 w = *reinterpret_cast<const U2 *>(q.data + row * q.ld + col);
+    const float unit = read_unit(q.exps[(row >> q.shift) * q.ld_exps + col / kFp8Block]);
+    float v[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      typedef float Two __attribute__((ext_vector_type(2)));
+      const Two lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w[h]), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w[h]), true);
+      v[4 * h] = lo[0] * unit, v[4 * h + 1] = lo[1] * unit, v[4 * h + 2] = hi[0] * unit, v[4 * h + 3] = hi[1] * unit;
+    }
+    Entries<T, 8>::store(static_cast<typename T::Store *>(x.data) + row * x.ld + col, cols - col < 8 ? cols - col : 8, v);
+  }
+}
+
+template <typename T>
+void launch_unpack_fp8(const gosh_fp8 *q, const gosh_mat *x, hipStream_t st) {
+  const int32_t chunks = static_cast<int32_t>(ceil_div(x->cols, 8));
+  const dim3 grid(static_cast<unsigned>(std::min(ceil_div(x->rows * chunks, 256), kMostBlocks)));
+  unpack_fp8_kernel<T><<<grid, dim3(256), 0, st>>>(fp8_plane(q), plane_of(x), x->rows, x->cols, chunks);
+}
+
+// ---- products -------------------------------------------------------------------------------------
+
+Plane rows_of(Plane p, int64_t row, int32_t type, bool packed) { return rows_from(p, row, type, packed); }
+
+int product_fp8(int32_t type, ProductOut out, const Fp8Args &a, hipStream_t st) {
+  if (type == GOSH_F32) return launch_fp8<F32>(out, a, st);
+  if (type == GOSH_BF16) return launch_fp8<Bf16>(out, a, st);
+  return launch_fp8<F16>(out, a, st);
+}
+
+constexpr int64_t kTilesPerLaunch = int64_t{1} << 22;
+
+// All rows of A, as many to a launch as a grid takes.
+int product_of_rows_fp8(int32_t type, ProductOut out, Fp8Args a, int64_t rows, hipStream_t st) {
+  const int tile = 32;
+  a.g.tiles_n = static_cast<int32_t>(ceil_div(a.g.N, tile));
+  a.g.splits = std::max(a.g.splits, 1);
+  a.g.k_per_split = ceil_div(a.g.K, a.g.splits);
+  const int64_t rows_per_launch = std::max<int64_t>(kTilesPerLaunch / a.g.tiles_n * tile / kFp8Block, 1) * kFp8Block;
+  const Fp8Args all = a;
+  for (int64_t r = 0; r < rows; r += rows_per_launch) {
+    a.g.M = std::min(rows_per_launch, rows - r);
+    a.g.tiles_m = static_cast<int32_t>(ceil_div(a.g.M, tile));
+    a.x.data = all.x.data + r * all.x.ld;
+    a.x.exps = all.x.exps + (r >> all.x.shift) * all.x.ld_exps;
+    a.g.out = rows_of(all.g.out, r, type, false);
+    a.g.forward.residual = rows_of(all.g.forward.residual, r, type, false);
+    a.g.forward.y = rows_of(all.g.forward.y, r, type, false);
+    a.g.forward.z = rows_of(all.g.forward.z, r, type, all.g.forward.z_packed != 0);
+    if (int rc = product_fp8(type, out, a, st)) return rc;
+  }
+  return GOSH_OK;
+}
+
+uint64_t round_up(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// How dw is split along the rows.
+struct Fp8DwPlan {
+  int32_t tiles_m, tiles_n, splits;
+  int64_t blocks_per_split;
+};
+Fp8DwPlan plan_dw_fp8(int64_t rows, int32_t in, int32_t out) {
+  Fp8DwPlan p;
+  p.tiles_m = static_cast<int32_t>(ceil_div(out, 32));
+  p.tiles_n = static_cast<int32_t>(ceil_div(in, 32));
+  const int64_t tiles = static_cast<int64_t>(p.tiles_m) * p.tiles_n, blocks = ceil_div(rows, kFp8Block);
+  const int64_t want = std::max<int64_t>(1, std::min(blocks / 8, 1024 / tiles));
+  p.blocks_per_split = std::max<int64_t>(1, ceil_div(blocks, want));
+  p.splits = static_cast<int32_t>(ceil_div(blocks, p.blocks_per_split));
+  return p;
+}
+
+// What the gradient's workspace holds, as offsets.
+struct Fp8BackwardPlan {
+  Fp8DwPlan dw;
+  int64_t ld, ld_exps, ld_t, ld_exps_t;
+  uint64_t q, exps, qt, exps_t, sums, dw_parts, bytes;
+};
+Fp8BackwardPlan plan_backward_fp8(int64_t rows, int32_t in, int32_t out) {
+  Fp8BackwardPlan p;
+  p.dw = plan_dw_fp8(rows, in, out);
+  const int64_t blocks = ceil_div(out, kFp8Block), blocks_t = ceil_div(rows, kFp8Block);
+  p.ld = blocks * kFp8Block, p.ld_exps = ceil_div(blocks, 4) * 4;
+  p.ld_t = blocks_t * kFp8Block, p.ld_exps_t = ceil_div(blocks_t, 4) * 4;
+  uint64_t at = 0;
+  const auto take = [&](uint64_t bytes) {
+    const uint64_t from = at;
+    at += round_up(bytes);
+    return from;
+  };
+  p.q = take(static_cast<uint64_t>(rows) * p.ld);
+  p.exps = take(static_cast<uint64_t>(rows) * p.ld_exps);
+  p.qt = take(static_cast<uint64_t>(out) * p.ld_t);
+  p.exps_t = take(static_cast<uint64_t>(out) * p.ld_exps_t);
+  p.sums = take(static_cast<uint64_t>(blocks_t) * out * 4);
+  p.dw_parts = take(static_cast<uint64_t>(p.dw.splits) * in * out * 4);
+  p.bytes = at;
+  return p;
+}
+
+}  // namespace
+}  // namespace gosh
+
+extern "C" {
+
+int gosh_pack_fp8(const gosh_mat *x, const gosh_fp8 *q, const gosh_fp8 *qt, void *hip_stream) {
+  using namespace gosh;
+  if (int rc = check_mat(x, "x")) return rc;
+  if (int rc = check_fp8(q, "q", kOptional)) return rc;
+  if (int rc = check_fp8(qt, "qt", kOptional)) return rc;
+  if (int rc = check_fp8_shape(q, "q", x->rows, x->cols)) return rc;
+  if (int rc = check_fp8_shape(qt, "qt", x->cols, x->rows)) return rc;
+  if (q != nullptr && qt != nullptr && q->block_rows != qt->block_rows)
+    return fail(GOSH_EINVAL, "q and qt: block_rows = %d and %d: must be the same", q->block_rows, qt->block_rows);
+  if (x->rows == 0 || (q == nullptr && qt == nullptr)) return GOSH_OK;
+  PackArgs a{};
+  a.x = plane_of(x);
+  a.q = fp8_out(q);
+  a.qt = fp8_out(qt);
+  a.rows = x->rows;
+  a.cols = x->cols;
+  return pack_fp8(x->type, a, (q != nullptr ? q : qt)->block_rows == kFp8Block, false, as_stream(hip_stream));
+}
+
+int gosh_unpack_fp8(const gosh_fp8 *q, const gosh_mat *x, void *hip_stream) {
+  using namespace gosh;
+  if (int rc = check_fp8(q, "q")) return rc;
+  if (int rc = check_mat(x, "x")) return rc;
+  if (int rc = check_fp8_shape(q, "q", x->rows, x->cols)) return rc;
+  if (x->rows == 0) return GOSH_OK;
+  hipStream_t st = as_stream(hip_stream);
+  if (x->type == GOSH_F32) launch_unpack_fp8<F32>(q, x, st);
+  else if (x->type == GOSH_BF16) launch_unpack_fp8<Bf16>(q, x, st);
+  else launch_unpack_fp8<F16>(q, x, st);
+  return check_launch("8-bit floating point back");
+}
+
+int gosh_linear_fp8(const gosh_mat *x, const gosh_fp8 *x8, const gosh_fp8 *w, const float *bias, int32_t act,
+                    const gosh_mat *residual, const gosh_mat *y, const gosh_mat *z, void *hip_stream) {
+  using namespace gosh;
+  if (int rc = check_mat(x, "x", kOptional)) return rc;
+  if (int rc = check_fp8(x8, "x8")) return rc;
+  if (int rc = check_fp8(w, "w")) return rc;
+  if (int rc = check_mat(y, "y")) return rc;
+  if (int rc = check_mat(residual, "residual", kOptional)) return rc;
+  if (int rc = check_mat(z, "z", kOptional | kMayBePacked)) return rc;
+  if (act < GOSH_ACT_NONE || act > GOSH_ACT_SILU) return fail(GOSH_EINVAL, "act = %d: no activation", act);
+  if (w->rows < 1 || w->rows > GOSH_MAT_MAX_COLS)
+    return fail(GOSH_EINVAL, "w: rows = %lld: must be in [1, %d]", (long long)w->rows, GOSH_MAT_MAX_COLS);
+  if (w->cols < 1 || w->cols > GOSH_MAT_MAX_COLS)
+    return fail(GOSH_EINVAL, "w: cols = %lld: must be in [1, %d]", (long long)w->cols, GOSH_MAT_MAX_COLS);
+  if (x8->block_rows != 1) return fail(GOSH_EINVAL, "x8: block_rows = %d: must be 1", x8->block_rows);
+  const int32_t out = static_cast<int32_t>(w->rows), in = static_cast<int32_t>(w->cols);
+  const int64_t rows = x8->rows;
+  if (int rc = check_fp8_shape(x8, "x8", rows, in)) return rc;
+  if (int rc = check_shape(x, "x", rows, in)) return rc;
+  const struct { const gosh_mat *m; const char *what; } outs[] = {{y, "y"}, {residual, "residual"}, {z, "z"}};
+  for (const auto &o : outs) {
+    if (int rc = check_shape(o.m, o.what, rows, out)) return rc;
+    if (int rc = check_type(o.m, o.what, y->type)) return rc;
+  }
+  if (int rc = check_floats(bias, out, "bias", true)) return rc;
+  if (rows == 0) return GOSH_OK;
+  hipStream_t st = as_stream(hip_stream);
+  if (x != nullptr)
+    if (int rc = gosh_pack_fp8(x, x8, nullptr, hip_stream)) return rc;
+  Fp8Args a{};
+  a.x = fp8_plane(x8);
+  a.w = fp8_plane(w);
+  a.g.N = out;
+  a.g.K = ceil_div(in, kFp8Block);
+  a.g.forward = ForwardOut{bias, plane_of(residual), plane_of(y), plane_of(z), Plane{nullptr, nullptr, 0, 0}, act, z != nullptr && z->packed, 0};
+  return product_of_rows_fp8(y->type, kForward, a, rows, st);
+}
+
+uint64_t gosh_linear_fp8_backward_workspace(int64_t rows, int32_t in, int32_t out) {
+  if (!gosh::rows_fit(rows) || in < 1 || out < 1 || in > GOSH_MAT_MAX_COLS || out > GOSH_MAT_MAX_COLS) return 0;
+  return gosh::plan_backward_fp8(rows, in, out).bytes;
+}
+
+int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_fp8 *wt, const gosh_mat *z, int32_t act,
+                             const gosh_mat *dx, const gosh_mat *dw, float *db, void *workspace, uint64_t workspace_bytes,
+                             void *hip_stream) {
+  using namespace gosh;
+  if (int rc = check_mat(dy, "dy")) return rc;
+  if (int rc = check_fp8(xt, "xt", dw == nullptr ? kOptional : 0)) return rc;
+  if (int rc = check_fp8(wt, "wt", dx == nullptr ? kOptional : 0)) return rc;
+  if (act < GOSH_ACT_NONE || act > GOSH_ACT_SILU) return fail(GOSH_EINVAL, "act = %d: no activation", act);
+  if (int rc = check_mat(z, "z", kMayBePacked | (act == GOSH_ACT_NONE ? kOptional : 0))) return rc;
+  if (int rc = check_mat(dx, "dx", kOptional)) return rc;
+  if (int rc = check_mat(dw, "dw", kOptional)) return rc;
+  if (dx == nullptr && dw == nullptr) return fail(GOSH_EINVAL, "dx and dw are null: gosh_linear_backward gives db alone");
+  const int64_t rows = dy->rows;
+  const int32_t out = dy->cols, in = dx != nullptr ? dx->cols : dw->cols;
+  if (out > GOSH_MAT_MAX_COLS) return fail(GOSH_EINVAL, "dy: cols = %d: must be at most %d", out, GOSH_MAT_MAX_COLS);
+  if (dw != nullptr && rows > GOSH_FP8_MAX_LD)
+    return fail(GOSH_EINVAL, "dy: rows = %lld: dw takes at most %d", (long long)rows, GOSH_FP8_MAX_LD);
+  if (int rc = check_fp8_shape(xt, "xt", in, rows)) return rc;
+  if (int rc = check_fp8_shape(wt, "wt", in, out)) return rc;
+  if (xt != nullptr && xt->block_rows != 1) return fail(GOSH_EINVAL, "xt: block_rows = %d: must be 1", xt->block_rows);
+  if (int rc = check_shape(z, "z", rows, out)) return rc;
+  if (int rc = check_shape(dx, "dx", rows, in)) return rc;
+  if (int rc = check_shape(dw, "dw", out, in)) return rc;
+  if (int rc = check_type(z, "z", dy->type)) return rc;
+  if (int rc = check_type(dx, "dx", dy->type)) return rc;
+  if (dw != nullptr && dw->type != GOSH_F32)
+    if (int rc = check_type(dw, "dw", dy->type)) return rc;
+  if (int rc = check_floats(db, out, "db", true)) return rc;
+  const Fp8BackwardPlan p = plan_backward_fp8(rows, in, out);
+  if (int rc = check_workspace(workspace, workspace_bytes, p.bytes)) return rc;
+  hipStream_t st = as_stream(hip_stream);
+  uint8_t *const ws = static_cast<uint8_t *>(workspace);
+  float *const sums = reinterpret_cast<float *>(ws + p.sums), *const dw_parts = reinterpret_cast<float *>(ws + p.dw_parts);
+  JoinJob jobs[3];
+  int joins = 0;
+  if (rows > 0) {
+    PackArgs a{};
+    a.x = plane_of(dy);
+    a.z = plane_of(act == GOSH_ACT_NONE ? nullptr : z);
+    if (dx != nullptr) a.q = Fp8Out{ws + p.q, ws + p.exps, p.ld, p.ld_exps};
+    if (dw != nullptr) a.qt = Fp8Out{ws + p.qt, ws + p.exps_t, p.ld_t, p.ld_exps_t};
+    a.sums = db != nullptr ? sums : nullptr;
+    a.rows = rows;
+    a.cols = out;
+    a.act = act;
+    a.z_packed = act != GOSH_ACT_NONE && z->packed;
+    if (int rc = pack_fp8(dy->type, a, false, true, st)) return rc;
+  }
+  if (dx != nullptr && rows > 0) {
+    Fp8Args a{};
+    a.x = Fp8Plane{ws + p.q, ws + p.exps, p.ld, p.ld_exps, 0};
+    a.w = fp8_plane(wt);
+    a.g.N = in;
+    a.g.K = ceil_div(out, kFp8Block);
+    a.g.out = plane_of(dx);
+    if (int rc = product_of_rows_fp8(dx->type, kStore, a, rows, st)) return rc;
+  }
+  if (dw != nullptr) {
+    if (rows > 0) {
+      Fp8Args a{};
+      a.x = Fp8Plane{ws + p.qt, ws + p.exps_t, p.ld_t, p.ld_exps_t, 0};
+      a.w = fp8_plane(xt);
+      a.g.M = out;
+      a.g.N = in;
+      a.g.K = ceil_div(rows, kFp8Block);
+      a.g.tiles_m = p.dw.tiles_m;
+      a.g.tiles_n = p.dw.tiles_n;
+      a.g.splits = p.dw.splits;
+      a.g.k_per_split = p.dw.blocks_per_split;
+      a.g.parts = dw_parts;
+      if (int rc = dw->type == GOSH_F32 ? launch_fp8<F32>(kParts, a, st) : launch_fp8<Bf16>(kParts, a, st)) return rc;
+    }
+    const int64_t n = static_cast<int64_t>(out) * in;
+    jobs[joins++] = {dw_parts, n, n, dw->ld, dw->data, rows > 0 ? p.dw.splits : 0, in, dw->type};
+  }
+  if (db != nullptr) jobs[joins++] = {sums, out, out, out, db, static_cast<int32_t>(ceil_div(rows, kFp8Block)), out, GOSH_F32};
+  return join_parts(jobs, joins, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,11 @@
+// Matrix products in 8-bit floating point, results of type F16.
+#include "gosh_fp8_product.h"
+
+namespace gosh {
+
+template <>
+int launch_fp8<F16>(ProductOut out, const Fp8Args &args, hipStream_t st) {
+  return launch_fp8_any<F16>(out, args, st);
+}
+
+}  // namespace gosh

@@ -28,10 +28,12 @@ inline Fp8Plane fp8_plane(const gosh_fp8 *m) {
 struct Fp8Args {
   Fp8Plane x, w;   // A (M rows), B (N rows)
   ProductArgs g;   // M, N, tiles, splits and where the results go; K and k_per_split count blocks
+  int32_t tile;    // side of a tile: 32, or 64, 128 and 256 straight to LDS
+  int32_t exact;   // kForward in bf16: see fp8_mma
 };
 
 // Defined in gosh_fp8_{f32,bf16,f16}.hip, by the type of the results; kParts: F32 for sums that stay in 32 bits, Bf16 for
-// those that are rounded to 16.
+// those that are rounded to bf16.
 template <typename T>
 int launch_fp8(ProductOut out, const Fp8Args &args, hipStream_t st);
 template <>
@@ -85,11 +87,12 @@ __device__ __forceinline__ S8 widened(uint32_t lo, uint32_t hi, float unit) {
 // 64 k of 32 x 32 products, 32 bytes of each lane's row; any order of k is right that both sides share.
 //
 // Exact: through bf16, which holds a number of 4 bits times a power of two as it is, and whose products the matrix cores sum
-// in 32 bits.  Otherwise in 8 bits, at twice the rate: there the cores align eight products (of neighbouring k) to the largest of them
-// and cut off what is below 2^-13 of its power of two, so that a sum ends up to 7 * 2^-13 of its largest products off, by measurement
-// 1.3e-5 of its rms for normal entries and 8e-5 for entries that differ by e^1.5 (32-bit sums: 1e-7).  That is a
-// thousandth of what the entries' own rounding to 4 bits does, and below half a step of 16-bit results: those take 8 bits,
-// 32-bit results bf16.
+// in 32 bits.  Otherwise in 8 bits, at twice the rate: there the cores align eight products (of neighbouring k) to the largest of
+// them and cut off what is below 2^-13 of its power of two, so that a sum ends up to 7 * 2^-13 of its largest products off,
+// by measurement 1.3e-5 of its rms for normal entries and 8e-5 for entries that differ by e^1.5 (32-bit sums: 1e-7).
+// That is a thousandth of what the entries' own rounding to 4 bits does, and less than half a step of bf16, 2^-8: results of bf16
+// take it.  It is more than half a step of f16 or f32, which are exact, and so is a layer with ReLU, whose slope jumps with z's
+// sign: 20,011 x 132 -> 517 had a z in 100,000 on the other side of 0, and db ended 0.4 % of its rms off.
 template <bool Exact>
 __device__ __forceinline__ F16x fp8_mma(const U4 (&a)[2], const U4 (&b)[2], uint32_t byte_a, uint32_t byte_b, F16x c) {
   if constexpr (Exact) {

@@ -232,9 +232,22 @@ int product_fp8(int32_t type, ProductOut out, const Fp8Args &a, hipStream_t st) 
 
 constexpr int64_t kTilesPerLaunch = int64_t{1} << 22;
 
+// The side of the tiles of a product of which the busiest of the device's 256 CUs has the least work.
+int fp8_tiles_for(int64_t M, int64_t N) {
+  if (M <= 32) return 32;
+  int best = 64;
+  double least = 0;
+  for (int s : {64, 128, 256}) {
+    const double turns = static_cast<double>(ceil_div(ceil_div(M, s) * ceil_div(N, s), 256));
+    const double work = turns * s * s * (s == 256 ? 1.0 : s == 128 ? 1.2 : 2.6);
+    if (s == 64 || work <= least) best = s, least = work;
+  }
+  return best;
+}
+
 // All rows of A, as many to a launch as a grid takes.
 int product_of_rows_fp8(int32_t type, ProductOut out, Fp8Args a, int64_t rows, hipStream_t st) {
-  const int tile = 32;
+  const int tile = a.tile = fp8_tiles_for(rows, a.g.N);
   a.g.tiles_n = static_cast<int32_t>(ceil_div(a.g.N, tile));
   a.g.splits = std::max(a.g.splits, 1);
   a.g.k_per_split = ceil_div(a.g.K, a.g.splits);
@@ -258,18 +271,27 @@ uint64_t round_up(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // How dw is split along the rows.
 struct Fp8DwPlan {
-  int32_t tiles_m, tiles_n, splits;
+  int32_t tile, tiles_m, tiles_n, splits;
   int64_t blocks_per_split;
 };
 Fp8DwPlan plan_dw_fp8(int64_t rows, int32_t in, int32_t out) {
-  Fp8DwPlan p;
-  p.tiles_m = static_cast<int32_t>(ceil_div(out, 32));
-  p.tiles_n = static_cast<int32_t>(ceil_div(in, 32));
-  const int64_t tiles = static_cast<int64_t>(p.tiles_m) * p.tiles_n, blocks = ceil_div(rows, kFp8Block);
-  const int64_t want = std::max<int64_t>(1, std::min(blocks / 8, 1024 / tiles));
-  p.blocks_per_split = std::max<int64_t>(1, ceil_div(blocks, want));
-  p.splits = static_cast<int32_t>(ceil_div(blocks, p.blocks_per_split));
-  return p;
+  Fp8DwPlan best{};
+  double least = 0;
+  const int64_t blocks = ceil_div(rows, kFp8Block);
+  for (int s : {64, 128, 256}) {
+    Fp8DwPlan p;
+    p.tile = s;
+    p.tiles_m = static_cast<int32_t>(ceil_div(out, s));
+    p.tiles_n = static_cast<int32_t>(ceil_div(in, s));
+    const int64_t tiles = static_cast<int64_t>(p.tiles_m) * p.tiles_n;
+    const int64_t want = std::max<int64_t>(1, std::min(blocks / 4, (s == 256 ? 256 : 512) / tiles));
+    p.blocks_per_split = std::max<int64_t>(1, ceil_div(blocks, want));
+    p.splits = static_cast<int32_t>(ceil_div(blocks, p.blocks_per_split));
+    // of the busiest CU
+    const double work = static_cast<double>(ceil_div(tiles * p.splits, 256)) * s * s * (s == 256 ? 1.0 : s == 128 ? 1.2 : 2.6) * p.blocks_per_split;
+    if (s == 64 || work <= least) best = p, least = work;
+  }
+  return best;
 }
 
 // What the gradient's workspace holds, as offsets.
@@ -372,6 +394,7 @@ int gosh_linear_fp8(const gosh_mat *x, const gosh_fp8 *x8, const gosh_fp8 *w, co
   a.g.N = out;
   a.g.K = ceil_div(in, kFp8Block);
   a.g.forward = ForwardOut{bias, plane_of(residual), plane_of(y), plane_of(z), Plane{nullptr, nullptr, 0, 0}, act, z != nullptr && z->packed, 0};
+  a.exact = act == GOSH_ACT_RELU;
   return product_of_rows_fp8(y->type, kForward, a, rows, st);
 }
 
@@ -445,12 +468,13 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
       a.g.M = out;
       a.g.N = in;
       a.g.K = ceil_div(rows, kFp8Block);
+      a.tile = p.dw.tile;
       a.g.tiles_m = p.dw.tiles_m;
       a.g.tiles_n = p.dw.tiles_n;
       a.g.splits = p.dw.splits;
       a.g.k_per_split = p.dw.blocks_per_split;
       a.g.parts = dw_parts;
-      if (int rc = dw->type == GOSH_F32 ? launch_fp8<F32>(kParts, a, st) : launch_fp8<Bf16>(kParts, a, st)) return rc;
+      if (int rc = dw->type == GOSH_BF16 ? launch_fp8<Bf16>(kParts, a, st) : launch_fp8<F32>(kParts, a, st)) return rc;
     }
     const int64_t n = static_cast<int64_t>(out) * in;
     jobs[joins++] = {dw_parts, n, n, dw->ld, dw->data, rows > 0 ? p.dw.splits : 0, in, dw->type};

@@ -54,19 +54,19 @@ def fp8_values(q, exps, rows, cols, tall):
     return v[:, :cols] * two(e[:, :cols] - 127)
 
 
-def product_bound(a, b, dtype):
+def product_bound(a, b, dtype, kind=H.NONE):
     """How far the sum over the columns of a and b of products may be off before it is rounded to `dtype`, values that 8 bits
     stand for: a product of two e4m3 numbers and powers of two is exact in 32 bits, and the matrix cores may cut a sum of them
-    off where 32 bits would round it, 2^-23 a term.  For 16-bit results they take eight products at a time, of which seven
-    may lose what is below 2^-13 of the largest: 7 * 2^-13 of the magnitudes."""
+    off where 32 bits would round it, 2^-23 a term.  For bfloat16 (not with ReLU) they take eight products at a time, of which
+    seven may lose what is below 2^-13 of the largest: 7 * 2^-13 of the magnitudes."""
     size = a.abs() @ b.abs().t()
-    return size * (2 * (a.shape[1] + 8) * F32 + (0 if dtype == torch.float32 else 7 * 2.0 ** -13))
+    return size * (2 * (a.shape[1] + 8) * F32 + (7 * 2.0 ** -13 if dtype == torch.bfloat16 and kind != H.RELU else 0))
 
 
 def linear_fp8(x, w, b, kind, r, dtype):
     """As H.linear, of values that 8 bits stand for, with the bound of their products."""
     y, z, ey, ez = H.linear(x, w, b, kind, r)
-    more = product_bound(x, w, dtype)
+    more = product_bound(x, w, dtype, kind)
     return y, z, ey + 1.13 * more, ez + more
 
 

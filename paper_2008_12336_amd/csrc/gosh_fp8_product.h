@@ -103,7 +103,6 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
   typedef Fp8Units<BM, BN, kWaves> Units;
   constexpr int WM = BM / 2, WN = BN / kAcross, RM = WM / 32, RN = WN / 32, kRing = 2;
   constexpr int kStep = TA::kBytes + TB::kBytes + Units::kBytes;
-  constexpr int kStores = RM * 4;  // of a wavefront for a whole tile, at least
   __shared__ __attribute__((aligned(1024))) uint16_t lds[kRing * kStep / 2];
   __shared__ __attribute__((aligned(16))) float slabs[kWaves * Slab<WN>::kFloats];
 
@@ -143,7 +142,6 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
   };
   begin();
   fetch();
-  fetch();
 
   const uint16_t *now = lds;
   U4 fa[2][2], fb[2][RN][2];  // 32 rows by 64 k: the ones in work and the next
@@ -169,11 +167,9 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
   };
   float bias[RN];
   load_bias<RN, Out>(g, place_of(g, turns.id, BM, BN).n0 + wn, bias);
-  constexpr int kLoads = TA::kLoads + TB::kLoads + 1;
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(kLoads) : "memory");
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
   take_b(0);
   take_a(0, 0, 0);
-  bool stored = false;  // the wavefront has written a whole tile just before
   for (int id = turns.id; id < turns.end; id += turns.step) {
     const Place at = place_of(g, id, BM, BN);
     const int steps = static_cast<int>(at.k1 - at.k0);
@@ -186,6 +182,8 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
       for (int j = 0; j < RN; ++j) acc[i][j] = fp8_mma<Exact>(fa[from], fb[half][j], ea[i], eb[j], acc[i][j]);
     };
     for (int s = 0; s < steps; ++s) {
+      // Before the products, since there is a branch in it: the compiler would move the products behind it.
+      fetch();
       take_units(static_cast<int>(at.k0) + s);
       constexpr int kTurns = 2 * RM;  // 32 rows by 64 k each
 #pragma unroll
@@ -196,14 +194,11 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
         multiply(t & 1, t % RM, t / RM);
         __builtin_amdgcn_sched_barrier(0);
       }
-      // The next step's loads are there: followed only, in the first step after a tile, by its stores.  Then every wavefront's
-      // part is, and every wavefront is done with this step's tile, which the next loads replace.
-      if (stored && s == 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(kStores) : "memory");
-      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      // The next step's tile is there, every wavefront's part of it, and every wavefront is done with this step's.
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       now = now == lds ? lds + kStep / 2 : lds;
       take_b(0);
       take_a(0, 0, 0);
-      fetch();
       __builtin_amdgcn_sched_barrier(0);
       multiply((kTurns - 1) & 1, RM - 1, 1);
     }
@@ -211,7 +206,6 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
 #pragma unroll
     for (int j = 0; j < RN; ++j) asm volatile("" : "+v"(bias[j]));
     finish<T, RM, RN, Out>(g, acc, slabs + wave * Slab<WN>::kFloats, at.m0 + wm, at.n0 + wn, at.split);
-    stored = WN == 64 && at.m0 + wm + WM <= g.M && at.n0 + wn + WN <= g.N;
   }
   // no load may land in LDS that is another workgroup's by then
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");

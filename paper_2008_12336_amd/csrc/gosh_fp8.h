@@ -52,20 +52,11 @@ __device__ __forceinline__ uint32_t fp8_byte(uint32_t most) {
   return e < 9 ? 1 : e - 8;
 }
 
-// The magnitude's bits, of what is finite.
-__device__ __forceinline__ uint32_t finite_bits(float v) {
-  const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
-  return b < 0x7f800000u ? b : 0u;
-}
-
-// Four entries' e4m3 as a word, from entries in 32 bits that are at most 448 units or not finite.
+// Four entries' e4m3 as a word, from entries in 32 bits that are at most 448 units or NaN, which stays NaN.  The product is
+// exact, or below what rounds to zero.
 __device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d, float inverse) {
-  const auto in = [&](float v) {
-    const float x = v * inverse;  // exact, or below what rounds to zero
-    return __builtin_fabsf(x) < INFINITY ? x : __uint_as_float(0x7fc00000u);
-  };
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(in(a), in(b), 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(in(c), in(d), w, true);
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inverse, b * inverse, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inverse, d * inverse, w, true);
   return static_cast<uint32_t>(w);
 }
 

@@ -57,53 +57,107 @@ __global__ __launch_bounds__(256) void fp8_small_kernel(const Fp8Args a) {
 
 // ---- many tiles: straight to LDS ------------------------------------------------------------------------
 
-// The exponents of a step: a lane of the wavefront that has 64 rows of an operand loads four blocks' bytes of its row
-// straight to LDS, of which a step takes one.  64 rows of A for each of the first wavefronts, then of B; those that are left
-// over load what the first ones do, so that all have as many loads under way.
+// The range of memory that a wavefront's loads may touch, in scalar registers; the loads move along it.
+struct Fp8Range {
+  uint64_t base;
+  uint32_t bytes;
+  __device__ __forceinline__ U4 words() const {
+    return U4{static_cast<uint32_t>(base), static_cast<uint32_t>(base >> 32) & 0xffffu, bytes, 0x00020000u};
+  }
+};
+// m0, which the compiler sets, holds where the first lane's bytes land.  The compiler does not count the wait states of an
+// instruction that it cannot see: s_nop 4 are the five that the load needs behind a vector instruction that wrote its range.
+template <bool Dword>
+__device__ __forceinline__ void load_to_lds(uint32_t off, const Fp8Range &r, uint32_t lds) {
+  if constexpr (Dword)
+    asm volatile("s_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" :: "v"(off), "s"(r.words()), "{m0}"(lds) : "memory");
+  else
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" :: "v"(off), "s"(r.words()), "{m0}"(lds) : "memory");
+}
+
+// BX rows of an operand by 128 k, which the memory system writes to LDS by itself, 1 KB an instruction of a wavefront: the lanes
+// ask for the chunks of 16 bytes that belong where theirs land.  Rows past the end read as zero.
+template <int BX, int Waves>
+struct Fp8Tile {
+  static constexpr int kBytes = BX * kFp8Block, kLoads = kBytes / 1024 / Waves;
+  Fp8Range range;
+  uint32_t off[kLoads];
+  __device__ __forceinline__ void init(const Fp8Plane &p) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = (static_cast<int>(threadIdx.x / 64) * kLoads + i) * 64 + (threadIdx.x & 63), row = at / 8, slot = at % 8;
+      // the shifts are their own inverse
+      off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(p.ld) + Spread<BX, 64>::k_major(row, slot) / 8 % 8 * 16;
+    }
+  }
+  // At most 256 rows of 2^23 bytes: 2^31.
+  __device__ __forceinline__ void begin(const Fp8Plane &p, int64_t x, int64_t rows, int64_t blocks, int64_t k0) {
+    range.base = reinterpret_cast<uint64_t>(p.data) + x * p.ld + k0 * kFp8Block;
+    const int64_t here = rows - x < BX ? rows - x : BX;
+    range.bytes = static_cast<uint32_t>((here - 1) * p.ld + (blocks - k0) * kFp8Block);
+  }
+  __device__ __forceinline__ void load(int i, uint32_t lds) const {
+    load_to_lds<false>(off[i], range, lds + (__builtin_amdgcn_readfirstlane(threadIdx.x / 64) * kLoads + i) * 1024);
+  }
+};
+
+// The exponents of a step: a lane of the wavefront that has 64 rows of an operand loads four blocks' bytes of its row,
+// of which a step takes one.  64 rows of A for each of the first wavefronts, then of B; those that are left over load what the
+// first ones do.
 template <int BM, int BN, int Waves>
 struct Fp8Units {
   static constexpr int kSlots = (BM + BN) / 64, kBytes = Waves * 256;
   static_assert(kSlots <= Waves, "a wavefront has one slot");
-  uint64_t base;
-  int64_t bytes, left;   // of the matrix's exponents from base on; blocks of k up to the row's end
+  Fp8Range range;
   uint32_t off;
-  int block;             // of k, the next to load
+  int block;  // of k
 
   __device__ __forceinline__ void begin(const Fp8Args &a, int64_t m0, int64_t n0, int64_t k0) {
     const int slot = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % kSlots;
     const bool of_a = slot < BM / 64;
-    const Fp8Plane &p = of_a ? a.x : a.w;
-    const int64_t rows = of_a ? a.g.M : a.g.N, row0 = of_a ? m0 + 64 * slot : n0 + 64 * (slot - BM / 64);
-    const int64_t first = row0 >> p.shift, last = (rows - 1) >> p.shift;
-    base = reinterpret_cast<uint64_t>(p.exps) + first * p.ld_exps;
-    bytes = (last - first) * p.ld_exps + (a.g.K + 3) / 4 * 4;
-    off = static_cast<uint32_t>((((row0 + (threadIdx.x & 63)) >> p.shift) - first) * p.ld_exps);
+    const uint8_t *const exps = of_a ? a.x.exps : a.w.exps;
+    const int64_t ld = of_a ? a.x.ld_exps : a.w.ld_exps, rows = of_a ? a.g.M : a.g.N;
+    const int shift = of_a ? a.x.shift : a.w.shift;
+    const int64_t row0 = of_a ? m0 + 64 * slot : n0 + 64 * (slot - BM / 64);
+    const int64_t first = row0 >> shift, end = rows < row0 + 64 ? rows : row0 + 64;
+    range.base = reinterpret_cast<uint64_t>(exps) + first * ld;
+    range.bytes = end <= row0 ? 0 : static_cast<uint32_t>((((end - 1) >> shift) - first) * ld + (a.g.K + 3) / 4 * 4);
+    off = static_cast<uint32_t>(((row0 + (threadIdx.x & 63)) >> shift) - first) * static_cast<uint32_t>(ld);
     block = static_cast<int>(k0);
   }
-  __device__ __forceinline__ void fetch(uint32_t lds) {
-    const U4 range{static_cast<uint32_t>(base), static_cast<uint32_t>(base >> 32) & 0xffffu,
-                   static_cast<uint32_t>(bytes <= 0 ? 0 : bytes > 0x7fffffff ? 0x7fffffff : bytes), 0x00020000u};
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t o = off + (block & ~3);
-    // as the loads of the tiles
-    asm volatile("s_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" :: "v"(o), "s"(range), "{m0}"(lds + wave * 256) : "memory");
-    ++block;
+  __device__ __forceinline__ void load(uint32_t lds) const {
+    load_to_lds<true>(off + (block & ~3), range, lds + __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 256);
   }
 };
 
-// A ring of two tiles of 128 k, as the products in 16 bits have it: rows of 128 bytes lie in LDS as theirs of 64 entries do.
-// A wavefront multiplies 32 rows by 64 k at a time, while the next such rows of A (and, before the second half of a step, B's) are
-// read from LDS.
+// The id-th tile: of eight rows of tiles those of one column after each other, then the next column's, so that the 32 CUs
+// of an XCD, which work on 32 tiles in a row, share eight tiles of A and four of B: of 131,072 x 1024 -> 4096 those of B alone, 4
+// MB, fill an L2, and with row after row they were fetched again and again (727 -> 697 us).
+__device__ __forceinline__ Place fp8_place(const ProductArgs &g, int id, int bm, int bn) {
+  constexpr int kGroup = 8;
+  const int all = g.tiles_m * g.tiles_n, split = id / all, rest = id % all;
+  const int first = rest / (kGroup * g.tiles_n) * kGroup, tall = g.tiles_m - first < kGroup ? g.tiles_m - first : kGroup;
+  const int in = rest - first * g.tiles_n;
+  const int64_t k0 = split * g.k_per_split;
+  return {static_cast<int64_t>(first + in % tall) * bm, static_cast<int64_t>(in / tall) * bn, k0,
+          k0 + g.k_per_split < g.K ? k0 + g.k_per_split : g.K, split};
+}
+
+// Two tiles in LDS: while a step is multiplied the next one's loads are under way, also across the end of a tile: a workgroup
+// goes from tile to tile.  Rows of 128 bytes lie as those of 64 entries of 16 bits do.  A wavefront multiplies 32 rows by 64
+// k at a time, while the next such rows of A (and, before the second half of a step, B's) are read from LDS.
+//
+// 16,384 x 8192 -> 4096 takes 434 us, 2.53 PFLOP/s, and 427 without the results' way to memory.  131,072 x 1024 -> 4096 takes 621, of
+// which 495 are left without that (2.2 PFLOP/s): 1.07 GB of results need 155 at the rate of a fill.
 template <typename T, int BM, int BN, bool Exact, ProductOut Out>
 __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void fp8_product_kernel(const Fp8Args args) {
   constexpr int kWaves = direct_waves(BN), kAcross = kWaves / 2;
-  constexpr int kHalf = kFp8Block / 2;  // k of a step in the 16-bit units of the tiles
-  typedef DirectTile<BM, kHalf, true, kWaves> TA;
-  typedef DirectTile<BN, kHalf, true, kWaves> TB;
+  typedef Fp8Tile<BM, kWaves> TA;
+  typedef Fp8Tile<BN, kWaves> TB;
   typedef Fp8Units<BM, BN, kWaves> Units;
-  constexpr int WM = BM / 2, WN = BN / kAcross, RM = WM / 32, RN = WN / 32, kRing = 2;
-  constexpr int kStep = TA::kBytes + TB::kBytes + Units::kBytes;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[kRing * kStep / 2];
+  constexpr int WM = BM / 2, WN = BN / kAcross, RM = WM / 32, RN = WN / 32;
+  constexpr int kStep = TA::kBytes + TB::kBytes + Units::kBytes, kLoads = TA::kLoads + TB::kLoads + 1;
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[2 * kStep / 2];
   __shared__ __attribute__((aligned(16))) float slabs[kWaves * Slab<WN>::kFloats];
 
   const ProductArgs &g = args.g;
@@ -111,85 +165,96 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
   const int wm = wave / kAcross * WM, wn = wave % kAcross * WN;
   const Turns turns = turns_of(g.tiles_m * g.tiles_n * g.splits);
   if (turns.id >= turns.end) return;
-  const Plane pa{const_cast<uint8_t *>(args.x.data), nullptr, args.x.ld / 2, 0}, pb{const_cast<uint8_t *>(args.w.data), nullptr, args.w.ld / 2, 0};
 
   const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint16_t *)lds));
   TA a;
   TB b;
   Units units;
-  a.init(pa);
-  b.init(pb);
-  // The loads run ahead of the computation, over tiles; after the last tile they load nothing.
+  a.init(args.x);
+  b.init(args.w);
   uint32_t into = base;
-  int turn = turns.id;
-  int to_go;
+  int turn = turns.id, to_go;
   const auto begin = [&]() {
-    const Place from = place_of(g, turn, BM, BN);
-    a.begin(pa, from.m0, g.M, from.k0 * kHalf, from.k1 * kHalf);
-    b.begin(pb, from.n0, g.N, from.k0 * kHalf, from.k1 * kHalf);
+    const Place from = fp8_place(g, turn, BM, BN);
+    a.begin(args.x, from.m0, g.M, g.K, from.k0);
+    b.begin(args.w, from.n0, g.N, g.K, from.k0);
     units.begin(args, from.m0, from.n0, from.k0);
     to_go = static_cast<int>(from.k1 - from.k0);
   };
-  const auto fetch = [&]() {
-    a.fetch(pa, into);
-    b.fetch(pb, into + TA::kBytes);
-    units.fetch(into + TA::kBytes + TB::kBytes);
+  // On to the step after: the next of the tile, or the first of the next tile, or none, whose loads read nothing.
+  const auto advance = [&]() {
     into = into == base ? base + kStep : base;
-    if (--to_go <= 0 && turn + turns.step < turns.end) {
-      turn += turns.step;
-      begin();
-    }
+    a.range.base += kFp8Block, a.range.bytes -= kFp8Block;
+    b.range.base += kFp8Block, b.range.bytes -= kFp8Block;
+    ++units.block;
+    if (--to_go > 0) return;
+    turn += turns.step;
+    if (turn < turns.end) begin();
+    else a.range.bytes = b.range.bytes = units.range.bytes = 0, to_go = 0x7fffffff;
+  };
+  const auto load = [&](int i) {
+    if (i < TA::kLoads) a.load(i, into);
+    else if (i < TA::kLoads + TB::kLoads) b.load(i - TA::kLoads, into + TA::kBytes);
+    else units.load(into + TA::kBytes + TB::kBytes);
   };
   begin();
-  fetch();
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) load(i);
 
   const uint16_t *now = lds;
   U4 fa[2][2], fb[2][RN][2];  // 32 rows by 64 k: the ones in work and the next
-  uint32_t ea[RM], eb[RN];
+  uint32_t ea[2][RM], eb[2][RN];
   const auto take_a = [&](int to, int i, int half) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) fa[to][c] = __builtin_bit_cast(U4, Spread<BM, kHalf>::template take<true>(now, wm + 32 * i, 2 * half + c));
+    for (int c = 0; c < 2; ++c) fa[to][c] = __builtin_bit_cast(U4, Spread<BM, 64>::template take<true>(now, wm + 32 * i, 2 * half + c));
   };
   const auto take_b = [&](int half) {
 #pragma unroll
     for (int j = 0; j < RN; ++j)
 #pragma unroll
       for (int c = 0; c < 2; ++c)
-        fb[half][j][c] = __builtin_bit_cast(U4, Spread<BN, kHalf>::template take<true>(now + TA::kBytes / 2, wn + 32 * j, 2 * half + c));
+        fb[half][j][c] = __builtin_bit_cast(U4, Spread<BN, 64>::template take<true>(now + TA::kBytes / 2, wn + 32 * j, 2 * half + c));
   };
-  const auto take_units = [&](int block) {
+  const auto take_units = [&](uint32_t (&x)[RM], uint32_t (&w)[RN]) {
     const uint32_t *const e = reinterpret_cast<const uint32_t *>(now + (TA::kBytes + TB::kBytes) / 2);
-    const int shift = (block & 3) * 8;
 #pragma unroll
-    for (int i = 0; i < RM; ++i) ea[i] = e[wm + 32 * i + (lane & 31)] >> shift & 255u;
+    for (int i = 0; i < RM; ++i) x[i] = e[wm + 32 * i + (lane & 31)];
 #pragma unroll
-    for (int j = 0; j < RN; ++j) eb[j] = e[BM + wn + 32 * j + (lane & 31)] >> shift & 255u;
+    for (int j = 0; j < RN; ++j) w[j] = e[BM + wn + 32 * j + (lane & 31)];
   };
   float bias[RN];
-  load_bias<RN, Out>(g, place_of(g, turns.id, BM, BN).n0 + wn, bias);
+  load_bias<RN, Out>(g, fp8_place(g, turns.id, BM, BN).n0 + wn, bias);
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  take_units(ea[0], eb[0]);
   take_b(0);
   take_a(0, 0, 0);
   for (int id = turns.id; id < turns.end; id += turns.step) {
-    const Place at = place_of(g, id, BM, BN);
+    const Place at = fp8_place(g, id, BM, BN);
     const int steps = static_cast<int>(at.k1 - at.k0);
     F16x acc[RM][RN];
     start<RM, RN>(bias, acc);
     if (is_forward(Out) && id + turns.step < turns.end)
-      load_bias<RN, Out>(g, place_of(g, id + turns.step, BM, BN).n0 + wn, bias);
-    const auto multiply = [&](int from, int i, int half) {
-#pragma unroll
-      for (int j = 0; j < RN; ++j) acc[i][j] = fp8_mma<Exact>(fa[from], fb[half][j], ea[i], eb[j], acc[i][j]);
-    };
+      load_bias<RN, Out>(g, fp8_place(g, id + turns.step, BM, BN).n0 + wn, bias);
     for (int s = 0; s < steps; ++s) {
-      // Before the products, since there is a branch in it: the compiler would move the products behind it.
-      fetch();
-      take_units(static_cast<int>(at.k0) + s);
+      advance();  // before the products: the compiler would move them behind its branches
+      const int shift = (static_cast<int>(at.k0) + s & 3) * 8;
+#pragma unroll
+      for (int i = 0; i < RM; ++i) ea[1][i] = ea[0][i] >> shift & 255u;
+#pragma unroll
+      for (int j = 0; j < RN; ++j) eb[1][j] = eb[0][j] >> shift & 255u;
+      const auto multiply = [&](int from, int i, int half) {
+#pragma unroll
+        for (int j = 0; j < RN; ++j) acc[i][j] = fp8_mma<Exact>(fa[from], fb[half][j], ea[1][i], eb[1][j], acc[i][j]);
+      };
       constexpr int kTurns = 2 * RM;  // 32 rows by 64 k each
 #pragma unroll
       for (int t = 0; t + 1 < kTurns; ++t) {
         if (t + 1 == RM) take_b(1);
         take_a((t + 1) & 1, (t + 1) % RM, (t + 1) / RM);
+        if (t == 0) {  // all at once: spread over the turns the last ones arrive late (716 -> 727 us)
+#pragma unroll
+          for (int i = 0; i < kLoads; ++i) load(i);
+        }
         __builtin_amdgcn_sched_barrier(0);
         multiply(t & 1, t % RM, t / RM);
         __builtin_amdgcn_sched_barrier(0);
@@ -197,6 +262,7 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
       // The next step's tile is there, every wavefront's part of it, and every wavefront is done with this step's.
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       now = now == lds ? lds + kStep / 2 : lds;
+      take_units(ea[0], eb[0]);
       take_b(0);
       take_a(0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
@@ -214,6 +280,8 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
 template <typename T, TileSize Size, bool Exact, ProductOut Out>
 int launch_fp8_tiles(const Fp8Args &a, hipStream_t st) {
   constexpr int kTile = tile_m(Size), kWaves = direct_waves(kTile);
+  if constexpr (Size == kLarge && Out == kForward && T::kType != GOSH_F32)
+    if (a.g.forward.past) return launch_fp8_tiles<T, Size, Exact, kPast>(a, st);
   const unsigned blocks = static_cast<unsigned>(a.g.tiles_m) * a.g.tiles_n * a.g.splits;
   const unsigned held = static_cast<unsigned>(resident_waves()) / 4 / kWaves;  // eight wavefronts a CU
   fp8_product_kernel<T, kTile, kTile, Exact, Out><<<dim3(blocks < held ? blocks : held), dim3(64 * kWaves), 0, st>>>(a);

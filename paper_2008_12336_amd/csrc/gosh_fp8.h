@@ -28,7 +28,9 @@ inline Fp8Plane fp8_plane(const gosh_fp8 *m) {
 struct Fp8Args {
   Fp8Plane x, w;   // A (M rows), B (N rows)
   ProductArgs g;   // M, N, tiles, splits and where the results go; K and k_per_split count blocks
-  int32_t tile;    // side of a tile: 32, or 64, 128 and 256 straight to LDS
+  int32_t tile;    // side of a tile: 64, 128 or 256; or 32: a few rows of kForward
+  Plane pack;      // a few rows: x of pack_type and pack_cols columns that is put into 8 bits first, or null
+  int32_t pack_type, pack_cols;
   int32_t exact;   // kForward in bf16: see fp8_mma
 };
 

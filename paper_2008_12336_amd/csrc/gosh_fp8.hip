@@ -298,9 +298,11 @@ constexpr int64_t kTilesPerLaunch = int64_t{1} << 22;
 // 131,072 x 1024 -> 4096 (1.07 GB): 727 us, 643 with it.
 constexpr int64_t kPastCaches = int64_t{256} << 20;
 
+constexpr int64_t kFewRows = 32;
+
 // The side of the tiles of a product of which the busiest of the device's 256 CUs has the least work.
-int fp8_tiles_for(int64_t M, int64_t N) {
-  if (M <= 32) return 32;
+int fp8_tiles_for(ProductOut out, int64_t M, int64_t N) {
+  if (out == kForward && M <= kFewRows) return 32;
   int best = 64;
   double least = 0;
   for (int s : {64, 128, 256}) {
@@ -313,7 +315,7 @@ int fp8_tiles_for(int64_t M, int64_t N) {
 
 // All rows of A, as many to a launch as a grid takes.
 int product_of_rows_fp8(int32_t type, ProductOut out, Fp8Args a, int64_t rows, hipStream_t st) {
-  const int tile = a.tile = fp8_tiles_for(rows, a.g.N);
+  const int tile = a.tile = fp8_tiles_for(out, rows, a.g.N);
   a.g.tiles_n = static_cast<int32_t>(ceil_div(a.g.N, tile));
   a.g.splits = std::max(a.g.splits, 1);
   a.g.k_per_split = ceil_div(a.g.K, a.g.splits);
@@ -452,15 +454,20 @@ int gosh_linear_fp8(const gosh_mat *x, const gosh_fp8 *x8, const gosh_fp8 *w, co
   if (int rc = check_floats(bias, out, "bias", true)) return rc;
   if (rows == 0) return GOSH_OK;
   hipStream_t st = as_stream(hip_stream);
-  if (x != nullptr)
-    if (int rc = gosh_pack_fp8(x, x8, nullptr, hip_stream)) return rc;
   Fp8Args a{};
+  if (x != nullptr && rows <= kFewRows) {  // in the product's launch
+    a.pack = plane_of(x);
+    a.pack_type = x->type;
+    a.pack_cols = in;
+  } else if (x != nullptr) {
+    if (int rc = gosh_pack_fp8(x, x8, nullptr, hip_stream)) return rc;
+  }
   a.x = fp8_plane(x8);
   a.w = fp8_plane(w);
   a.g.N = out;
   a.g.K = ceil_div(in, kFp8Block);
   a.g.forward = ForwardOut{bias, plane_of(residual), plane_of(y), plane_of(z), Plane{nullptr, nullptr, 0, 0}, act, z != nullptr && z->packed,
-                           z == nullptr && rows * out * (y->type == GOSH_F32 ? 4 : 2) >= kPastCaches};
+                           rows * out * (y->type == GOSH_F32 ? 4 : 2) >= kPastCaches};
   a.exact = act == GOSH_ACT_RELU;
   return product_of_rows_fp8(y->type, kForward, a, rows, st);
 }

@@ -6,7 +6,7 @@
 
 namespace gosh {
 
-// ---- a few tiles: four wavefronts share the blocks of k of 32 x 32 results ----------------------------
+// ---- a few rows: the wavefronts of a workgroup share the blocks of k of 32 x 32 results -----------------
 
 // The rows of a tile that a lane reads; rows past the end read the last one's, for results that nobody stores.
 struct Fp8Lane {
@@ -16,29 +16,71 @@ struct Fp8Lane {
     q = p.data + r * p.ld + (threadIdx.x >> 5 & 1) * 32;
     e = p.exps + (r >> p.shift) * p.ld_exps;
   }
+  // Block k: 32 bytes of each half.
+  __device__ __forceinline__ uint32_t load(int64_t k, U4 (&v)[2][2]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i / 2][i % 2] = *reinterpret_cast<const U4 *>(q + k * kFp8Block + i / 2 * 64 + i % 2 * 16);
+    return e[k];
+  }
 };
 
-template <typename T, bool Exact, ProductOut Out>
-__global__ __launch_bounds__(256) void fp8_small_kernel(const Fp8Args a) {
-  __shared__ __attribute__((aligned(16))) float lds[3][16][64];
+// The same of a row that is put into 8 bits on the way, and stored if `keep`: block k's 128 entries are two lanes'.
+template <typename X>
+__device__ __forceinline__ uint32_t pack_block(const Fp8Args &a, int64_t row, int64_t k, bool keep, U4 (&v)[2][2]) {
+  typedef typename X::Store S;
+  const int64_t r = row < a.g.M ? row : a.g.M - 1;
+  const int first = static_cast<int>(k) * kFp8Block + (threadIdx.x >> 5 & 1) * 32;  // column
+  const S *const x = static_cast<const S *>(a.pack.data) + r * a.pack.ld + first;
+  float f[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int left = a.pack_cols - first - (i / 4 * 64 + i % 4 * 8);
+    Entries<X, 8>::load(x + i / 4 * 64 + i % 4 * 8, left < 0 ? 0 : left, f[i]);
+  }
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      f[i][e] = __builtin_fabsf(f[i][e]) == INFINITY ? __uint_as_float(0x7fc00000u) : f[i][e];
+      most = fmaxf(most, __builtin_fabsf(f[i][e]));
+    }
+  most = fmaxf(most, __shfl_xor(most, 32));
+  const uint32_t byte = fp8_byte(__float_as_uint(most));
+  const float inv = inverse_unit(byte);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[i / 4][i / 2 % 2][i % 2 * 2] = to_e4m3(f[i][0], f[i][1], f[i][2], f[i][3], inv);
+    v[i / 4][i / 2 % 2][i % 2 * 2 + 1] = to_e4m3(f[i][4], f[i][5], f[i][6], f[i][7], inv);
+  }
+  if (keep && row < a.g.M) {
+    uint8_t *const to = const_cast<uint8_t *>(a.x.data) + row * a.x.ld + first;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<U4 *>(to + i / 2 * 64 + i % 2 * 16) = v[i / 2][i % 2];
+    if ((threadIdx.x & 32) == 0) const_cast<uint8_t *>(a.x.exps)[row * a.x.ld_exps + k] = static_cast<uint8_t>(byte);
+  }
+  return byte;
+}
+
+// X: the type of the x that is put into 8 bits, or void.
+template <typename T, typename X, bool Exact, int Waves>
+__global__ __launch_bounds__(64 * Waves) void fp8_few_rows_kernel(const Fp8Args a) {
+  __shared__ __attribute__((aligned(16))) float lds[Waves - 1][16][64];
   __shared__ __attribute__((aligned(16))) float slab[Slab<32>::kFloats];
   const ProductArgs &g = a.g;
-  const Place at = place_of(g, static_cast<int>(blockIdx.x), 32, 32);
+  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 32;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const Fp8Lane x(a.x, at.m0 + (lane & 31), g.M), w(a.w, at.n0 + (lane & 31), g.N);
+  const Fp8Lane w(a.w, n0 + (lane & 31), g.N);
   F16x acc[1][1];
   float bias[1] = {0.f};
-  if (wave == 0) load_bias<1, Out>(g, at.n0, bias);
+  if (wave == 0) load_bias<1, kForward>(g, n0, bias);
   start<1, 1>(bias, acc);
-  for (int64_t k = at.k0 + wave; k < at.k1; k += 4) {
+  for (int64_t k = wave; k < g.K; k += Waves) {
     U4 qa[2][2], qb[2][2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t off = k * kFp8Block + i / 2 * 64 + i % 2 * 16;
-      qa[i / 2][i % 2] = *reinterpret_cast<const U4 *>(x.q + off);
-      qb[i / 2][i % 2] = *reinterpret_cast<const U4 *>(w.q + off);
-    }
-    const uint32_t ua = x.e[k], ub = w.e[k];
+    const uint32_t ub = w.load(k, qb);
+    uint32_t ua;
+    if constexpr (std::is_void<X>::value) ua = Fp8Lane(a.x, lane & 31, g.M).load(k, qa);
+    else ua = pack_block<X>(a, lane & 31, k, blockIdx.x == 0, qa);
 #pragma unroll
     for (int h = 0; h < 2; ++h) acc[0][0] = fp8_mma<Exact>(qa[h], qb[h], ua, ub, acc[0][0]);
   }
@@ -49,10 +91,25 @@ __global__ __launch_bounds__(256) void fp8_small_kernel(const Fp8Args a) {
   __syncthreads();
   if (wave != 0) return;
 #pragma unroll
-  for (int s = 0; s < 3; ++s)
+  for (int s = 0; s < Waves - 1; ++s)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[0][0][i] += lds[s][i][lane];
-  finish<T, 1, 1, Out>(g, acc, slab, at.m0, at.n0, at.split);
+  finish<T, 1, 1, kForward>(g, acc, slab, 0, n0, 0);
+}
+
+template <typename T, typename X, bool Exact>
+int launch_fp8_few_rows(const Fp8Args &a, hipStream_t st) {
+  const dim3 grid(static_cast<unsigned>(ceil_div(a.g.N, 32)));
+  if (a.g.K <= 8) fp8_few_rows_kernel<T, X, Exact, 4><<<grid, dim3(256), 0, st>>>(a);
+  else fp8_few_rows_kernel<T, X, Exact, 16><<<grid, dim3(1024), 0, st>>>(a);
+  return check_launch("product of a few rows in 8-bit floating point");
+}
+template <typename T, bool Exact>
+int launch_fp8_few_rows(const Fp8Args &a, hipStream_t st) {
+  if (a.pack.data == nullptr) return launch_fp8_few_rows<T, void, Exact>(a, st);
+  if (a.pack_type == GOSH_F32) return launch_fp8_few_rows<T, F32, Exact>(a, st);
+  if (a.pack_type == GOSH_BF16) return launch_fp8_few_rows<T, Bf16, Exact>(a, st);
+  return launch_fp8_few_rows<T, F16, Exact>(a, st);
 }
 
 // ---- many tiles: straight to LDS ------------------------------------------------------------------------
@@ -281,7 +338,8 @@ template <typename T, TileSize Size, bool Exact, ProductOut Out>
 int launch_fp8_tiles(const Fp8Args &a, hipStream_t st) {
   constexpr int kTile = tile_m(Size), kWaves = direct_waves(kTile);
   if constexpr (Size == kLarge && Out == kForward && T::kType != GOSH_F32)
-    if (a.g.forward.past) return launch_fp8_tiles<T, Size, Exact, kPast>(a, st);
+    if (a.g.forward.past)
+      return a.g.forward.z.data == nullptr ? launch_fp8_tiles<T, Size, Exact, kPast>(a, st) : launch_fp8_tiles<T, Size, Exact, kPastZ>(a, st);
   const unsigned blocks = static_cast<unsigned>(a.g.tiles_m) * a.g.tiles_n * a.g.splits;
   const unsigned held = static_cast<unsigned>(resident_waves()) / 4 / kWaves;  // eight wavefronts a CU
   fp8_product_kernel<T, kTile, kTile, Exact, Out><<<dim3(blocks < held ? blocks : held), dim3(64 * kWaves), 0, st>>>(a);
@@ -293,12 +351,11 @@ int launch_fp8_out(const Fp8Args &a, hipStream_t st) {
   switch (a.tile) {
     case 256: return launch_fp8_tiles<T, kLarge, Exact, Out>(a, st);
     case 128: return launch_fp8_tiles<T, kMiddle, Exact, Out>(a, st);
-    case 64: return launch_fp8_tiles<T, kSmall, Exact, Out>(a, st);
     default: break;
   }
-  const unsigned blocks = static_cast<unsigned>(a.g.tiles_m) * a.g.tiles_n * a.g.splits;
-  fp8_small_kernel<T, Exact, Out><<<dim3(blocks), dim3(256), 0, st>>>(a);
-  return check_launch("product in 8-bit floating point");
+  if constexpr (Out == kForward)
+    if (a.tile == 32) return launch_fp8_few_rows<T, Exact>(a, st);
+  return launch_fp8_tiles<T, kSmall, Exact, Out>(a, st);
 }
 
 template <typename T>

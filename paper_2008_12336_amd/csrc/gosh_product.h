@@ -36,8 +36,9 @@ namespace gosh {
 // kPast: kForward of y alone, in tiles of kLarge, past the caches.  (A kernel of its own: as a branch at each store it
 // cost the other calls 2 to 20 %, in registers.  kForward, with every optional output, has 112 scalar registers in lanes of
 // vector ones there, kPast 18: 131,072 x 512 -> 1024 with SiLU takes 180 us, 214 with z and 226 with a packed z.)
-enum ProductOut : int { kForward, kStore, kParts, kPast };
-constexpr bool is_forward(ProductOut out) { return out == kForward || out == kPast; }
+// kPastZ: kPast with z beside y.
+enum ProductOut : int { kForward, kStore, kParts, kPast, kPastZ };
+constexpr bool is_forward(ProductOut out) { return out == kForward || out == kPast || out == kPastZ; }
 
 struct ForwardOut {
   const float *bias;
@@ -290,8 +291,9 @@ struct Spot {
   }
 };
 
-// E entries of a row of z become entries of y; r: the residual's.  Full: all of them are there.  Past: see kPast.
-template <typename T, int E, bool Full, bool Past>
+// E entries of a row of z become entries of y; r: the residual's.  Full: all of them are there.  Past, More: see kPast; More:
+// z and y8 may be asked for.
+template <typename T, int E, bool Full, bool Past, bool More>
 __device__ __forceinline__ void put_forward(const ForwardOut &f, const Spot &at, int there, float (&v)[E],
                                             const typename Entries<T, E>::Vec &r) {
   typedef typename T::Store S;
@@ -302,9 +304,9 @@ __device__ __forceinline__ void put_forward(const ForwardOut &f, const Spot &at,
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = i < count ? v[i] : 0.f;  // entries that are not there count in no group
   }
-  if (!Past && f.z.data != nullptr) {
+  if (More && f.z.data != nullptr) {
     if (f.z_packed) store_packed<T, E>(at.in<int8_t>(f.z), at.exponent_in(f.z), count, v, head, kLanes);
-    else if (Full || count > 0) Entries<T, E>::store(at.in<S>(f.z), count, v);
+    else if (Full || count > 0) Entries<T, E>::template store<Past>(at.in<S>(f.z), count, v);
   }
   with_activation(f.act, [&](auto a) {
 #pragma unroll
@@ -314,7 +316,7 @@ __device__ __forceinline__ void put_forward(const ForwardOut &f, const Spot &at,
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] += T::up(r[i]);
   }
-  if (!Past && f.y8.data != nullptr) {
+  if (More && f.y8.data != nullptr) {
     if (!Full) {
 #pragma unroll
       for (int i = 0; i < E; ++i) v[i] = i < count ? v[i] : 0.f;
@@ -428,7 +430,7 @@ __device__ __forceinline__ void finish(const ProductArgs &g, const F16x (&acc)[R
           for (int e = 0; e < 4; ++e) v[w + e] = x[e];
         }
         if constexpr (is_forward(Out)) {
-          put_forward<T, E, kFull, Out == kPast>(g.forward, spot_of(turn), count, v, residual[turn % (kAhead + 1)]);
+          put_forward<T, E, kFull, Out == kPast || Out == kPastZ, Out != kPast>(g.forward, spot_of(turn), count, v, residual[turn % (kAhead + 1)]);
         } else if constexpr (Out == kStore) {
           if (count > 0) Entries<T, E>::store(spot_of(turn).template in<S>(g.out), count, v);
         } else {

@@ -11,7 +11,9 @@ namespace gosh {
 namespace {
 
 constexpr int kBlock = 128;   // entries that share an exponent
-constexpr int kChunk = 4096;  // entries of a workgroup
+// Entries of a workgroup, eight a thread.  2^27 entries in 8 bits: 391 us, 411 with chunks of 4,096 and 425 of 8,192; 192
+// tensors of 3,000,000 in all: 11.8, 15.4 and 16.9.
+constexpr int kChunk = 2048;
 constexpr int kThreads = 256;
 constexpr int64_t kMostEntries = int64_t{1} << 40;
 

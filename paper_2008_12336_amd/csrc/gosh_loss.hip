@@ -16,7 +16,7 @@ struct LossArgs {
   const void *targets;
   const float *weight;
   float *loss;
-  int64_t rows;
+  int64_t rows, first;  // first: of the launch
   int32_t cols, targets_are64;
   float scale;
 };
@@ -32,12 +32,13 @@ __device__ __forceinline__ float over_lanes(float v, Op op) {
 }
 
 // The loss and the gradient of a row, Lanes lanes with Count chunks of E entries each: chunk c of lane l is at (c * Lanes
-// + l) * E.
+// + l) * E.  At most one chunk of a row is there in part: it is loaded and stored by itself, once.
 template <typename T, int Lanes, int Count>
 __global__ __launch_bounds__(Lanes > 256 ? Lanes : 256) void loss_kernel(const LossArgs a) {
   constexpr int E = T::kType == GOSH_F32 ? 4 : 8;
   constexpr int kThreads = Lanes > 256 ? Lanes : 256, kRows = kThreads / Lanes, kWaves = Lanes / 64;
   typedef typename T::Store S;
+  typedef typename Entries<T, E>::Vec Vec;
   __shared__ float lds[kWaves > 1 ? 2 * kThreads / 64 : 1];
   const int lane = threadIdx.x % Lanes;
   const auto join = [&](float v, int which, auto op) {
@@ -53,73 +54,99 @@ __global__ __launch_bounds__(Lanes > 256 ? Lanes : 256) void loss_kernel(const L
     }
     return v;
   };
-  // every thread of a workgroup takes as many turns: the joins wait for each other
-  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kRows; row0 < a.rows; row0 += static_cast<int64_t>(gridDim.x) * kRows) {
-    const int64_t row = row0 + threadIdx.x / Lanes;
-    const bool there = row < a.rows;
-    int64_t target = -1;
-    float weight = 1.f;
-    if (there) {
-      target = a.targets_are64 ? static_cast<const int64_t *>(a.targets)[row] : static_cast<const int32_t *>(a.targets)[row];
-      if (a.weight != nullptr) weight = a.weight[row];
-    }
-    const S *const x = static_cast<const S *>(a.x.data) + row * a.x.ld;
-    float v[Count][E], most = -INFINITY;
-#pragma unroll
-    for (int c = 0; c < Count; ++c) {
-      const int at = (c * Lanes + lane) * E;
-      const int left = there ? a.cols - at : 0;
-      Entries<T, E>::load(x + at, left < 0 ? 0 : left, v[c]);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        v[c][e] = e < left ? v[c][e] : -INFINITY;
-        most = larger(most, v[c][e]);
-      }
-    }
-    most = join(most, 0, larger);
-    const bool nothing = target < 0 || weight == 0.f || most == -INFINITY;
-    const float from = nothing ? 0.f : most;
-    float sum = 0.f, hit = -INFINITY;  // hit: the target's logit
-#pragma unroll
-    for (int c = 0; c < Count; ++c)
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if ((c * Lanes + lane) * E + e == target) hit = v[c][e];
-        v[c][e] = __expf(v[c][e] - from);
-        sum += v[c][e];
-      }
-    sum = join(sum, 1, [](float p, float q) { return p + q; });
-    const bool wrong = target >= a.cols;
-    if (there) {
-      const float nan = __uint_as_float(0x7fc00000u);
-      const int holder = static_cast<int>(target / E % Lanes);
-      if (nothing || wrong ? lane == 0 : lane == holder)
-        a.loss[row] = nothing ? 0.f : wrong ? nan : weight * (logf(sum) + (most - hit));
-      if (a.d.data != nullptr) {
-        const float share = nothing ? 0.f : a.scale * weight / sum, whole = wrong ? nan : a.scale * weight;
-        S *const d = static_cast<S *>(a.d.data) + row * a.d.ld;
-#pragma unroll
-        for (int c = 0; c < Count; ++c) {
-          const int at = (c * Lanes + lane) * E, left = a.cols - at;
-          if (left <= 0) continue;
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            v[c][e] = nothing ? 0.f : wrong ? nan : v[c][e] * share;
-            if (at + e == target) v[c][e] -= nothing ? 0.f : whole;
-          }
-          Entries<T, E>::store(d + at, left, v[c]);
-        }
-      }
-    }
+  const int64_t row = a.first + static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / Lanes;
+  const bool there = row < a.rows;
+  int64_t target = -1;
+  float weight = 1.f;
+  if (there) {
+    target = a.targets_are64 ? static_cast<const int64_t *>(a.targets)[row] : static_cast<const int32_t *>(a.targets)[row];
+    if (a.weight != nullptr) weight = a.weight[row];
   }
+  const bool wrong = target >= a.cols;
+  const S *const x = static_cast<const S *>(a.x.data) + row * a.x.ld;
+  const int whole_chunks = a.cols / E, over = a.cols % E;
+  const int part_count = whole_chunks / Lanes;  // which of a lane's chunks is the one that is there in part, if it is its own
+  const bool part = there && over != 0 && lane == whole_chunks % Lanes;
+  Vec raw[Count], rest = 0;
+#pragma unroll
+  for (int c = 0; c < Count; ++c) {
+    raw[c] = 0;
+    if (there && c * Lanes + lane < whole_chunks) raw[c] = Entries<T, E>::fetch(x + (c * Lanes + lane) * E, E);
+  }
+  if (part) rest = Entries<T, E>::fetch(x + whole_chunks * E, over);
+  // the target's logit: a load of its own is cheaper than to compare every column
+  const float hit = target < 0 || wrong ? 0.f : T::up(x[target]);
+  float v[Count][E], most = -INFINITY;
+#pragma unroll
+  for (int c = 0; c < Count; ++c) {
+    const bool mine = part && c == part_count, none = !mine && c * Lanes + lane >= whole_chunks;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[c][e] = T::up(raw[c][e]);
+    if (mine) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[c][e] = e < over ? T::up(rest[e]) : -INFINITY;
+    }
+    if (none) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[c][e] = -INFINITY;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) most = larger(most, v[c][e]);
+  }
+  most = join(most, 0, larger);
+  const bool nothing = target < 0 || weight == 0.f || most == -INFINITY;
+  const float from = nothing ? 0.f : most;
+  float sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < Count; ++c)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      v[c][e] = __expf(v[c][e] - from);
+      sum += v[c][e];
+    }
+  sum = join(sum, 1, [](float p, float q) { return p + q; });
+  if (!there) return;
+  const float nan = __uint_as_float(0x7fc00000u);
+  if (lane == 0) a.loss[row] = nothing ? 0.f : wrong ? nan : weight * (logf(sum) + (most - hit));
+  if (a.d.data == nullptr) return;
+  const float whole = a.scale * weight, share = wrong ? nan : whole / sum;
+  S *const d = static_cast<S *>(a.d.data) + row * a.d.ld;
+  float last[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) last[e] = 0.f;
+#pragma unroll
+  for (int c = 0; c < Count; ++c) {
+    const int at = (c * Lanes + lane) * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[c][e] *= share;
+    const int here = static_cast<int>(target) - at;  // a target past the columns has NaN everywhere
+    if (static_cast<unsigned>(here) < static_cast<unsigned>(E)) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[c][e] -= e == here ? whole : 0.f;
+    }
+    if (nothing) {  // whatever the row holds, NaN also
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[c][e] = 0.f;
+    }
+    if (c == part_count) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) last[e] = v[c][e];
+    }
+    if (c * Lanes + lane < whole_chunks) Entries<T, E>::store(d + at, E, v[c]);
+  }
+  if (part) Entries<T, E>::store(d + whole_chunks * E, over, last);
 }
 
 template <typename T, int Lanes, int Count>
-int launch_loss(const LossArgs &a, hipStream_t st) {
+int launch_loss(LossArgs a, hipStream_t st) {
   constexpr int kThreads = Lanes > 256 ? Lanes : 256, kRows = kThreads / Lanes;
-  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(ceil_div(a.rows, kRows), int64_t{1} << 20));
-  loss_kernel<T, Lanes, Count><<<dim3(blocks), dim3(kThreads), 0, st>>>(a);
-  return check_launch("softmax loss");
+  constexpr int64_t kBlocks = int64_t{1} << 20;  // a grid's threads stay below 2^31
+  for (a.first = 0; a.first < a.rows; a.first += kBlocks * kRows) {
+    const unsigned blocks = static_cast<unsigned>(std::min(ceil_div(a.rows - a.first, kRows), kBlocks));
+    loss_kernel<T, Lanes, Count><<<dim3(blocks), dim3(kThreads), 0, st>>>(a);
+    if (int rc = check_launch("softmax loss")) return rc;
+  }
+  return GOSH_OK;
 }
 
 template <typename T>
@@ -128,17 +155,24 @@ int loss_of(const LossArgs &a, hipStream_t st) {
   const int64_t chunks = ceil_div(a.cols, E);
   if (chunks <= 4) return launch_loss<T, 4, 1>(a, st);
   if (chunks <= 8) return launch_loss<T, 8, 1>(a, st);
-  if (chunks <= 16) return launch_loss<T, 16, 1>(a, st);
+  if (chunks <= 16) return launch_loss<T, 8, 2>(a, st);
   if (chunks <= 32) return launch_loss<T, 16, 2>(a, st);
   if (chunks <= 64) return launch_loss<T, 32, 2>(a, st);
   if (chunks <= 128) return launch_loss<T, 64, 2>(a, st);
   if (chunks <= 256) return launch_loss<T, 64, 4>(a, st);
   if (chunks <= 512) return launch_loss<T, 256, 2>(a, st);
+  if (chunks <= 768) return launch_loss<T, 256, 3>(a, st);
   if (chunks <= 1024) return launch_loss<T, 256, 4>(a, st);
+  if (chunks <= 1536) return launch_loss<T, 512, 3>(a, st);
   if (chunks <= 2048) return launch_loss<T, 512, 4>(a, st);
+  if (chunks <= 3072) return launch_loss<T, 1024, 3>(a, st);
   if (chunks <= 4096) return launch_loss<T, 1024, 4>(a, st);
+  if (chunks <= 6144) return launch_loss<T, 1024, 6>(a, st);
   if (chunks <= 8192) return launch_loss<T, 1024, 8>(a, st);
-  if constexpr (T::kType == GOSH_F32) return launch_loss<T, 1024, 16>(a, st);
+  if constexpr (T::kType == GOSH_F32) {
+    if (chunks <= 12288) return launch_loss<T, 1024, 12>(a, st);
+    return launch_loss<T, 1024, 16>(a, st);
+  }
   return fail(GOSH_EINVAL, "logits: cols = %d: too many", a.cols);
 }
 
@@ -164,7 +198,7 @@ int gosh_softmax_loss(const gosh_mat *logits, const void *targets, int32_t targe
   if (int rc = check_floats(weight, rows, "weight", true)) return rc;
   if (int rc = check_floats(loss, rows, "loss", false)) return rc;
   if (rows == 0) return GOSH_OK;
-  LossArgs a{plane_of(logits), plane_of(dlogits), targets, weight, loss, rows, logits->cols, targets_are64, scale};
+  LossArgs a{plane_of(logits), plane_of(dlogits), targets, weight, loss, rows, 0, logits->cols, targets_are64, scale};
   hipStream_t st = as_stream(hip_stream);
   if (logits->type == GOSH_F32) return loss_of<F32>(a, st);
   if (logits->type == GOSH_BF16) return loss_of<Bf16>(a, st);

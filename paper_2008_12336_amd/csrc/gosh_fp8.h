@@ -32,7 +32,15 @@ struct Fp8Args {
   Plane pack;      // a few rows: x of pack_type and pack_cols columns that is put into 8 bits first, or null
   int32_t pack_type, pack_cols;
   int32_t exact;   // kForward in bf16: see fp8_mma
+  uint32_t by_all, by_group;  // reciprocals of the tiles of a split and of a group: set_reciprocals
 };
+
+constexpr int kTileGroup = 8;  // rows of tiles, see fp8_place
+inline uint32_t reciprocal_of(int64_t d) { return d <= 1 ? 0xffffffffu : static_cast<uint32_t>(((int64_t{1} << 32) + d - 1) / d); }
+inline void set_reciprocals(Fp8Args &a) {
+  a.by_all = reciprocal_of(static_cast<int64_t>(a.g.tiles_m) * a.g.tiles_n);
+  a.by_group = reciprocal_of(static_cast<int64_t>(kTileGroup) * a.g.tiles_n);
+}
 
 // Defined in gosh_fp8_{f32,bf16,f16}.hip, by the type of the results; kParts: F32 for sums that stay in 32 bits, Bf16 for
 // those that are rounded to bf16.

@@ -324,6 +324,7 @@ int product_of_rows_fp8(int32_t type, ProductOut out, Fp8Args a, int64_t rows, h
   for (int64_t r = 0; r < rows; r += rows_per_launch) {
     a.g.M = std::min(rows_per_launch, rows - r);
     a.g.tiles_m = static_cast<int32_t>(ceil_div(a.g.M, tile));
+    set_reciprocals(a);
     a.x.data = all.x.data + r * all.x.ld;
     a.x.exps = all.x.exps + (r >> all.x.shift) * all.x.ld_exps;
     a.g.out = rows_of(all.g.out, r, type, false);
@@ -548,6 +549,7 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
       a.g.splits = p.dw.splits;
       a.g.k_per_split = p.dw.blocks_per_split;
       a.g.parts = dw_parts;
+      set_reciprocals(a);
       if (int rc = dw->type == GOSH_BF16 ? launch_fp8<Bf16>(kParts, a, st) : launch_fp8<F32>(kParts, a, st)) return rc;
     }
     const int64_t n = static_cast<int64_t>(out) * in;

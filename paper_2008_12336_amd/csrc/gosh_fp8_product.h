@@ -187,17 +187,29 @@ struct Fp8Units {
   }
 };
 
+// n / d, and what is left, by d's reciprocal from the host: ceil(2^32 / d), or 2^32 - 1.  n < 2^31.
+__device__ __forceinline__ int divided(int n, int d, uint32_t reciprocal, int *rest) {
+  int q = static_cast<int>(__umulhi(static_cast<uint32_t>(n), reciprocal));  // right, or 1 too much; for d = 1 also 1 less
+  int r = n - q * d;
+  if (r < 0) --q, r += d;
+  if (r >= d) ++q, r -= d;
+  *rest = r;
+  return q;
+}
+
 // The id-th tile: of eight rows of tiles those of one column after each other, then the next column's, so that the 32 CUs
 // of an XCD, which work on 32 tiles in a row, share eight tiles of A and four of B: of 131,072 x 1024 -> 4096 those of B alone, 4
 // MB, fill an L2, and with row after row they were fetched again and again (727 -> 697 us).
-__device__ __forceinline__ Place fp8_place(const ProductArgs &g, int id, int bm, int bn) {
-  constexpr int kGroup = 8;
-  const int all = g.tiles_m * g.tiles_n, split = id / all, rest = id % all;
-  const int first = rest / (kGroup * g.tiles_n) * kGroup, tall = g.tiles_m - first < kGroup ? g.tiles_m - first : kGroup;
-  const int in = rest - first * g.tiles_n;
+__device__ __forceinline__ Place fp8_place(const Fp8Args &a, int id, int bm, int bn) {
+  const ProductArgs &g = a.g;
+  const int all = g.tiles_m * g.tiles_n;
+  int rest = id, split = 0, in;
+  if (g.splits > 1) split = divided(id, all, a.by_all, &rest);
+  const int first = divided(rest, kTileGroup * g.tiles_n, a.by_group, &in) * kTileGroup;
+  const int tall = g.tiles_m - first < kTileGroup ? g.tiles_m - first : kTileGroup;
+  const int tn = tall == kTileGroup ? in / kTileGroup : in / tall, tm = first + in - tn * tall;
   const int64_t k0 = split * g.k_per_split;
-  return {static_cast<int64_t>(first + in % tall) * bm, static_cast<int64_t>(in / tall) * bn, k0,
-          k0 + g.k_per_split < g.K ? k0 + g.k_per_split : g.K, split};
+  return {static_cast<int64_t>(tm) * bm, static_cast<int64_t>(tn) * bn, k0, k0 + g.k_per_split < g.K ? k0 + g.k_per_split : g.K, split};
 }
 
 // Two tiles in LDS: while a step is multiplied the next one's loads are under way, also across the end of a tile: a workgroup
@@ -231,8 +243,9 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
   b.init(args.w);
   uint32_t into = base;
   int turn = turns.id, to_go;
+  Place from;  // of the tile that is being loaded
   const auto begin = [&]() {
-    const Place from = fp8_place(g, turn, BM, BN);
+    from = fp8_place(args, turn, BM, BN);
     a.begin(args.x, from.m0, g.M, g.K, from.k0);
     b.begin(args.w, from.n0, g.N, g.K, from.k0);
     units.begin(args, from.m0, from.n0, from.k0);
@@ -257,6 +270,14 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
   begin();
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) load(i);
+  float bias[RN];
+  load_bias<RN, Out>(g, from.n0 + wn, bias);
+  bool ahead = to_go > 1;  // two steps are under way before the first
+  if (ahead) {
+    advance();
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(i);
+  }
 
   const uint16_t *now = lds;
   U4 fa[2][2], fb[2][RN][2];  // 32 rows by 64 k: the ones in work and the next
@@ -279,21 +300,25 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
 #pragma unroll
     for (int j = 0; j < RN; ++j) w[j] = e[BM + wn + 32 * j + (lane & 31)];
   };
-  float bias[RN];
-  load_bias<RN, Out>(g, fp8_place(g, turns.id, BM, BN).n0 + wn, bias);
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  if (ahead) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(kLoads) : "memory");
+  else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
   take_units(ea[0], eb[0]);
   take_b(0);
   take_a(0, 0, 0);
   for (int id = turns.id; id < turns.end; id += turns.step) {
-    const Place at = fp8_place(g, id, BM, BN);
+    const Place at = from;
     const int steps = static_cast<int>(at.k1 - at.k0);
     F16x acc[RM][RN];
     start<RM, RN>(bias, acc);
-    if (is_forward(Out) && id + turns.step < turns.end)
-      load_bias<RN, Out>(g, fp8_place(g, id + turns.step, BM, BN).n0 + wn, bias);
     for (int s = 0; s < steps; ++s) {
-      advance();  // before the products: the compiler would move them behind its branches
+      // before the products: the compiler would move them behind the branches
+      if (!ahead) {
+        advance();
+        if (is_forward(Out) && s + 1 == steps) load_bias<RN, Out>(g, from.n0 + wn, bias);  // the next tile's, or this one's again
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load(i);
+      }
+      ahead = false;
       const int shift = (static_cast<int>(at.k0) + s & 3) * 8;
 #pragma unroll
       for (int i = 0; i < RM; ++i) ea[1][i] = ea[0][i] >> shift & 255u;
@@ -308,10 +333,6 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
       for (int t = 0; t + 1 < kTurns; ++t) {
         if (t + 1 == RM) take_b(1);
         take_a((t + 1) & 1, (t + 1) % RM, (t + 1) / RM);
-        if (t == 0) {  // all at once: spread over the turns the last ones arrive late (716 -> 727 us)
-#pragma unroll
-          for (int i = 0; i < kLoads; ++i) load(i);
-        }
         __builtin_amdgcn_sched_barrier(0);
         multiply(t & 1, t % RM, t / RM);
         __builtin_amdgcn_sched_barrier(0);

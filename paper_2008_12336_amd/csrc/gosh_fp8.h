@@ -28,12 +28,15 @@ inline Fp8Plane fp8_plane(const gosh_fp8 *m) {
 struct Fp8Args {
   Fp8Plane x, w;   // A (M rows), B (N rows)
   ProductArgs g;   // M, N, tiles, splits and where the results go; K and k_per_split count blocks
-  int32_t tile;    // side of a tile: 64, 128 or 256; or 32: a few rows of kForward
-  Plane pack;      // a few rows: x of pack_type and pack_cols columns that is put into 8 bits first, or null
+  int32_t tile;    // side of a tile: 64, 128 or 256; or 32: few results (not for kParts)
+  Plane pack;      // up to 32 rows of kForward: x of pack_type and pack_cols columns that is put into 8 bits first, or null
   int32_t pack_type, pack_cols;
   int32_t exact;   // kForward in bf16: see fp8_mma
   uint32_t by_all, by_group;  // reciprocals of the tiles of a split and of a group: set_reciprocals
 };
+
+// Wavefronts that share the blocks of k of few results.
+inline int few_waves(int64_t blocks) { return blocks <= 8 ? 4 : 16; }
 
 constexpr int kTileGroup = 8;  // rows of tiles, see fp8_place
 inline uint32_t reciprocal_of(int64_t d) { return d <= 1 ? 0xffffffffu : static_cast<uint32_t>(((int64_t{1} << 32) + d - 1) / d); }

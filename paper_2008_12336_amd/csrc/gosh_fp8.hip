@@ -2,6 +2,7 @@
 #include "gosh_fp8.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace gosh {
 
@@ -298,24 +299,35 @@ constexpr int64_t kTilesPerLaunch = int64_t{1} << 22;
 // 131,072 x 1024 -> 4096 (1.07 GB): 727 us, 643 with it.
 constexpr int64_t kPastCaches = int64_t{256} << 20;
 
-constexpr int64_t kFewRows = 32;
+constexpr int64_t kFewRows = 32;  // that are put into 8 bits in the product's launch
 
-// The side of the tiles of a product of which the busiest of the device's 256 CUs has the least work.
-int fp8_tiles_for(ProductOut out, int64_t M, int64_t N) {
-  if (out == kForward && M <= kFewRows) return 32;
-  int best = 64;
+// The us that a product takes by its tiles, from what it took here (bf16 results with GELU, in a graph; us with few, 64, 128 and 256:
+// 64 x 4096 -> 4096: 13.9, 18.4, 25.5, 50.2; 512 x 256 -> 1024: 5.3, 6.0, 7.4, 13.2; 4096 x 2048 -> 256: 24.4, 12.0, 15.5, 30.1;
+// 8192 x 512 -> 512: 21.8, 14.0, 9.6, 17.2; 131,072 x 128 -> 128: 33.5, 35.5, 17.6, 32.5; 65,536 x 512 -> 512: 124, 89, 40.7, 34.6).
+// A CU works on four tiles of 64 together, two of 128 or one of 256; each has its way out, and steps that are as long as a load
+// is under way where it is alone.
+double fp8_time(int tile, int64_t tiles, int64_t blocks) {
+  const double k = static_cast<double>(blocks), per_cu = static_cast<double>(ceil_div(tiles, 256));
+  if (tile == 32) return few_waves(blocks) == 4 ? 4.0 + per_cu * (0.5 + 0.12 * k) : 3.7 + per_cu * 0.32 * k;
+  const double held = tile == 256 ? 1 : tile == 128 ? 2 : 4, together = std::min(per_cu, held), turns = std::ceil(per_cu / held);
+  if (tile == 256) return 2.0 + turns * (10.0 + 1.2 * k);
+  if (tile == 128) return 2.0 + turns * (4.5 + 0.75 * together + k * (together > 1 ? 0.95 : 0.6));
+  return 1.5 + turns * (2.0 + 1.25 * together + k * (0.22 + 0.2 * together));
+}
+int fp8_tile_for(int64_t M, int64_t N, int64_t blocks, bool few) {
+  int best = 0;
   double least = 0;
-  for (int s : {64, 128, 256}) {
-    const double turns = static_cast<double>(ceil_div(ceil_div(M, s) * ceil_div(N, s), 256));
-    const double work = turns * s * s * (s == 256 ? 1.0 : s == 128 ? 1.2 : 2.6);
-    if (s == 64 || work <= least) best = s, least = work;
+  for (int s : {256, 128, 64, 32}) {
+    if (s == 32 && (!few || M > 65535 * 32)) continue;
+    const double time = fp8_time(s, ceil_div(M, s) * ceil_div(N, s), blocks);
+    if (best == 0 || time < least) best = s, least = time;
   }
   return best;
 }
 
 // All rows of A, as many to a launch as a grid takes.
 int product_of_rows_fp8(int32_t type, ProductOut out, Fp8Args a, int64_t rows, hipStream_t st) {
-  const int tile = a.tile = fp8_tiles_for(out, rows, a.g.N);
+  const int tile = a.tile = a.pack.data != nullptr ? 32 : fp8_tile_for(rows, a.g.N, a.g.K, true);
   a.g.tiles_n = static_cast<int32_t>(ceil_div(a.g.N, tile));
   a.g.splits = std::max(a.g.splits, 1);
   a.g.k_per_split = ceil_div(a.g.K, a.g.splits);
@@ -338,7 +350,7 @@ int product_of_rows_fp8(int32_t type, ProductOut out, Fp8Args a, int64_t rows, h
 
 uint64_t round_up(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// How dw is split along the rows.
+// How dw is split along the rows: the parts are written and read again, at 5 TB/s.  Few results (32) are not.
 struct Fp8DwPlan {
   int32_t tile, tiles_m, tiles_n, splits;
   int64_t blocks_per_split;
@@ -347,18 +359,16 @@ Fp8DwPlan plan_dw_fp8(int64_t rows, int32_t in, int32_t out) {
   Fp8DwPlan best{};
   double least = 0;
   const int64_t blocks = ceil_div(rows, kFp8Block);
-  for (int s : {64, 128, 256}) {
-    Fp8DwPlan p;
-    p.tile = s;
-    p.tiles_m = static_cast<int32_t>(ceil_div(out, s));
-    p.tiles_n = static_cast<int32_t>(ceil_div(in, s));
-    const int64_t tiles = static_cast<int64_t>(p.tiles_m) * p.tiles_n;
-    const int64_t want = std::max<int64_t>(1, std::min(blocks / 4, (s == 256 ? 256 : 512) / tiles));
-    p.blocks_per_split = std::max<int64_t>(1, ceil_div(blocks, want));
-    p.splits = static_cast<int32_t>(ceil_div(blocks, p.blocks_per_split));
-    // of the busiest CU
-    const double work = static_cast<double>(ceil_div(tiles * p.splits, 256)) * s * s * (s == 256 ? 1.0 : s == 128 ? 1.2 : 2.6) * p.blocks_per_split;
-    if (s == 64 || work <= least) best = p, least = work;
+  for (int s : {256, 128, 64, 32}) {
+    const int64_t tiles_m = ceil_div(out, s), tiles_n = ceil_div(in, s), tiles = tiles_m * tiles_n;
+    for (int64_t want = 1; want <= (s == 32 ? 1 : std::min<int64_t>(std::max<int64_t>(blocks, 1), 1024)); want *= 2) {
+      const int64_t per = std::max<int64_t>(1, ceil_div(blocks, want)), splits = ceil_div(blocks, per);
+      if (want > 1 && tiles * splits > 2048) break;
+      const double time = fp8_time(s, tiles * splits, per) + (s == 32 ? 0 : 2.5 + 1.6e-6 * static_cast<double>(splits) * in * out);
+      if (best.tile != 0 && time >= least) continue;
+      least = time;
+      best = Fp8DwPlan{s, static_cast<int32_t>(tiles_m), static_cast<int32_t>(tiles_n), static_cast<int32_t>(splits), per};
+    }
   }
   return best;
 }
@@ -386,7 +396,7 @@ Fp8BackwardPlan plan_backward_fp8(int64_t rows, int32_t in, int32_t out) {
   p.qt = take(static_cast<uint64_t>(out) * p.ld_t);
   p.exps_t = take(static_cast<uint64_t>(out) * p.ld_exps_t);
   p.sums = take(static_cast<uint64_t>(blocks_t) * out * 4);
-  p.dw_parts = take(static_cast<uint64_t>(p.dw.splits) * in * out * 4);
+  p.dw_parts = take(p.dw.tile == 32 ? 0 : static_cast<uint64_t>(p.dw.splits) * in * out * 4);
   p.bytes = at;
   return p;
 }
@@ -535,23 +545,28 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
     a.g.out = plane_of(dx);
     if (int rc = product_of_rows_fp8(dx->type, kStore, a, rows, st)) return rc;
   }
-  if (dw != nullptr) {
-    if (rows > 0) {
-      Fp8Args a{};
-      a.x = Fp8Plane{ws + p.qt, ws + p.exps_t, p.ld_t, p.ld_exps_t, 0};
-      a.w = fp8_plane(xt);
-      a.g.M = out;
-      a.g.N = in;
-      a.g.K = ceil_div(rows, kFp8Block);
-      a.tile = p.dw.tile;
-      a.g.tiles_m = p.dw.tiles_m;
-      a.g.tiles_n = p.dw.tiles_n;
-      a.g.splits = p.dw.splits;
-      a.g.k_per_split = p.dw.blocks_per_split;
-      a.g.parts = dw_parts;
-      set_reciprocals(a);
-      if (int rc = dw->type == GOSH_BF16 ? launch_fp8<Bf16>(kParts, a, st) : launch_fp8<F32>(kParts, a, st)) return rc;
-    }
+  const bool few = rows > 0 && p.dw.tile == 32;
+  if (dw != nullptr && rows > 0) {
+    Fp8Args a{};
+    a.x = Fp8Plane{ws + p.qt, ws + p.exps_t, p.ld_t, p.ld_exps_t, 0};
+    a.w = fp8_plane(xt);
+    a.tile = p.dw.tile;
+    a.g.M = out;
+    a.g.N = in;
+    a.g.K = ceil_div(rows, kFp8Block);
+    a.g.tiles_m = p.dw.tiles_m;
+    a.g.tiles_n = p.dw.tiles_n;
+    a.g.splits = p.dw.splits;
+    a.g.k_per_split = p.dw.blocks_per_split;
+    a.g.out = plane_of(dw);
+    a.g.parts = dw_parts;
+    set_reciprocals(a);
+    // parts are in 32 bits: here the type says by which products
+    if (int rc = few ? product_fp8(dw->type, kStore, a, st)
+                     : dw->type == GOSH_BF16 ? launch_fp8<Bf16>(kParts, a, st) : launch_fp8<F32>(kParts, a, st))
+      return rc;
+  }
+  if (dw != nullptr && !few) {
     const int64_t n = static_cast<int64_t>(out) * in;
     jobs[joins++] = {dw_parts, n, n, dw->ld, dw->data, rows > 0 ? p.dw.splits : 0, in, dw->type};
   }

@@ -6,7 +6,7 @@
 
 namespace gosh {
 
-// ---- a few rows: the wavefronts of a workgroup share the blocks of k of 32 x 32 results -----------------
+// ---- few results: the wavefronts of a workgroup share the blocks of k of 32 x 32 of them -----------------
 
 // The rows of a tile that a lane reads; rows past the end read the last one's, for results that nobody stores.
 struct Fp8Lane {
@@ -62,24 +62,27 @@ __device__ __forceinline__ uint32_t pack_block(const Fp8Args &a, int64_t row, in
   return byte;
 }
 
-// X: the type of the x that is put into 8 bits, or void.
-template <typename T, typename X, bool Exact, int Waves>
-__global__ __launch_bounds__(64 * Waves) void fp8_few_rows_kernel(const Fp8Args a) {
+// A product of few results has few tiles, whose blocks of k one after the other are a chain of waits for memory: here four or 16
+// wavefronts have a block each at a time, loaded by themselves.  (A training step of 512 x 256 -> 1024, products in tiles of 64 x
+// 64: forward 7.8 us, dx 6.8, dw 5.4.)
+// X: the type of the x, up to 32 rows, that is put into 8 bits on the way; or void.
+template <typename T, typename X, bool Exact, int Waves, ProductOut Out>
+__global__ __launch_bounds__(64 * Waves) void fp8_few_kernel(const Fp8Args a) {
   __shared__ __attribute__((aligned(16))) float lds[Waves - 1][16][64];
   __shared__ __attribute__((aligned(16))) float slab[Slab<32>::kFloats];
   const ProductArgs &g = a.g;
-  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 32;
+  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 32, m0 = static_cast<int64_t>(blockIdx.y) * 32;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const Fp8Lane w(a.w, n0 + (lane & 31), g.N);
+  const Fp8Lane x(a.x, m0 + (lane & 31), g.M), w(a.w, n0 + (lane & 31), g.N);
   F16x acc[1][1];
   float bias[1] = {0.f};
-  if (wave == 0) load_bias<1, kForward>(g, n0, bias);
+  if (wave == 0) load_bias<1, Out>(g, n0, bias);
   start<1, 1>(bias, acc);
   for (int64_t k = wave; k < g.K; k += Waves) {
     U4 qa[2][2], qb[2][2];
     const uint32_t ub = w.load(k, qb);
     uint32_t ua;
-    if constexpr (std::is_void<X>::value) ua = Fp8Lane(a.x, lane & 31, g.M).load(k, qa);
+    if constexpr (std::is_void<X>::value) ua = x.load(k, qa);
     else ua = pack_block<X>(a, lane & 31, k, blockIdx.x == 0, qa);
 #pragma unroll
     for (int h = 0; h < 2; ++h) acc[0][0] = fp8_mma<Exact>(qa[h], qb[h], ua, ub, acc[0][0]);
@@ -94,22 +97,24 @@ __global__ __launch_bounds__(64 * Waves) void fp8_few_rows_kernel(const Fp8Args 
   for (int s = 0; s < Waves - 1; ++s)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[0][0][i] += lds[s][i][lane];
-  finish<T, 1, 1, kForward>(g, acc, slab, 0, n0, 0);
+  finish<T, 1, 1, Out>(g, acc, slab, m0, n0, 0);
 }
 
-template <typename T, typename X, bool Exact>
-int launch_fp8_few_rows(const Fp8Args &a, hipStream_t st) {
-  const dim3 grid(static_cast<unsigned>(ceil_div(a.g.N, 32)));
-  if (a.g.K <= 8) fp8_few_rows_kernel<T, X, Exact, 4><<<grid, dim3(256), 0, st>>>(a);
-  else fp8_few_rows_kernel<T, X, Exact, 16><<<grid, dim3(1024), 0, st>>>(a);
-  return check_launch("product of a few rows in 8-bit floating point");
+template <typename T, typename X, bool Exact, ProductOut Out>
+int launch_fp8_few(const Fp8Args &a, hipStream_t st) {
+  const dim3 grid(static_cast<unsigned>(ceil_div(a.g.N, 32)), static_cast<unsigned>(ceil_div(a.g.M, 32)));
+  if (few_waves(a.g.K) == 4) fp8_few_kernel<T, X, Exact, 4, Out><<<grid, dim3(256), 0, st>>>(a);
+  else fp8_few_kernel<T, X, Exact, 16, Out><<<grid, dim3(1024), 0, st>>>(a);
+  return check_launch("product of few results in 8-bit floating point");
 }
-template <typename T, bool Exact>
-int launch_fp8_few_rows(const Fp8Args &a, hipStream_t st) {
-  if (a.pack.data == nullptr) return launch_fp8_few_rows<T, void, Exact>(a, st);
-  if (a.pack_type == GOSH_F32) return launch_fp8_few_rows<T, F32, Exact>(a, st);
-  if (a.pack_type == GOSH_BF16) return launch_fp8_few_rows<T, Bf16, Exact>(a, st);
-  return launch_fp8_few_rows<T, F16, Exact>(a, st);
+template <typename T, bool Exact, ProductOut Out>
+int launch_fp8_few(const Fp8Args &a, hipStream_t st) {
+  if constexpr (Out == kForward) {
+    if (a.pack.data != nullptr && a.pack_type == GOSH_F32) return launch_fp8_few<T, F32, Exact, Out>(a, st);
+    if (a.pack.data != nullptr && a.pack_type == GOSH_BF16) return launch_fp8_few<T, Bf16, Exact, Out>(a, st);
+    if (a.pack.data != nullptr) return launch_fp8_few<T, F16, Exact, Out>(a, st);
+  }
+  return launch_fp8_few<T, void, Exact, Out>(a, st);
 }
 
 // ---- many tiles: straight to LDS ------------------------------------------------------------------------
@@ -374,8 +379,8 @@ int launch_fp8_out(const Fp8Args &a, hipStream_t st) {
     case 128: return launch_fp8_tiles<T, kMiddle, Exact, Out>(a, st);
     default: break;
   }
-  if constexpr (Out == kForward)
-    if (a.tile == 32) return launch_fp8_few_rows<T, Exact>(a, st);
+  if constexpr (Out != kParts)
+    if (a.tile == 32) return launch_fp8_few<T, Exact, Out>(a, st);
   return launch_fp8_tiles<T, kSmall, Exact, Out>(a, st);
 }
 

@@ -766,6 +766,9 @@ def gosh_linear_backward(dy: torch.Tensor, x, w, z, act: int = GOSH_ACT_NONE, dx
 # ---- the head in 8-bit floating point --------------------------------------------------------
 
 
+_E4M3, _U8 = torch.float8_e4m3fn, torch.uint8
+
+
 class PackedFp8:
     """A rows x cols matrix in 8-bit floating point: e4m3 entries `q` (rows padded to 128, which the library's calls write as
     zeros) and exponent bytes `exps`, one for each 128 columns of a row or, with block_rows = 128, of 128 rows.  Zeros at
@@ -787,9 +790,9 @@ class PackedFp8:
 
     def _fp8(self, name: str) -> gosh_fp8:
         q, exps, rows, cols = self.q, self.exps, self.rows, self.cols
-        if q.dtype != torch.float8_e4m3fn or exps.dtype != torch.uint8:
+        if q.dtype is not _E4M3 or exps.dtype is not _U8:
             raise TypeError(f"{name}: q must be float8_e4m3fn and exps uint8")
-        blocks, wide, long = -(-rows // self.block_rows), -(-cols // 128) * 128, -(-cols // 512) * 4
+        blocks, wide, long = -(-rows // self.block_rows), (cols + 127) & -128, (cols + 511) // 512 * 4
         ld, ld_exps = _rows_apart(q, rows, wide), _rows_apart(exps, blocks, long)
         if ld is None or ld_exps is None:
             raise TypeError(f"{name}: q must have {rows} rows of at least {wide} contiguous entries, exps {blocks} of {long}")

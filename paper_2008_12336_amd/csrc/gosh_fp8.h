@@ -56,6 +56,16 @@ int launch_fp8<Bf16>(ProductOut, const Fp8Args &, hipStream_t);
 template <>
 int launch_fp8<F16>(ProductOut, const Fp8Args &, hipStream_t);
 
+// dx and dw, both of few results (dx may have none: tiles_m = 0), and db's sum (or none: n = 0) in one launch.
+template <typename T>
+int launch_fp8_gradients(const Fp8Args &dx, const Fp8Args &dw, int32_t dw_type, const JoinJob &db, hipStream_t st);
+template <>
+int launch_fp8_gradients<F32>(const Fp8Args &, const Fp8Args &, int32_t, const JoinJob &, hipStream_t);
+template <>
+int launch_fp8_gradients<Bf16>(const Fp8Args &, const Fp8Args &, int32_t, const JoinJob &, hipStream_t);
+template <>
+int launch_fp8_gradients<F16>(const Fp8Args &, const Fp8Args &, int32_t, const JoinJob &, hipStream_t);
+
 // ---- device -------------------------------------------------------------------------------------
 
 // The exponent byte of a block whose largest finite magnitude, f * 2^E with f in [1, 2), has the bits `most`: 448 is 1.75 *

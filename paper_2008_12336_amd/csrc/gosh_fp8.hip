@@ -521,8 +521,6 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
   hipStream_t st = as_stream(hip_stream);
   uint8_t *const ws = static_cast<uint8_t *>(workspace);
   float *const sums = reinterpret_cast<float *>(ws + p.sums), *const dw_parts = reinterpret_cast<float *>(ws + p.dw_parts);
-  JoinJob jobs[3];
-  int joins = 0;
   if (rows > 0) {
     PackArgs a{};
     a.x = plane_of(dy);
@@ -536,41 +534,56 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
     a.z_packed = act != GOSH_ACT_NONE && z->packed;
     if (int rc = pack_fp8(dy->type, a, false, true, st)) return rc;
   }
-  if (dx != nullptr && rows > 0) {
-    Fp8Args a{};
-    a.x = Fp8Plane{ws + p.q, ws + p.exps, p.ld, p.ld_exps, 0};
-    a.w = fp8_plane(wt);
-    a.g.N = in;
-    a.g.K = ceil_div(out, kFp8Block);
-    a.g.out = plane_of(dx);
-    if (int rc = product_of_rows_fp8(dx->type, kStore, a, rows, st)) return rc;
+  Fp8Args gx{}, gw{};
+  if (dx != nullptr) {
+    gx.x = Fp8Plane{ws + p.q, ws + p.exps, p.ld, p.ld_exps, 0};
+    gx.w = fp8_plane(wt);
+    gx.g.N = in;
+    gx.g.K = ceil_div(out, kFp8Block);
+    gx.g.out = plane_of(dx);
   }
-  const bool few = rows > 0 && p.dw.tile == 32;
+  if (dw != nullptr) {
+    gw.x = Fp8Plane{ws + p.qt, ws + p.exps_t, p.ld_t, p.ld_exps_t, 0};
+    gw.w = fp8_plane(xt);
+    gw.tile = p.dw.tile;
+    gw.g.M = out;
+    gw.g.N = in;
+    gw.g.K = ceil_div(rows, kFp8Block);
+    gw.g.tiles_m = p.dw.tiles_m;
+    gw.g.tiles_n = p.dw.tiles_n;
+    gw.g.splits = p.dw.splits;
+    gw.g.k_per_split = p.dw.blocks_per_split;
+    gw.g.out = plane_of(dw);
+    gw.g.parts = dw_parts;
+    set_reciprocals(gw);
+  }
+  const JoinJob db_job{sums, out, db != nullptr ? out : 0, out, db, static_cast<int32_t>(ceil_div(rows, kFp8Block)), out, GOSH_F32};
+  const bool few = rows > 0 && dw != nullptr && p.dw.tile == 32;
+  if (few && (dx == nullptr || fp8_tile_for(rows, in, gx.g.K, true) == 32)) {
+    if (dx != nullptr) {
+      gx.g.M = rows;
+      gx.g.tiles_m = static_cast<int32_t>(ceil_div(rows, 32));
+      gx.g.tiles_n = static_cast<int32_t>(ceil_div(in, 32));
+    }
+    if (dy->type == GOSH_F32) return launch_fp8_gradients<F32>(gx, gw, dw->type, db_job, st);
+    if (dy->type == GOSH_BF16) return launch_fp8_gradients<Bf16>(gx, gw, dw->type, db_job, st);
+    return launch_fp8_gradients<F16>(gx, gw, dw->type, db_job, st);
+  }
+  if (dx != nullptr && rows > 0)
+    if (int rc = product_of_rows_fp8(dx->type, kStore, gx, rows, st)) return rc;
+  JoinJob jobs[3];
+  int joins = 0;
   if (dw != nullptr && rows > 0) {
-    Fp8Args a{};
-    a.x = Fp8Plane{ws + p.qt, ws + p.exps_t, p.ld_t, p.ld_exps_t, 0};
-    a.w = fp8_plane(xt);
-    a.tile = p.dw.tile;
-    a.g.M = out;
-    a.g.N = in;
-    a.g.K = ceil_div(rows, kFp8Block);
-    a.g.tiles_m = p.dw.tiles_m;
-    a.g.tiles_n = p.dw.tiles_n;
-    a.g.splits = p.dw.splits;
-    a.g.k_per_split = p.dw.blocks_per_split;
-    a.g.out = plane_of(dw);
-    a.g.parts = dw_parts;
-    set_reciprocals(a);
     // parts are in 32 bits: here the type says by which products
-    if (int rc = few ? product_fp8(dw->type, kStore, a, st)
-                     : dw->type == GOSH_BF16 ? launch_fp8<Bf16>(kParts, a, st) : launch_fp8<F32>(kParts, a, st))
+    if (int rc = few ? product_fp8(dw->type, kStore, gw, st)
+                     : dw->type == GOSH_BF16 ? launch_fp8<Bf16>(kParts, gw, st) : launch_fp8<F32>(kParts, gw, st))
       return rc;
   }
   if (dw != nullptr && !few) {
     const int64_t n = static_cast<int64_t>(out) * in;
     jobs[joins++] = {dw_parts, n, n, dw->ld, dw->data, rows > 0 ? p.dw.splits : 0, in, dw->type};
   }
-  if (db != nullptr) jobs[joins++] = {sums, out, out, out, db, static_cast<int32_t>(ceil_div(rows, kFp8Block)), out, GOSH_F32};
+  if (db != nullptr) jobs[joins++] = db_job;
   return join_parts(jobs, joins, st);
 }
 

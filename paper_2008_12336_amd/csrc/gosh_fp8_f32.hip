@@ -8,4 +8,9 @@ int launch_fp8<F32>(ProductOut out, const Fp8Args &args, hipStream_t st) {
   return launch_fp8_any<F32>(out, args, st);
 }
 
+template <>
+int launch_fp8_gradients<F32>(const Fp8Args &dx, const Fp8Args &dw, int32_t dw_type, const JoinJob &db, hipStream_t st) {
+  return launch_fp8_few_gradients<F32, F32>(dx, dw, db, st);
+}
+
 }  // namespace gosh

@@ -306,20 +306,25 @@ constexpr int64_t kFewRows = 32;  // that are put into 8 bits in the product's l
 // 8192 x 512 -> 512: 21.8, 14.0, 9.6, 17.2; 131,072 x 128 -> 128: 33.5, 35.5, 17.6, 32.5; 65,536 x 512 -> 512: 124, 89, 40.7, 34.6).
 // A CU works on four tiles of 64 together, two of 128 or one of 256; each has its way out, and steps that are as long as a load
 // is under way where it is alone.
-double fp8_time(int tile, int64_t tiles, int64_t blocks) {
+// Exact products (see fp8_mma; 50,021 x 260 -> 1037 in f32: 123, 96 and 105 us; 65,536 x 1024 -> 1024 in f16: 273, 158 and 169)
+// take longer, the largest tiles the most.
+double fp8_time(int tile, int64_t tiles, int64_t blocks, bool exact) {
   const double k = static_cast<double>(blocks), per_cu = static_cast<double>(ceil_div(tiles, 256));
   if (tile == 32) return few_waves(blocks) == 4 ? 4.0 + per_cu * (0.5 + 0.12 * k) : 3.7 + per_cu * 0.32 * k;
   const double held = tile == 256 ? 1 : tile == 128 ? 2 : 4, together = std::min(per_cu, held), turns = std::ceil(per_cu / held);
+  if (exact && tile == 256) return 2.0 + turns * (17.0 + 2.9 * k);
+  if (exact && tile == 128) return 2.0 + turns * (together > 1 ? 8.0 + 1.4 * k : 5.0 + 1.3 * k);
+  if (exact) return 1.5 + turns * (2.5 + together + k * (0.4 + 0.25 * together));
   if (tile == 256) return 2.0 + turns * (10.0 + 1.2 * k);
   if (tile == 128) return 2.0 + turns * (4.5 + 0.75 * together + k * (together > 1 ? 0.95 : 0.6));
   return 1.5 + turns * (2.0 + 1.25 * together + k * (0.22 + 0.2 * together));
 }
-int fp8_tile_for(int64_t M, int64_t N, int64_t blocks, bool few) {
+int fp8_tile_for(int64_t M, int64_t N, int64_t blocks, bool exact) {
   int best = 0;
   double least = 0;
   for (int s : {256, 128, 64, 32}) {
-    if (s == 32 && (!few || M > 65535 * 32)) continue;
-    const double time = fp8_time(s, ceil_div(M, s) * ceil_div(N, s), blocks);
+    if (s == 32 && M > 65535 * 32) continue;  // a grid's rows
+    const double time = fp8_time(s, ceil_div(M, s) * ceil_div(N, s), blocks, exact);
     if (best == 0 || time < least) best = s, least = time;
   }
   return best;
@@ -327,7 +332,7 @@ int fp8_tile_for(int64_t M, int64_t N, int64_t blocks, bool few) {
 
 // All rows of A, as many to a launch as a grid takes.
 int product_of_rows_fp8(int32_t type, ProductOut out, Fp8Args a, int64_t rows, hipStream_t st) {
-  const int tile = a.tile = a.pack.data != nullptr ? 32 : fp8_tile_for(rows, a.g.N, a.g.K, true);
+  const int tile = a.tile = a.pack.data != nullptr ? 32 : fp8_tile_for(rows, a.g.N, a.g.K, type != GOSH_BF16 || a.exact);
   a.g.tiles_n = static_cast<int32_t>(ceil_div(a.g.N, tile));
   a.g.splits = std::max(a.g.splits, 1);
   a.g.k_per_split = ceil_div(a.g.K, a.g.splits);
@@ -364,7 +369,7 @@ Fp8DwPlan plan_dw_fp8(int64_t rows, int32_t in, int32_t out) {
     for (int64_t want = 1; want <= (s == 32 ? 1 : std::min<int64_t>(std::max<int64_t>(blocks, 1), 1024)); want *= 2) {
       const int64_t per = std::max<int64_t>(1, ceil_div(blocks, want)), splits = ceil_div(blocks, per);
       if (want > 1 && tiles * splits > 2048) break;
-      const double time = fp8_time(s, tiles * splits, per) + (s == 32 ? 0 : 2.5 + 1.6e-6 * static_cast<double>(splits) * in * out);
+      const double time = fp8_time(s, tiles * splits, per, false) + (s == 32 ? 0 : 2.5 + 1.6e-6 * static_cast<double>(splits) * in * out);
       if (best.tile != 0 && time >= least) continue;
       least = time;
       best = Fp8DwPlan{s, static_cast<int32_t>(tiles_m), static_cast<int32_t>(tiles_n), static_cast<int32_t>(splits), per};
@@ -559,7 +564,7 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
   }
   const JoinJob db_job{sums, out, db != nullptr ? out : 0, out, db, static_cast<int32_t>(ceil_div(rows, kFp8Block)), out, GOSH_F32};
   const bool few = rows > 0 && dw != nullptr && p.dw.tile == 32;
-  if (few && (dx == nullptr || fp8_tile_for(rows, in, gx.g.K, true) == 32)) {
+  if (few && (dx == nullptr || fp8_tile_for(rows, in, gx.g.K, dy->type != GOSH_BF16) == 32)) {
     if (dx != nullptr) {
       gx.g.M = rows;
       gx.g.tiles_m = static_cast<int32_t>(ceil_div(rows, 32));

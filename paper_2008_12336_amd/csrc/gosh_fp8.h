@@ -15,14 +15,16 @@ constexpr int kFp8Block = 128;
 
 int check_fp8(const gosh_fp8 *m, const char *what, int use = 0);
 
-// An operand of a product, k along its rows.  shift: 0, or 7 where 128 rows share their exponents.
+// An operand of a product, k along its rows.  shift: 0, or 7 where 128 rows share their exponents.  step: bytes from one
+// block of 128 k to the next: 128, but in workspaces, where a block's 128 bytes of all rows lie together.
 struct Fp8Plane {
   const uint8_t *data, *exps;
   int64_t ld, ld_exps;
   int32_t shift;
+  int64_t step;
 };
 inline Fp8Plane fp8_plane(const gosh_fp8 *m) {
-  return {static_cast<const uint8_t *>(m->data), m->exps, m->ld, m->ld_exps, m->block_rows == 1 ? 0 : 7};
+  return {static_cast<const uint8_t *>(m->data), m->exps, m->ld, m->ld_exps, m->block_rows == 1 ? 0 : 7, kFp8Block};
 }
 
 struct Fp8Args {

@@ -39,10 +39,10 @@ int check_fp8_shape(const gosh_fp8 *m, const char *what, int64_t rows, int64_t c
 
 struct Fp8Out {
   uint8_t *data, *exps;
-  int64_t ld, ld_exps;
+  int64_t ld, ld_exps, step;  // step: see Fp8Plane
 };
 Fp8Out fp8_out(const gosh_fp8 *m) {
-  return m == nullptr ? Fp8Out{nullptr, nullptr, 0, 0} : Fp8Out{static_cast<uint8_t *>(m->data), m->exps, m->ld, m->ld_exps};
+  return m == nullptr ? Fp8Out{nullptr, nullptr, 0, 0, 0} : Fp8Out{static_cast<uint8_t *>(m->data), m->exps, m->ld, m->ld_exps, kFp8Block};
 }
 
 struct PackArgs {
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(256, 3) void pack_fp8_kernel(const PackArgs a) {
         if (first + col >= a.cols) continue;
         const U4 x = *reinterpret_cast<const U4 *>(turned + col * kFp8Block + (2 * pair ^ (shift & 14)) * 8);
         const U4 out = shift & 1 ? U4{x[2], x[3], x[0], x[1]} : x;
-        *reinterpret_cast<U4 *>(a.qt.data + (first + col) * a.qt.ld + block * kFp8Block + 16 * pair) = out;
+        *reinterpret_cast<U4 *>(a.qt.data + (first + col) * a.qt.ld + block * a.qt.step + 16 * pair) = out;
       }
     }
   }
@@ -381,7 +381,7 @@ Fp8DwPlan plan_dw_fp8(int64_t rows, int32_t in, int32_t out) {
 // What the gradient's workspace holds, as offsets.
 struct Fp8BackwardPlan {
   Fp8DwPlan dw;
-  int64_t ld, ld_exps, ld_t, ld_exps_t;
+  int64_t ld, ld_exps, step_t, ld_exps_t;  // the transposed dz: a block of 128 rows of all columns lies together
   uint64_t q, exps, qt, exps_t, sums, dw_parts, bytes;
 };
 Fp8BackwardPlan plan_backward_fp8(int64_t rows, int32_t in, int32_t out) {
@@ -389,7 +389,7 @@ Fp8BackwardPlan plan_backward_fp8(int64_t rows, int32_t in, int32_t out) {
   p.dw = plan_dw_fp8(rows, in, out);
   const int64_t blocks = ceil_div(out, kFp8Block), blocks_t = ceil_div(rows, kFp8Block);
   p.ld = blocks * kFp8Block, p.ld_exps = ceil_div(blocks, 4) * 4;
-  p.ld_t = blocks_t * kFp8Block, p.ld_exps_t = ceil_div(blocks_t, 4) * 4;
+  p.step_t = static_cast<int64_t>(out) * kFp8Block, p.ld_exps_t = ceil_div(blocks_t, 4) * 4;
   uint64_t at = 0;
   const auto take = [&](uint64_t bytes) {
     const uint64_t from = at;
@@ -398,7 +398,7 @@ Fp8BackwardPlan plan_backward_fp8(int64_t rows, int32_t in, int32_t out) {
   };
   p.q = take(static_cast<uint64_t>(rows) * p.ld);
   p.exps = take(static_cast<uint64_t>(rows) * p.ld_exps);
-  p.qt = take(static_cast<uint64_t>(out) * p.ld_t);
+  p.qt = take(static_cast<uint64_t>(blocks_t) * p.step_t);
   p.exps_t = take(static_cast<uint64_t>(out) * p.ld_exps_t);
   p.sums = take(static_cast<uint64_t>(blocks_t) * out * 4);
   p.dw_parts = take(p.dw.tile == 32 ? 0 : static_cast<uint64_t>(p.dw.splits) * in * out * 4);
@@ -530,8 +530,8 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
     PackArgs a{};
     a.x = plane_of(dy);
     a.z = plane_of(act == GOSH_ACT_NONE ? nullptr : z);
-    if (dx != nullptr) a.q = Fp8Out{ws + p.q, ws + p.exps, p.ld, p.ld_exps};
-    if (dw != nullptr) a.qt = Fp8Out{ws + p.qt, ws + p.exps_t, p.ld_t, p.ld_exps_t};
+    if (dx != nullptr) a.q = Fp8Out{ws + p.q, ws + p.exps, p.ld, p.ld_exps, kFp8Block};
+    if (dw != nullptr) a.qt = Fp8Out{ws + p.qt, ws + p.exps_t, kFp8Block, p.ld_exps_t, p.step_t};
     a.sums = db != nullptr ? sums : nullptr;
     a.rows = rows;
     a.cols = out;
@@ -541,14 +541,14 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
   }
   Fp8Args gx{}, gw{};
   if (dx != nullptr) {
-    gx.x = Fp8Plane{ws + p.q, ws + p.exps, p.ld, p.ld_exps, 0};
+    gx.x = Fp8Plane{ws + p.q, ws + p.exps, p.ld, p.ld_exps, 0, kFp8Block};
     gx.w = fp8_plane(wt);
     gx.g.N = in;
     gx.g.K = ceil_div(out, kFp8Block);
     gx.g.out = plane_of(dx);
   }
   if (dw != nullptr) {
-    gw.x = Fp8Plane{ws + p.qt, ws + p.exps_t, p.ld_t, p.ld_exps_t, 0};
+    gw.x = Fp8Plane{ws + p.qt, ws + p.exps_t, kFp8Block, p.ld_exps_t, 0, p.step_t};
     gw.w = fp8_plane(xt);
     gw.tile = p.dw.tile;
     gw.g.M = out;

@@ -13,7 +13,8 @@ namespace gosh {
 // The rows of a tile that a lane reads; rows past the end read the last one's, for results that nobody stores.
 struct Fp8Lane {
   const uint8_t *q, *e;
-  __device__ __forceinline__ Fp8Lane(const Fp8Plane &p, int64_t row, int64_t rows) {
+  int64_t step;
+  __device__ __forceinline__ Fp8Lane(const Fp8Plane &p, int64_t row, int64_t rows) : step(p.step) {
     const int64_t r = row < rows ? row : rows - 1;
     q = p.data + r * p.ld + (threadIdx.x >> 5 & 1) * 32;
     e = p.exps + (r >> p.shift) * p.ld_exps;
@@ -21,7 +22,7 @@ struct Fp8Lane {
   // Block k: 32 bytes of each half.
   __device__ __forceinline__ uint32_t load(int64_t k, U4 (&v)[2][2]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i / 2][i % 2] = *reinterpret_cast<const U4 *>(q + k * kFp8Block + i / 2 * 64 + i % 2 * 16);
+    for (int i = 0; i < 4; ++i) v[i / 2][i % 2] = *reinterpret_cast<const U4 *>(q + k * step + i / 2 * 64 + i % 2 * 16);
     return e[k];
   }
 };
@@ -194,19 +195,19 @@ struct Fp8Tile {
       off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(p.ld) + Spread<BX, 64>::k_major(row, slot) / 8 % 8 * 16;
     }
   }
-  // At most 256 rows of 2^23 bytes: 2^31.
-  __device__ __forceinline__ void begin(const Fp8Plane &p, int64_t x, int64_t rows, int64_t blocks, int64_t k0) {
-    range.base = reinterpret_cast<uint64_t>(p.data) + x * p.ld + k0 * kFp8Block;
+  // A block of the tile's rows: at most 256 rows of 2^23 bytes, 2^31.
+  __device__ __forceinline__ void begin(const Fp8Plane &p, int64_t x, int64_t rows, int64_t k0) {
+    range.base = reinterpret_cast<uint64_t>(p.data) + x * p.ld + k0 * p.step;
     const int64_t here = rows - x < BX ? rows - x : BX;
-    range.bytes = static_cast<uint32_t>((here - 1) * p.ld + (blocks - k0) * kFp8Block);
+    range.bytes = static_cast<uint32_t>((here - 1) * p.ld + kFp8Block);
   }
   __device__ __forceinline__ void load(int i, uint32_t lds) const {
     load_to_lds<false>(off[i], range, lds + (__builtin_amdgcn_readfirstlane(threadIdx.x / 64) * kLoads + i) * 1024);
   }
 };
 
-// The exponents of a step: a lane of the wavefront that has 64 rows of an operand loads four blocks' bytes of its row,
-// of which a step takes one.  64 rows of A for each of the first wavefronts, then of B; those that are left over load what the
+// The exponents: a lane of the wavefront that has 64 rows of an operand loads four blocks' bytes of its row, which
+// last for up to four steps.  64 rows of A for each of the first wavefronts, then of B; those that are left over load what the
 // first ones do.
 template <int BM, int BN, int Waves>
 struct Fp8Units {
@@ -272,8 +273,8 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
   typedef Fp8Tile<BN, kWaves> TB;
   typedef Fp8Units<BM, BN, kWaves> Units;
   constexpr int WM = BM / 2, WN = BN / kAcross, RM = WM / 32, RN = WN / 32;
-  constexpr int kStep = TA::kBytes + TB::kBytes + Units::kBytes, kLoads = TA::kLoads + TB::kLoads + 1;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[2 * kStep / 2];
+  constexpr int kStep = TA::kBytes + TB::kBytes, kLoads = TA::kLoads + TB::kLoads;
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[(2 * kStep + 2 * Units::kBytes) / 2];
   __shared__ __attribute__((aligned(16))) float slabs[kWaves * Slab<WN>::kFloats];
 
   const ProductArgs &g = args.g;
@@ -289,41 +290,50 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
   a.init(args.x);
   b.init(args.w);
   uint32_t into = base;
+  // exponents go to their two places in turns: a place is written again only a whole step after it was read last
+  uint32_t units_into = base + 2 * kStep, units_from = units_into;
   int turn = turns.id, to_go;
   Place from;  // of the tile that is being loaded
+  bool units_next;  // the step that is loaded next needs other exponents
   const auto begin = [&]() {
     from = fp8_place(args, turn, BM, BN);
-    a.begin(args.x, from.m0, g.M, g.K, from.k0);
-    b.begin(args.w, from.n0, g.N, g.K, from.k0);
+    a.begin(args.x, from.m0, g.M, from.k0);
+    b.begin(args.w, from.n0, g.N, from.k0);
     units.begin(args, from.m0, from.n0, from.k0);
     to_go = static_cast<int>(from.k1 - from.k0);
+    units_next = true;
   };
   // On to the step after: the next of the tile, or the first of the next tile, or none, whose loads read nothing.
   const auto advance = [&]() {
     into = into == base ? base + kStep : base;
-    a.range.base += kFp8Block, a.range.bytes -= kFp8Block;
-    b.range.base += kFp8Block, b.range.bytes -= kFp8Block;
-    ++units.block;
+    a.range.base += args.x.step;
+    b.range.base += args.w.step;
+    units_next = (++units.block & 3) == 0;
     if (--to_go > 0) return;
     turn += turns.step;
     if (turn < turns.end) begin();
     else a.range.bytes = b.range.bytes = units.range.bytes = 0, to_go = 0x7fffffff;
   };
-  const auto load = [&](int i) {
-    if (i < TA::kLoads) a.load(i, into);
-    else if (i < TA::kLoads + TB::kLoads) b.load(i - TA::kLoads, into + TA::kBytes);
-    else units.load(into + TA::kBytes + TB::kBytes);
+  const auto load = [&]() {
+#pragma unroll
+    for (int i = 0; i < TA::kLoads; ++i) a.load(i, into);
+#pragma unroll
+    for (int i = 0; i < TB::kLoads; ++i) b.load(i, into + TA::kBytes);
+    if (units_next) {
+      units.load(units_into);
+      units_from = units_into;
+      units_into = units_into == base + 2 * kStep ? units_into + Units::kBytes : base + 2 * kStep;
+    }
   };
   begin();
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) load(i);
+  load();
+  const uint32_t units_first = units_from;
   float bias[RN];
   load_bias<RN, Out>(g, from.n0 + wn, bias);
   bool ahead = to_go > 1;  // two steps are under way before the first
   if (ahead) {
     advance();
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(i);
+    load();
   }
 
   const uint16_t *now = lds;
@@ -340,16 +350,17 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
       for (int c = 0; c < 2; ++c)
         fb[half][j][c] = __builtin_bit_cast(U4, Spread<BN, 64>::template take<true>(now + TA::kBytes / 2, wn + 32 * j, 2 * half + c));
   };
-  const auto take_units = [&](uint32_t (&x)[RM], uint32_t (&w)[RN]) {
-    const uint32_t *const e = reinterpret_cast<const uint32_t *>(now + (TA::kBytes + TB::kBytes) / 2);
+  const auto take_units = [&](uint32_t where, uint32_t (&x)[RM], uint32_t (&w)[RN]) {
+    const uint32_t *const e = reinterpret_cast<const uint32_t *>(lds + (where - base) / 2);
 #pragma unroll
     for (int i = 0; i < RM; ++i) x[i] = e[wm + 32 * i + (lane & 31)];
 #pragma unroll
     for (int j = 0; j < RN; ++j) w[j] = e[BM + wn + 32 * j + (lane & 31)];
   };
+  // all but the loads of the second step, of which there are kLoads or, with its exponents, one more
   if (ahead) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(kLoads) : "memory");
   else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  take_units(ea[0], eb[0]);
+  take_units(units_first, ea[0], eb[0]);
   take_b(0);
   take_a(0, 0, 0);
   for (int id = turns.id; id < turns.end; id += turns.step) {
@@ -362,8 +373,7 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
       if (!ahead) {
         advance();
         if (is_forward(Out) && s + 1 == steps) load_bias<RN, Out>(g, from.n0 + wn, bias);  // the next tile's, or this one's again
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) load(i);
+        load();
       }
       ahead = false;
       const int shift = (static_cast<int>(at.k0) + s & 3) * 8;
@@ -387,7 +397,7 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
       // The next step's tile is there, every wavefront's part of it, and every wavefront is done with this step's.
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       now = now == lds ? lds + kStep / 2 : lds;
-      take_units(ea[0], eb[0]);
+      take_units(units_from, ea[0], eb[0]);
       take_b(0);
       take_a(0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);

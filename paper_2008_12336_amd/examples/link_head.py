@@ -5,8 +5,9 @@ products of the rows of vertex pairs, and says how well it tells held-out edges 
 
 The head is layer norm (rows of hubs are orders of magnitude longer than others), a linear layer with GELU to four
 times the width, one back with the features added, and one to a single logit.  Between the passes it keeps the normalised
-rows, the layers' inputs and the pre-activations in 8 bits, a byte an entry, of which the backward calls read them.
-torch holds the parameters and their optimiser; every operator of the head is one of the library's kernels."""
+rows, the layers' inputs and the pre-activations in 8 bits, a byte an entry, of which the backward calls read them.  The
+optimiser keeps its moments in 8 bits too and writes the weights' 16-bit copies, of which the layers read them.  torch holds the
+parameters and takes the loss; every operator of the head and its optimiser is one of the library's kernels."""
 from __future__ import annotations
 
 import argparse
@@ -31,6 +32,7 @@ class LinkHead:
         self.params = dict(gamma=torch.ones(dim, device=DEV), beta=zeros(dim), w1=init(wide, dim), b1=zeros(wide),
                            w2=0.1 * init(dim, wide), b2=zeros(dim), w3=init(1, dim), b3=zeros(1))
         self.grads = {name: torch.empty_like(p) for name, p in self.params.items()}
+        self.copies = {name: self.params[name].to(dtype) for name in ("w1", "w2", "w3")}
         act = lambda n: torch.empty(rows, n, dtype=dtype, device=DEV)  # noqa: E731
         eight = lambda n: G.Packed8(rows, n, dtype, DEV)  # noqa: E731
         self.h, self.a, self.o, self.s = act(dim), act(wide), act(dim), act(1)
@@ -38,8 +40,11 @@ class LinkHead:
         self.rstd = torch.empty(rows, device=DEV)
         self.xhat8, self.h8, self.z8, self.a8 = eight(dim), eight(dim), eight(wide), eight(wide)
 
-    def weights(self):
-        return {name: self.params[name].to(self.dtype) for name in ("w1", "w2", "w3")}
+    def optimiser(self):
+        """AdamW over all parameters, which keeps the copies up to date."""
+        names = list(self.params)
+        return G.gosh_adamw_create([self.params[n] for n in names], [self.grads[n] for n in names], bits=8,
+                                   copies=[self.copies.get(n) for n in names])
 
     def forward(self, x: torch.Tensor, w: dict) -> torch.Tensor:
         """The logits of `rows` pairs' features."""
@@ -61,7 +66,7 @@ class LinkHead:
 
     def score(self, x: torch.Tensor) -> torch.Tensor:
         """Logits of any number of pairs, nothing kept."""
-        p, w, n = self.params, self.weights(), x.shape[0]
+        p, w, n = self.params, self.copies, x.shape[0]
         new = lambda k: torch.empty(n, k, dtype=self.dtype, device=DEV)  # noqa: E731
         h, a, o, s = new(x.shape[1]), new(4 * x.shape[1]), new(x.shape[1]), new(1)
         G.gosh_layer_norm(x, p["gamma"], p["beta"], h)
@@ -102,21 +107,16 @@ def train(scale: int = 14, dim: int = 64, steps: int = 200, rows: int = 16384, s
     head = LinkHead(dim, rows, seed=seed)
     test_pos, test_neg = (features(M, p, unit, head.dtype) for p in (held, none(held.shape[0])))
     before = auc(head.score(test_pos), head.score(test_neg))
-    for p in head.params.values():
-        p.requires_grad_(False)
-    optimiser = torch.optim.Adam(head.params.values(), lr=2e-3)
+    optimiser = head.optimiser()
     target = torch.cat((torch.ones(rows // 2, device=DEV), torch.zeros(rows - rows // 2, device=DEV)))
     losses = []
-    for _ in range(steps):
+    for step in range(1, steps + 1):
         some = kept[torch.randint(kept.shape[0], (rows // 2,), generator=gen, device=DEV)]
         x = features(M, torch.cat((some, none(rows - rows // 2))), unit, head.dtype)
-        w = head.weights()
-        logits = head.forward(x, w).float()
+        logits = head.forward(x, head.copies).float()
         losses.append(torch.nn.functional.softplus(torch.where(target > 0, -logits, logits)).mean())
-        grads = head.backward(((torch.sigmoid(logits) - target) / rows).to(head.dtype), w)
-        for name, p in head.params.items():
-            p.grad = grads[name]
-        optimiser.step()
+        head.backward(((torch.sigmoid(logits) - target) / rows).to(head.dtype), head.copies)
+        G.gosh_adamw_step(optimiser, lr=2e-3, step=step)
     return before, auc(head.score(test_pos), head.score(test_neg)), [float(v) for v in losses]
 
 

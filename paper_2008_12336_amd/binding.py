@@ -827,6 +827,8 @@ def gosh_linear_fp8(x, x8: PackedFp8, w: PackedFp8, y: torch.Tensor, bias=None, 
     """y = act(x8 w^T + bias) + residual, after x was put into x8; x None: x8 holds it.  z: a tensor or a Packed8 that
     receives x8 w^T + bias."""
     v = _fp8(w, "w")
+    if v is None:
+        raise TypeError("w must be a PackedFp8")
     _check(lib().gosh_linear_fp8(_mat(x, "x"), _fp8(x8, "x8"), v, _floats(bias, "bias", v.rows), act, _mat(residual, "residual"),
                                  _mat(y, "y"), _mat(z, "z"), _stream(stream)))
 

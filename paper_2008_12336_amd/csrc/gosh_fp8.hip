@@ -355,7 +355,8 @@ int product_of_rows_fp8(int32_t type, ProductOut out, Fp8Args a, int64_t rows, h
 
 uint64_t round_up(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// How dw is split along the rows: the parts are written and read again, at 5 TB/s.  Few results (32) are not.
+// How dw is split along the rows: the parts are written and read again, at 5 TB/s.  Few results (32) are not split; what is not is
+// stored as it is.
 struct Fp8DwPlan {
   int32_t tile, tiles_m, tiles_n, splits;
   int64_t blocks_per_split;
@@ -369,7 +370,7 @@ Fp8DwPlan plan_dw_fp8(int64_t rows, int32_t in, int32_t out) {
     for (int64_t want = 1; want <= (s == 32 ? 1 : std::min<int64_t>(std::max<int64_t>(blocks, 1), 1024)); want *= 2) {
       const int64_t per = std::max<int64_t>(1, ceil_div(blocks, want)), splits = ceil_div(blocks, per);
       if (want > 1 && tiles * splits > 2048) break;
-      const double time = fp8_time(s, tiles * splits, per, false) + (s == 32 ? 0 : 2.5 + 1.6e-6 * static_cast<double>(splits) * in * out);
+      const double time = fp8_time(s, tiles * splits, per, false) + (splits <= 1 ? 0 : 2.5 + 1.6e-6 * static_cast<double>(splits) * in * out);
       if (best.tile != 0 && time >= least) continue;
       least = time;
       best = Fp8DwPlan{s, static_cast<int32_t>(tiles_m), static_cast<int32_t>(tiles_n), static_cast<int32_t>(splits), per};
@@ -401,7 +402,7 @@ Fp8BackwardPlan plan_backward_fp8(int64_t rows, int32_t in, int32_t out) {
   p.qt = take(static_cast<uint64_t>(blocks_t) * p.step_t);
   p.exps_t = take(static_cast<uint64_t>(out) * p.ld_exps_t);
   p.sums = take(static_cast<uint64_t>(blocks_t) * out * 4);
-  p.dw_parts = take(p.dw.tile == 32 ? 0 : static_cast<uint64_t>(p.dw.splits) * in * out * 4);
+  p.dw_parts = take(p.dw.splits == 1 ? 0 : static_cast<uint64_t>(p.dw.splits) * in * out * 4);
   p.bytes = at;
   return p;
 }
@@ -580,11 +581,11 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
   int joins = 0;
   if (dw != nullptr && rows > 0) {
     // parts are in 32 bits: here the type says by which products
-    if (int rc = few ? product_fp8(dw->type, kStore, gw, st)
+    if (int rc = p.dw.splits == 1 ? product_fp8(dw->type, kStore, gw, st)
                      : dw->type == GOSH_BF16 ? launch_fp8<Bf16>(kParts, gw, st) : launch_fp8<F32>(kParts, gw, st))
       return rc;
   }
-  if (dw != nullptr && !few) {
+  if (dw != nullptr && (rows == 0 || p.dw.splits > 1)) {
     const int64_t n = static_cast<int64_t>(out) * in;
     jobs[joins++] = {dw_parts, n, n, dw->ld, dw->data, rows > 0 ? p.dw.splits : 0, in, dw->type};
   }

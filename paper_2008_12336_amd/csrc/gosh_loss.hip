@@ -75,7 +75,8 @@ __global__ __launch_bounds__(Lanes > 256 ? Lanes : 256) void loss_kernel(const L
   }
   if (part) rest = Entries<T, E>::fetch(x + whole_chunks * E, over);
   // the target's logit: a load of its own is cheaper than to compare every column
-  const float hit = target < 0 || wrong ? 0.f : T::up(x[target]);
+  float hit = target < 0 || wrong ? 0.f : T::up(x[target]);
+  asm volatile("" : "+v"(hit));  // here by now: another wavefront may write the gradient over it as soon as all have joined
   float v[Count][E], most = -INFINITY;
 #pragma unroll
   for (int c = 0; c < Count; ++c) {

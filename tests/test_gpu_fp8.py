@@ -164,6 +164,59 @@ def test_linear_backward(shape, dtype):
 
 
 @types
+@pytest.mark.parametrize("shape", [(20011, 512, 1024, 0, 0), (70001, 300, 520, 3, 1), (3000, 4000, 700, 0, 0)], ids=lambda s: "x".join(map(str, s)))
+def test_many_rows(shape, dtype):
+    """Every size of tiles, more of them than the device holds at once, and sums that are split."""
+    test_linear(shape, dtype)
+    test_linear_backward(shape, dtype)
+
+
+@types
+@pytest.mark.parametrize("pad", [0, 8])
+def test_results_larger_than_the_caches(pad, dtype):
+    rows, k, n = 65281, 140, 2056
+    rnd = gen(rows + pad)
+    x8, w8 = packed(rnd(rows, k).to(dtype)), packed(rnd(n, k) / math.sqrt(k), 128)
+    a, w, b, r = values(x8), values(w8), 0.3 * rnd(n), view(rnd(rows, n), dtype, pad, pad)[0]
+    for kind, use_r, use_z in ((H.GELU, False, True), (H.SILU, True, False), (H.RELU, True, True), (H.NONE, False, False)):
+        y, ymem = view(torch.zeros(rows, n, device=DEV), dtype, pad, pad)
+        z, zmem = view(torch.zeros(rows, n, device=DEV), dtype, pad, pad)
+        G.gosh_linear_fp8(None, x8, w8, y, bias=b, act=kind, residual=r if use_r else None, z=z if use_z else None)
+        wy, wz, ey, ez = S.linear_fp8(a, w, b.double(), kind, r.double() if use_r else None, dtype)
+        within(y, wy, H.rounded(ey, wy, dtype), f"y, activation {kind}")
+        if use_z:
+            within(z, wz, H.rounded(ez, wz, dtype), f"z, activation {kind}")
+        again = r.clone()
+        G.gosh_linear_fp8(None, x8, w8, again, bias=b, act=kind, residual=again if use_r else None)  # in place, and the same bits
+        assert torch.equal(again, y)
+        beside(y, ymem)
+        beside(z, zmem)
+
+
+@pytest.mark.parametrize("rows", [3, 200, 9000])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_units_far_apart(rows, dtype):
+    """Powers of two come out of both operands as they are: rows scaled by 2^100 against weights scaled by 2^-100, and down to where
+    results have no digits left."""
+    rnd = gen(rows)
+    k, n = 260, 40
+    x, w = rnd(rows, k).to(dtype), rnd(n, k).to(dtype)
+    out = []
+    for up, down in ((0, 0), (100, -100), (-60, 60), (-100, 90)):
+        x8, w8 = packed(x * 2.0 ** up), packed(w * 2.0 ** down, 128)
+        y = torch.empty(rows, n, dtype=dtype, device=DEV)
+        G.gosh_linear_fp8(None, x8, w8, y)
+        out.append(y.double() * 2.0 ** -(up + down))
+    assert all(torch.equal(y, out[0]) for y in out[1:])
+    y = torch.empty(rows, n, dtype=dtype, device=DEV)
+    G.gosh_linear_fp8(None, packed(x * 2.0 ** -120), packed(w * 2.0 ** -120, 128), y)
+    assert (y.abs() <= 2.0 ** -126).all()
+    G.gosh_linear_fp8(None, packed(x * 2.0 ** 100), packed(w * 2.0 ** 100, 128), y)
+    # every product is beyond the largest number, of either sign: infinities that cancel are NaN
+    assert not torch.isfinite(y[out[0] != 0]).any()
+
+
+@types
 def test_rows_of_none(dtype):
     e = lambda n: torch.empty(0, n, dtype=dtype, device=DEV)  # noqa: E731
     w8, wt = G.PackedFp8(5, 7, 128, DEV), G.PackedFp8(7, 5, 128, DEV)

@@ -1,9 +1,11 @@
 """Build libgosh.so (HIP kernels + C ABI) for gfx950 with hipcc, in-tree."""
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import shutil
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -41,12 +43,21 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False) -> str:
-    srcs = [os.path.join(CSRC, s) for s in SOURCES]
-    cmd = [hipcc(), *FLAGS, "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
-           "-x", "hip", *srcs, "-o", LIB]
-    if verbose:
-        print(" ".join(cmd))
-    subprocess.run(cmd, check=True)
+    """Every unit by itself, as many at once as there are processors, and the library out of them."""
+    flags = [f for f in FLAGS if f != "-shared"]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+
+    with tempfile.TemporaryDirectory(prefix="gosh_build_") as tmp:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        commands = [[hipcc(), *flags, "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-x", "hip", "-c",
+                     os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objects)]
+        with concurrent.futures.ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(run, commands))
+        run([hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-fopenmp", *objects, "-o", LIB])
     build_example(verbose)
     return LIB
 

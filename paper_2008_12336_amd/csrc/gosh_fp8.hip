@@ -472,20 +472,20 @@ int gosh_linear_fp8(const gosh_mat *x, const gosh_fp8 *x8, const gosh_fp8 *w, co
   if (rows == 0) return GOSH_OK;
   hipStream_t st = as_stream(hip_stream);
   Fp8Args a{};
-  if (x != nullptr && rows <= kFewRows) {  // in the product's launch
-    a.pack = plane_of(x);
+  a.x = fp8_plane(x8);
+  a.w = fp8_plane(w);
+  a.exact = act == GOSH_ACT_RELU;
+  a.g.N = out;
+  a.g.K = ceil_div(in, kFp8Block);
+  a.g.forward = ForwardOut{bias, plane_of(residual), plane_of(y), plane_of(z), Plane{nullptr, nullptr, 0, 0}, act, z != nullptr && z->packed,
+                           rows * out * (y->type == GOSH_F32 ? 4 : 2) >= kPastCaches};
+  if (x != nullptr && rows <= kFewRows && fp8_tile_for(rows, out, a.g.K, y->type != GOSH_BF16 || a.exact) == 32) {
+    a.pack = plane_of(x);  // in the product's launch
     a.pack_type = x->type;
     a.pack_cols = in;
   } else if (x != nullptr) {
     if (int rc = gosh_pack_fp8(x, x8, nullptr, hip_stream)) return rc;
   }
-  a.x = fp8_plane(x8);
-  a.w = fp8_plane(w);
-  a.g.N = out;
-  a.g.K = ceil_div(in, kFp8Block);
-  a.g.forward = ForwardOut{bias, plane_of(residual), plane_of(y), plane_of(z), Plane{nullptr, nullptr, 0, 0}, act, z != nullptr && z->packed,
-                           rows * out * (y->type == GOSH_F32 ? 4 : 2) >= kPastCaches};
-  a.exact = act == GOSH_ACT_RELU;
   return product_of_rows_fp8(y->type, kForward, a, rows, st);
 }
 

@@ -119,7 +119,8 @@ __device__ __forceinline__ void load_square(const PackArgs &a, int64_t row, int 
 // is joined over those 16 lanes, that along a column over the 16 lanes that have the others of its rows, through LDS, by one
 // thread a column; the transposed bytes are turned round in LDS too.  Square: one exponent for all of it.  Maxima pass over NaN,
 // which stays NaN in 8 bits by itself; infinities are made NaN first, where there are any.
-// Bound by memory, and by the slope where there is one.
+// Bound by memory: 131,072 x 1024 in bf16, as it is, takes 51 to 65 us (403 MB), 65,536 x 1024 both ways 65; with GELU's
+// slope, both ways and sums, 65,536 x 2048 take 170 us (805 MB, 4.7 TB/s; four wavefronts a SIMD instead of three spill and take 190).
 template <typename T, bool Square, bool Slope>
 __global__ __launch_bounds__(256, 3) void pack_fp8_kernel(const PackArgs a) {
   __shared__ __attribute__((aligned(16))) float most_of[16][kFp8Block];  // by rows' lanes and column

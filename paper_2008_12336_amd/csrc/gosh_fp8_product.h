@@ -264,8 +264,9 @@ __device__ __forceinline__ Place fp8_place(const Fp8Args &a, int id, int bm, int
 // goes from tile to tile.  Rows of 128 bytes lie as those of 64 entries of 16 bits do.  A wavefront multiplies 32 rows by 64
 // k at a time, while the next such rows of A (and, before the second half of a step, B's) are read from LDS.
 //
-// 16,384 x 8192 -> 4096 takes 434 us, 2.53 PFLOP/s, and 427 without the results' way to memory.  131,072 x 1024 -> 4096 takes 621, of
-// which 495 are left without that (2.2 PFLOP/s): 1.07 GB of results need 155 at the rate of a fill.
+// 16,384 x 8192 -> 4096 takes 437 us, 2.5 PFLOP/s (the matrix cores are busy 63 % of it; the vendor's product with a single
+// scale 416), and 427 without the results' way to memory.  131,072 x 1024 -> 4096 takes 540 to 605 (52 %; 519), of which 495 are left
+// without that: 1.07 GB of results need 155 at the rate of a fill, and the next tile's second step waits behind them.
 template <typename T, int BM, int BN, bool Exact, ProductOut Out>
 __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void fp8_product_kernel(const Fp8Args args) {
   constexpr int kWaves = direct_waves(BN), kAcross = kWaves / 2;

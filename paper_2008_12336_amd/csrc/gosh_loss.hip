@@ -4,6 +4,7 @@
 // entries in 32 bits), so that logits are read once and the gradient is written once: bound by memory.  Each lane subtracts
 // the row's maximum (joined over the lanes first), keeps e = exp(x - max), and the lanes join the sum of e:
 //   loss = log(sum) + (max - x[target]),  gradient = scale weight (e / sum - [class = target]).
+// 65,536 x 4096 in bf16 takes 183 us (5.9 TB/s), 4,096 x 50,000 180, 300,007 x 47 in f32 22 (5.1, partly from the caches).
 #include <algorithm>
 
 #include "gosh_head.h"

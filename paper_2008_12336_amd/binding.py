@@ -211,12 +211,13 @@ def _check(rc: int, stats=None) -> None:
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream) -> int:
     if stream is None:
         if _raw_stream is not None and torch.cuda.is_initialized():  # 2 us less than making a Stream object
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_device())
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -795,14 +796,14 @@ class PackedFp8:
         q, exps, rows, cols = self.q, self.exps, self.rows, self.cols
         if q.dtype is not _E4M3 or exps.dtype is not _U8:
             raise TypeError(f"{name}: q must be float8_e4m3fn and exps uint8")
-        blocks, wide, long = -(-rows // self.block_rows), (cols + 127) & -128, (cols + 511) // 512 * 4
+        tall = self.block_rows
+        blocks, wide, long = rows if tall == 1 else -(-rows // tall), (cols + 127) & -128, (cols + 511) // 512 * 4
         ld, ld_exps = _rows_apart(q, rows, wide), _rows_apart(exps, blocks, long)
         if ld is None or ld_exps is None:
             raise TypeError(f"{name}: q must have {rows} rows of at least {wide} contiguous entries, exps {blocks} of {long}")
         if not rows or not cols:
-            return gosh_fp8(None, None, rows, cols, wide, max(long, 4), self.block_rows)
-        return gosh_fp8(q.data_ptr(), exps.data_ptr(), rows, cols, wide if rows == 1 else ld, long if blocks == 1 else ld_exps,
-                        self.block_rows)
+            return gosh_fp8(None, None, rows, cols, wide, max(long, 4), tall)
+        return gosh_fp8(q.data_ptr(), exps.data_ptr(), rows, cols, ld, ld_exps, tall)
 
 
 def _fp8(m, name: str):
@@ -909,8 +910,13 @@ def gosh_adamw_create(params, grads, bits=8, states=None, copies=None, weight_de
     count = len(params)
     each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * count  # noqa: E731
     bits, decay, copies = each(bits), each(weight_decay), each(copies)
-    if states is None:
-        states = [torch.zeros(gosh_adamw_state_bytes(p.numel(), b), dtype=torch.uint8, device=p.device) for p, b in zip(params, bits)]
+    if states is None:  # slices of one allocation
+        sizes = [gosh_adamw_state_bytes(p.numel(), b) for p, b in zip(params, bits)]
+        starts = [0]
+        for size in sizes:
+            starts.append(starts[-1] + (size + 255) // 256 * 256)
+        memory = torch.zeros(starts[-1], dtype=torch.uint8, device=params[0].device if params else None)
+        states = [memory[a:a + size] for a, size in zip(starts, sizes)]
     states = list(states)
     if not count == len(grads) == len(states) == len(copies) == len(bits) == len(decay):
         raise ValueError("params, grads, states, copies, bits and weight_decay must be as many")

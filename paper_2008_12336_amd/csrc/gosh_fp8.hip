@@ -61,14 +61,28 @@ __device__ __forceinline__ float larger_of_16(float v) {  // v >= 0, whose bits 
   return __uint_as_float(larger_of_lanes<0x140>(b));
 }
 
-// A lane's 8 columns of 8 rows, from row, col on, as they lie in memory, all of them requested at once.
+// A lane's 8 columns of 8 rows, from row, col on, as they lie in memory, all of them requested at once.  Full: all are there.
+// Otherwise rows past the end read the last one and are made zero, and only lanes of fewer than 8 columns take them in
+// pieces (with a branch for each row and piece 517 x 132 in f16 took 7.1 us, now 5.0).
 template <typename T, bool Full>
 struct Square8 {
   typename Entries<T, 8>::Vec raw[8];
   __device__ __forceinline__ Square8(const Plane &x, int64_t row, int col, int64_t rows, int count) {
-    const typename T::Store *const p = static_cast<const typename T::Store *>(x.data) + row * x.ld + col;
+    typedef typename T::Store S;
+    const S *const p = static_cast<const S *>(x.data) + col;
+    const auto at = [&](int i) { return p + (Full || row + i < rows ? row + i : rows - 1) * x.ld; };
+    if (Full || count == 8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) raw[i] = Entries<T, 8>::fetch(p + i * x.ld, Full ? 8 : row + i < rows ? count : 0);
+      for (int i = 0; i < 8; ++i) raw[i] = Entries<T, 8>::fetch(at(i), 8);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) raw[i] = Entries<T, 8>::fetch(at(i), count);
+    }
+    if (!Full) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (row + i >= rows) raw[i] = 0;
+    }
   }
   __device__ __forceinline__ float at(int i, int e) const { return T::up(raw[i][e]); }
 };
@@ -78,13 +92,14 @@ struct PackedSquare8 {
   uint32_t q[8][2];
   float unit[8];
   __device__ __forceinline__ PackedSquare8(const Plane &x, int64_t row, int col, int64_t rows, int count) {
-    const int8_t *const p = static_cast<const int8_t *>(x.data) + row * x.ld + col;
-    const uint8_t *const e = x.exps + row * x.ld_exps + col / kGroup;
+    const int8_t *const p = static_cast<const int8_t *>(x.data) + col;
+    const uint8_t *const exps = x.exps + col / kGroup;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int here = Full ? 8 : row + i < rows ? count : 0;
-      load_bytes<8>(p + i * x.ld, here, q[i]);
-      unit[i] = here > 0 ? read_unit(e[i * x.ld_exps]) : 0.f;
+      const int64_t r = Full || row + i < rows ? row + i : rows - 1;
+      const bool there = Full || (row + i < rows && count > 0);
+      load_bytes<8>(p + r * x.ld, Full ? 8 : count, q[i]);
+      unit[i] = there ? read_unit(exps[r * x.ld_exps]) : 0.f;
     }
   }
   __device__ __forceinline__ float at(int i, int e) const {
@@ -122,7 +137,7 @@ __device__ __forceinline__ void load_square(const PackArgs &a, int64_t row, int 
 // Bound by memory: 131,072 x 1024 in bf16, as it is, takes 51 to 65 us (403 MB), 65,536 x 1024 both ways 65; with GELU's
 // slope, both ways and sums, 65,536 x 2048 take 170 us (805 MB, 4.7 TB/s; four wavefronts a SIMD instead of three spill and take 190).
 template <typename T, bool Square, bool Slope>
-__global__ __launch_bounds__(256, 3) void pack_fp8_kernel(const PackArgs a) {
+__global__ __launch_bounds__(256, Slope && T::kType == GOSH_F32 ? 2 : 3) void pack_fp8_kernel(const PackArgs a) {
   __shared__ __attribute__((aligned(16))) float most_of[16][kFp8Block];  // by rows' lanes and column
   __shared__ __attribute__((aligned(16))) float sum_of[Slope ? 16 : 1][kFp8Block];
   __shared__ __attribute__((aligned(16))) float inverse_of[kFp8Block];   // of the columns' units

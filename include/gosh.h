@@ -616,7 +616,8 @@ uint64_t gosh_linear_backward_workspace(int64_t rows, int32_t in, int32_t out, i
  * 0 <= rows < 2^31 - 1, 0 <= cols <= GOSH_FP8_MAX_LD; data 16-byte aligned, exps 4-byte aligned, both may be NULL without
  * entries; ld a multiple of 128, cols <= ld <= GOSH_FP8_MAX_LD; ld_exps a multiple of 4, at least ceil(cols / 128), at most
  * GOSH_FP8_MAX_LD.  The bytes from cols to the next multiple of 128 of each row are zero: gosh_pack_fp8 writes them, and the
- * products take them for entries.  Exponent bytes are 1 to 254.
+ * products take them for entries.  Exponent bytes are 1 to 254; those from ceil(cols / 128) to the next multiple of 4 of each
+ * row of them are read, whatever they hold.
  * gosh_pack_fp8 takes the smallest power of two, at least 2^-126, at which the block's largest finite magnitude is at most
  * 448, and rounds once, to the nearest, ties to even: half of 2^-3 of an entry's magnitude at most down to 2^-6 of the unit,
  * 2^-10 of the unit below.  An entry that is not finite becomes NaN. */

@@ -171,7 +171,9 @@ int loss_of(const LossArgs &a, hipStream_t st) {
   if (chunks <= 1024) return launch_loss<T, 256, 4>(a, st);
   if (chunks <= 1536) return launch_loss<T, 512, 3>(a, st);
   if (chunks <= 2048) return launch_loss<T, 512, 4>(a, st);
-  if (chunks <= 3072) return launch_loss<T, 1024, 3>(a, st);
+  // Three chunks a lane: 8,192 x 20,000 in bf16 115 us, 122 with four; near a full third it gains little (24,000: 133 and
+  // 137) or loses (12,000 in f32: 135 and 133).
+  if (chunks <= 2800) return launch_loss<T, 1024, 3>(a, st);
   if (chunks <= 4096) return launch_loss<T, 1024, 4>(a, st);
   if (chunks <= 6144) return launch_loss<T, 1024, 6>(a, st);
   if (chunks <= 8192) return launch_loss<T, 1024, 8>(a, st);

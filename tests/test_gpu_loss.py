@@ -15,7 +15,7 @@ pytestmark = pytest.mark.gpu
 SHAPES = [  # rows, classes, padding of the rows, entries off the start
     (1, 1, 0, 0), (1, 47, 0, 0), (5, 2, 1, 1), (300, 9, 0, 0), (7, 16, 3, 0), (1000, 33, 0, 1), (100, 64, 0, 0), (70, 100, 2, 3), (513, 250, 0, 0),
     (9, 257, 0, 0), (40, 513, 1, 0), (11, 1000, 0, 0), (6, 1025, 7, 1), (8, 2049, 0, 0), (3, 4096, 0, 0), (5, 5001, 0, 0), (2, 8193, 1, 1),
-    (3, 16385, 0, 0), (2, 20000, 0, 0), (2, 33001, 5, 0), (2, 65536, 0, 0), (70001, 12, 0, 0),
+    (3, 16385, 0, 0), (2, 20000, 0, 0), (2, 12001, 1, 0), (2, 25000, 0, 1), (2, 33001, 5, 0), (2, 65536, 0, 0), (70001, 12, 0, 0),
 ]
 
 

@@ -367,6 +367,30 @@ def test_offsets_past_32_bits():
     assert torch.equal(back, S.fp8(x[-128:].double().t().contiguous(), 1)[2])
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "f16"])
+def test_gradients_with_offsets_past_32_bits(dtype):
+    """The most rows that dw takes but for a piece of the last block; operands, workspace and dx are all longer than 2^32 bytes."""
+    rows, k, n, last = (1 << 23) - 51, 520, 524, 77
+    x, dy = torch.zeros(rows, k, dtype=dtype, device=DEV), torch.zeros(rows, n, dtype=dtype, device=DEV)
+    ends = torch.cat((torch.arange(128), torch.arange(rows - last, rows))).to(DEV)
+    rnd = gen(16)
+    x[ends], dy[ends] = rnd(128 + last, k).to(dtype), (0.1 * rnd(128 + last, n)).to(dtype)
+    xt, wt = G.PackedFp8(k, rows, 1, DEV), G.PackedFp8(k, n, 128, DEV)
+    G.gosh_pack_fp8(x, None, xt)
+    G.gosh_pack_fp8((rnd(n, k) / math.sqrt(k)).to(dtype), None, wt)
+    few = G.PackedFp8(k, 128 + last, 1, DEV)
+    G.gosh_pack_fp8(x[ends], None, few)
+    del x
+    dx, dw, db = torch.full((rows, k), MARK, dtype=dtype, device=DEV), torch.empty(n, k, device=DEV), torch.empty(n, device=DEV)
+    G.gosh_linear_fp8_backward(dy, xt, wt, None, H.NONE, dx=dx, dw=dw, db=db)
+    want, bounds = S.linear_fp8_backward(dy[ends].double(), values(few), values(wt).t(), None, H.NONE, dtype, dw.dtype)
+    within(dx[ends], want[0], H.rounded(bounds[0], want[0], dtype), "dx at the ends")
+    within(dw, want[1], H.rounded(bounds[1], want[1], dw.dtype), "dw")
+    within(db, want[2], H.rounded(bounds[2], want[2], torch.float32), "db")
+    for i in range(128, rows - last, 1 << 20):  # rows of zeros
+        assert not dx[i:min(i + (1 << 20), rows - last)].any()
+
+
 def test_refusals_on_the_device():
     x, y = torch.zeros(64, 32, device=DEV), torch.zeros(64, 16, device=DEV)
     x8, w8 = G.PackedFp8(64, 32, 1, DEV), G.PackedFp8(16, 32, 128, DEV)

@@ -111,7 +111,7 @@ __device__ __forceinline__ uint32_t most_of_block(const float (&v)[N]) {
 struct StepArgs {
   float beta1, rest1, beta2, rest2, eps, lr, log1, log2;
   float rate, root;  // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
-  uint32_t t;
+  int64_t t;
   const float *lr_dev, *scale;
   const int64_t *steps;
 };
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kThreads) void step_kernel(const Tensor *tensors, c
   const Chunk c = chunks[blockIdx.x];
   const Tensor t = tensors[c.tensor];
   float scale = 1.f, lr = a.lr, rate = a.rate, root = a.root;
-  uint32_t number = a.t;
+  uint32_t number = static_cast<uint32_t>(a.t);
   if (a.scale != nullptr) {
     scale = *a.scale;
     if (!(__builtin_fabsf(scale) < INFINITY)) return;
@@ -467,7 +467,7 @@ int gosh_adamw_step(void *optimiser, const gosh_adamw_options *options, void *hi
   a.log1 = static_cast<float>(std::log(q.beta1)), a.log2 = static_cast<float>(std::log(q.beta2));
   a.rate = static_cast<float>(q.lr / -std::expm1(t * std::log(q.beta1)));
   a.root = static_cast<float>(1 / std::sqrt(-std::expm1(t * std::log(q.beta2))));
-  a.t = static_cast<uint32_t>(q.step);
+  a.t = q.step;
   a.lr_dev = q.lr_dev, a.scale = q.scale, a.steps = q.steps;
   hipStream_t st = as_stream(hip_stream);
   if (int rc = in_launches(o, "AdamW", [&](dim3 grid, const Chunk *chunks) {

@@ -200,6 +200,23 @@ def test_number_rate_and_scale_on_the_device():
 
 
 @pytest.mark.parametrize("bits", [8, 32])
+def test_a_step_whose_number_passes_32_bits(bits):
+    """beta^t is 0 there: a rate from the device gives the same bits as one from the host, and the number of steps too."""
+    rnd = gen(8)
+    _, _, ps, gs = tensors([3000, 7], torch.float32, rnd)
+    lr, steps = torch.full((1,), HYPER["lr"], device=DEV), torch.full((1,), (1 << 32) - 1, dtype=torch.int64, device=DEV)
+    rest = {k: v for k, v in HYPER.items() if k != "lr"}
+    got = []
+    for how in (dict(lr=HYPER["lr"], step=1 << 32), dict(lr_dev=lr, step=1 << 32), dict(lr_dev=lr, steps=steps)):
+        qs = [p.clone() for p in ps]
+        opt = G.gosh_adamw_create(qs, gs, bits=bits)
+        G.gosh_adamw_step(opt, **how, **rest)
+        got.append(qs + opt.states)
+    assert int(steps) == 1 << 32 and all(torch.isfinite(q).all() for q in got[0][:2])
+    assert all(torch.equal(a, b) for other in got[1:] for a, b in zip(got[0], other))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
 def test_a_captured_graph_and_a_stream(bits):
     rnd = gen(11)
     _, _, ps, gs = tensors([9000, 5, 128], torch.bfloat16, rnd)

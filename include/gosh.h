@@ -605,9 +605,10 @@ uint64_t gosh_linear_backward_workspace(int64_t rows, int32_t in, int32_t out, i
 /* ---- the head in 8-bit floating point ------------------------------------------------------- */
 /* Linear layers whose operands are kept in 8 bits: twice the rate of 16 bits on the matrix cores, half of their bytes.  As
  * above: asynchronous, nothing allocated, the same bits for the same arguments.  Results are sums in 32 bits of exact
- * products; for those of GOSH_BF16 (but of a layer with GOSH_ACT_RELU) the matrix cores take eight products along the sum at a
- * time and cut off what is below 2^-13 of the largest: together less than 2^-10 of the magnitudes that are summed, typically
- * 2^-16. */
+ * products (an entry below 2^-133 may count as another, up to 2^-134 off); but for those of GOSH_BF16 (not of a layer with
+ * GOSH_ACT_RELU, and not where there are so few results that their rate does not matter) the matrix cores take eight products along
+ * the sum at a time and cut off what is below 2^-13 of the largest: together less than 2^-10 of the magnitudes that are summed,
+ * typically 2^-16. */
 
 /* Borrowed view of a rows x cols device matrix in 8-bit floating point.  data holds e4m3 entries q (a sign, 4 bits of
  * exponent, 3 of mantissa; largest 448, 0x7f and 0xff NaN), entry (r, c) at data[r * ld + c], and stands for

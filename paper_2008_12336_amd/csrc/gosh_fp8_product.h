@@ -68,13 +68,15 @@ __device__ __forceinline__ uint32_t pack_block(const Fp8Args &a, int64_t row, in
 // A product of few results has few tiles, whose blocks of k one after the other are a chain of waits for memory: here four or 16
 // wavefronts have a block each at a time, loaded by themselves.  (A training step of 512 x 256 -> 1024, products in tiles of 64 x
 // 64: forward 7.8 us, dx 6.8, dw 5.4.)
+// Products are exact whatever the type of the results: they are not what this waits for (1 x 512 -> 2048 in bf16 4.5 us and 4.6 with exact
+// products, 64 x 4096 -> 4096 14.1 and 14.1, 512 x 256 -> 1024 5.3 and 5.4, its gradient 13.7 and 13.8).
 // X: the type of the x, up to 32 rows, that is put into 8 bits on the way; or void.
 template <int Waves>
 struct FewLds {
   float parts[Waves - 1][16][64];
   float slab[Slab<32>::kFloats];
 };
-template <typename T, typename X, bool Exact, int Waves, ProductOut Out>
+template <typename T, typename X, int Waves, ProductOut Out>
 __device__ __forceinline__ void few_results(const Fp8Args &a, int64_t m0, int64_t n0, FewLds<Waves> &lds) {
   const ProductArgs &g = a.g;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -90,7 +92,7 @@ __device__ __forceinline__ void few_results(const Fp8Args &a, int64_t m0, int64_
     if constexpr (std::is_void<X>::value) ua = x.load(k, qa);
     else ua = pack_block<X>(a, lane & 31, k, n0 == 0, qa);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) acc[0][0] = fp8_mma<Exact>(qa[h], qb[h], ua, ub, acc[0][0]);
+    for (int h = 0; h < 2; ++h) acc[0][0] = fp8_mma<true>(qa[h], qb[h], ua, ub, acc[0][0]);
   }
   if (wave != 0) {
 #pragma unroll
@@ -104,10 +106,10 @@ __device__ __forceinline__ void few_results(const Fp8Args &a, int64_t m0, int64_
     for (int i = 0; i < 16; ++i) acc[0][0][i] += lds.parts[s][i][lane];
   finish<T, 1, 1, Out>(g, acc, lds.slab, m0, n0, 0);
 }
-template <typename T, typename X, bool Exact, int Waves, ProductOut Out>
+template <typename T, typename X, int Waves, ProductOut Out>
 __global__ __launch_bounds__(64 * Waves) void fp8_few_kernel(const Fp8Args a) {
   __shared__ __attribute__((aligned(16))) FewLds<Waves> lds;
-  few_results<T, X, Exact, Waves, Out>(a, static_cast<int64_t>(blockIdx.y) * 32, static_cast<int64_t>(blockIdx.x) * 32, lds);
+  few_results<T, X, Waves, Out>(a, static_cast<int64_t>(blockIdx.y) * 32, static_cast<int64_t>(blockIdx.x) * 32, lds);
 }
 
 // dx, dw and the sums of db's parts of a small layer in one launch: the workgroups of each after the others'.  (A training step of
@@ -118,12 +120,12 @@ __global__ __launch_bounds__(64 * Waves) void fp8_few_gradients_kernel(const Fp8
   unsigned id = blockIdx.x;
   const unsigned of_x = static_cast<unsigned>(x.g.tiles_m) * x.g.tiles_n, of_w = static_cast<unsigned>(w.g.tiles_m) * w.g.tiles_n;
   if (id < of_x) {
-    few_results<T, void, T::kType != GOSH_BF16, Waves, kStore>(x, id / x.g.tiles_n * int64_t{32}, id % x.g.tiles_n * int64_t{32}, lds);
+    few_results<T, void, Waves, kStore>(x, id / x.g.tiles_n * int64_t{32}, id % x.g.tiles_n * int64_t{32}, lds);
     return;
   }
   id -= of_x;
   if (id < of_w) {
-    few_results<W, void, W::kType != GOSH_BF16, Waves, kStore>(w, id / w.g.tiles_n * int64_t{32}, id % w.g.tiles_n * int64_t{32}, lds);
+    few_results<W, void, Waves, kStore>(w, id / w.g.tiles_n * int64_t{32}, id % w.g.tiles_n * int64_t{32}, lds);
     return;
   }
   const int64_t i = (id - of_w) * int64_t{64 * Waves} + threadIdx.x;
@@ -143,21 +145,21 @@ int launch_fp8_few_gradients(const Fp8Args &x, const Fp8Args &w, const JoinJob &
   return check_launch("gradients of a small layer in 8-bit floating point");
 }
 
-template <typename T, typename X, bool Exact, ProductOut Out>
+template <typename T, typename X, ProductOut Out>
 int launch_fp8_few(const Fp8Args &a, hipStream_t st) {
   const dim3 grid(static_cast<unsigned>(ceil_div(a.g.N, 32)), static_cast<unsigned>(ceil_div(a.g.M, 32)));
-  if (few_waves(a.g.K) == 4) fp8_few_kernel<T, X, Exact, 4, Out><<<grid, dim3(256), 0, st>>>(a);
-  else fp8_few_kernel<T, X, Exact, 16, Out><<<grid, dim3(1024), 0, st>>>(a);
+  if (few_waves(a.g.K) == 4) fp8_few_kernel<T, X, 4, Out><<<grid, dim3(256), 0, st>>>(a);
+  else fp8_few_kernel<T, X, 16, Out><<<grid, dim3(1024), 0, st>>>(a);
   return check_launch("product of few results in 8-bit floating point");
 }
-template <typename T, bool Exact, ProductOut Out>
+template <typename T, ProductOut Out>
 int launch_fp8_few(const Fp8Args &a, hipStream_t st) {
   if constexpr (Out == kForward) {
-    if (a.pack.data != nullptr && a.pack_type == GOSH_F32) return launch_fp8_few<T, F32, Exact, Out>(a, st);
-    if (a.pack.data != nullptr && a.pack_type == GOSH_BF16) return launch_fp8_few<T, Bf16, Exact, Out>(a, st);
-    if (a.pack.data != nullptr) return launch_fp8_few<T, F16, Exact, Out>(a, st);
+    if (a.pack.data != nullptr && a.pack_type == GOSH_F32) return launch_fp8_few<T, F32, Out>(a, st);
+    if (a.pack.data != nullptr && a.pack_type == GOSH_BF16) return launch_fp8_few<T, Bf16, Out>(a, st);
+    if (a.pack.data != nullptr) return launch_fp8_few<T, F16, Out>(a, st);
   }
-  return launch_fp8_few<T, void, Exact, Out>(a, st);
+  return launch_fp8_few<T, void, Out>(a, st);
 }
 
 // ---- many tiles: straight to LDS ------------------------------------------------------------------------
@@ -433,7 +435,7 @@ int launch_fp8_out(const Fp8Args &a, hipStream_t st) {
     default: break;
   }
   if constexpr (Out != kParts)
-    if (a.tile == 32) return launch_fp8_few<T, Exact, Out>(a, st);
+    if (a.tile == 32) return launch_fp8_few<T, Out>(a, st);
   return launch_fp8_tiles<T, kSmall, Exact, Out>(a, st);
 }
 

@@ -311,8 +311,8 @@ int product_fp8(int32_t type, ProductOut out, const Fp8Args &a, hipStream_t st) 
 }
 
 constexpr int64_t kTilesPerLaunch = int64_t{1} << 22;
-// Bytes of y from which it is stored past the caches, where nothing else is written: the 256 MB of the cache beside the memory.
-// 131,072 x 1024 -> 4096 (1.07 GB): 727 us, 643 with it.
+// Bytes of y from which it, and z with it, is stored past the caches: the 256 MB of the cache beside the memory.  131,072 x 1024 ->
+// 4096 (1.07 GB): 727 us, 643 with it.  By tiles of 256 alone; exact products (f16, f32, ReLU) have none here and store through the caches.
 constexpr int64_t kPastCaches = int64_t{256} << 20;
 
 constexpr int64_t kFewRows = 32;  // that are put into 8 bits in the product's launch
@@ -322,13 +322,12 @@ constexpr int64_t kFewRows = 32;  // that are put into 8 bits in the product's l
 // 8192 x 512 -> 512: 21.8, 14.0, 9.6, 17.2; 131,072 x 128 -> 128: 33.5, 35.5, 17.6, 32.5; 65,536 x 512 -> 512: 124, 89, 40.7, 34.6).
 // A CU works on four tiles of 64 together, two of 128 or one of 256; each has its way out, and steps that are as long as a load
 // is under way where it is alone.
-// Exact products (see fp8_mma; 50,021 x 260 -> 1037 in f32: 123, 96 and 105 us; 65,536 x 1024 -> 1024 in f16: 273, 158 and 169)
-// take longer, the largest tiles the most.
+// Exact products in tiles (see fp8_mma; 50,021 x 260 -> 1037 in f32 with 64 and 128: 123 and 96 us; 65,536 x 1024 -> 1024 in f16: 273
+// and 158) take longer.  In tiles of 256 they took 105 and 169, by their times never the least, and are there for dw alone.
 double fp8_time(int tile, int64_t tiles, int64_t blocks, bool exact) {
   const double k = static_cast<double>(blocks), per_cu = static_cast<double>(ceil_div(tiles, 256));
   if (tile == 32) return few_waves(blocks) == 4 ? 4.0 + per_cu * (0.5 + 0.12 * k) : 3.7 + per_cu * 0.32 * k;
   const double held = tile == 256 ? 1 : tile == 128 ? 2 : 4, together = std::min(per_cu, held), turns = std::ceil(per_cu / held);
-  if (exact && tile == 256) return 2.0 + turns * (17.0 + 2.9 * k);
   if (exact && tile == 128) return 2.0 + turns * (together > 1 ? 8.0 + 1.4 * k : 5.0 + 1.3 * k);
   if (exact) return 1.5 + turns * (2.5 + together + k * (0.4 + 0.25 * together));
   if (tile == 256) return 2.0 + turns * (10.0 + 1.2 * k);
@@ -339,6 +338,7 @@ int fp8_tile_for(int64_t M, int64_t N, int64_t blocks, bool exact) {
   int best = 0;
   double least = 0;
   for (int s : {256, 128, 64, 32}) {
+    if (s == 256 && exact) continue;
     if (s == 32 && M > 65535 * 32) continue;  // a grid's rows
     const double time = fp8_time(s, ceil_div(M, s) * ceil_div(N, s), blocks, exact);
     if (best == 0 || time < least) best = s, least = time;
@@ -372,7 +372,9 @@ int product_of_rows_fp8(int32_t type, ProductOut out, Fp8Args a, int64_t rows, h
 uint64_t round_up(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // How dw is split along the rows: the parts are written and read again, at 5 TB/s.  Few results (32) are not split; what is not is
-// stored as it is.
+// stored as it is.  By the times of products that are not exact, whatever dw's type: with those of exact ones, which are of the forward
+// pass, 65,536 x 1024 -> 2048 in f16 takes 330 us (with the pass over dy; 306 by these, in tiles of 256), 4,096 x 512 -> 512 18.6 (17.0), and
+// 16,384 x 2048 -> 4096, 8,192 x 1024 -> 1024 and 32,768 x 512 -> 512 take the same.
 struct Fp8DwPlan {
   int32_t tile, tiles_m, tiles_n, splits;
   int64_t blocks_per_split;

@@ -418,7 +418,7 @@ __global__ __launch_bounds__(64 * direct_waves(BN), 8 / direct_waves(BN)) void f
 template <typename T, TileSize Size, bool Exact, ProductOut Out>
 int launch_fp8_tiles(const Fp8Args &a, hipStream_t st) {
   constexpr int kTile = tile_m(Size), kWaves = direct_waves(kTile);
-  if constexpr (Size == kLarge && Out == kForward && T::kType != GOSH_F32)
+  if constexpr (Size == kLarge && Out == kForward)
     if (a.g.forward.past)
       return a.g.forward.z.data == nullptr ? launch_fp8_tiles<T, Size, Exact, kPast>(a, st) : launch_fp8_tiles<T, Size, Exact, kPastZ>(a, st);
   const unsigned blocks = static_cast<unsigned>(a.g.tiles_m) * a.g.tiles_n * a.g.splits;
@@ -429,11 +429,12 @@ int launch_fp8_tiles(const Fp8Args &a, hipStream_t st) {
 
 template <typename T, bool Exact, ProductOut Out>
 int launch_fp8_out(const Fp8Args &a, hipStream_t st) {
-  switch (a.tile) {
-    case 256: return launch_fp8_tiles<T, kLarge, Exact, Out>(a, st);
-    case 128: return launch_fp8_tiles<T, kMiddle, Exact, Out>(a, st);
-    default: break;
+  if constexpr (!Exact || Out != kForward) {  // see fp8_time
+    if (a.tile == 256) return launch_fp8_tiles<T, kLarge, Exact, Out>(a, st);
+  } else if (a.tile == 256) {
+    return fail(GOSH_EINVAL, "no exact forward products in tiles of 256");
   }
+  if (a.tile == 128) return launch_fp8_tiles<T, kMiddle, Exact, Out>(a, st);
   if constexpr (Out != kParts)
     if (a.tile == 32) return launch_fp8_few<T, Out>(a, st);
   return launch_fp8_tiles<T, kSmall, Exact, Out>(a, st);

@@ -33,10 +33,10 @@
 
 namespace gosh {
 
-// kPast: kForward of y alone, in tiles of kLarge, past the caches.  (A kernel of its own: as a branch at each store it
+// kPast: kForward of y alone, in tiles of kLarge, y stored past the caches.  (A kernel of its own: as a branch at each store it
 // cost the other calls 2 to 20 %, in registers.  kForward, with every optional output, has 112 scalar registers in lanes of
 // vector ones there, kPast 18: 131,072 x 512 -> 1024 with SiLU takes 180 us, 214 with z and 226 with a packed z.)
-// kPastZ: kPast with z beside y.
+// kPastZ: kPast with z beside y, a z that is not packed past the caches too.
 enum ProductOut : int { kForward, kStore, kParts, kPast, kPastZ };
 constexpr bool is_forward(ProductOut out) { return out == kForward || out == kPast || out == kPastZ; }
 

@@ -28,6 +28,7 @@ GOSH_ACT_NONE, GOSH_ACT_RELU, GOSH_ACT_GELU, GOSH_ACT_SILU = 0, 1, 2, 3
 GOSH_MAT_MAX_COLS = 65536
 GOSH_MAT_MAX_LD = 1048576
 GOSH_FP8_MAX_LD = 8388608
+GOSH_FP8_EXACT = 256
 GOSH_MAX_NEG = 15
 GOSH_STATIC_MAX_N = 1 << 26
 
@@ -814,6 +815,10 @@ def _fp8(m, name: str):
     return m._fp8(name)
 
 
+def _act(act: int, exact: bool) -> int:
+    return act | GOSH_FP8_EXACT if exact else act
+
+
 def gosh_pack_fp8(x: torch.Tensor, q: PackedFp8 = None, qt: PackedFp8 = None, stream=None) -> None:
     """x in 8-bit floating point: as it is into q, transposed into qt."""
     _check(lib().gosh_pack_fp8(_mat(x, "x"), _fp8(q, "q"), _fp8(qt, "qt"), _stream(stream)))
@@ -824,14 +829,14 @@ def gosh_unpack_fp8(q: PackedFp8, x: torch.Tensor, stream=None) -> None:
 
 
 def gosh_linear_fp8(x, x8: PackedFp8, w: PackedFp8, y: torch.Tensor, bias=None, act: int = GOSH_ACT_NONE, residual=None, z=None,
-                    stream=None) -> None:
+                    exact: bool = False, stream=None) -> None:
     """y = act(x8 w^T + bias) + residual, after x was put into x8; x None: x8 holds it.  z: a tensor or a Packed8 that
-    receives x8 w^T + bias."""
+    receives x8 w^T + bias.  exact: sums of exact products for bfloat16 results too, at half the rate."""
     v = _fp8(w, "w")
     if v is None:
         raise TypeError("w must be a PackedFp8")
-    _check(lib().gosh_linear_fp8(_mat(x, "x"), _fp8(x8, "x8"), v, _floats(bias, "bias", v.rows), act, _mat(residual, "residual"),
-                                 _mat(y, "y"), _mat(z, "z"), _stream(stream)))
+    _check(lib().gosh_linear_fp8(_mat(x, "x"), _fp8(x8, "x8"), v, _floats(bias, "bias", v.rows), _act(act, exact),
+                                 _mat(residual, "residual"), _mat(y, "y"), _mat(z, "z"), _stream(stream)))
 
 
 def gosh_linear_fp8_backward_workspace(rows: int, in_: int, out: int) -> int:
@@ -839,14 +844,14 @@ def gosh_linear_fp8_backward_workspace(rows: int, in_: int, out: int) -> int:
 
 
 def gosh_linear_fp8_backward(dy: torch.Tensor, xt, wt, z, act: int = GOSH_ACT_NONE, dx=None, dw=None, db=None, workspace=None,
-                             stream=None) -> None:
+                             exact: bool = False, stream=None) -> None:
     """dx, dw and db (those that are given, dx or dw among them) of gosh_linear_fp8, from x and w transposed in 8 bits."""
     v = _mat(dy, "dy")
     into = dx if dx is not None else dw
     nbytes = 0 if into is None else gosh_linear_fp8_backward_workspace(v.rows, into.shape[1], v.cols)
     workspace = _workspace(workspace, nbytes, stream, dy.device)
-    _check(lib().gosh_linear_fp8_backward(v, _fp8(xt, "xt"), _fp8(wt, "wt"), _mat(z, "z"), act, _mat(dx, "dx"), _mat(dw, "dw"),
-                                          _floats(db, "db", v.cols), workspace.data_ptr() or None, workspace.numel(),
+    _check(lib().gosh_linear_fp8_backward(v, _fp8(xt, "xt"), _fp8(wt, "wt"), _mat(z, "z"), _act(act, exact), _mat(dx, "dx"),
+                                          _mat(dw, "dw"), _floats(db, "db", v.cols), workspace.data_ptr() or None, workspace.numel(),
                                           _stream(stream)))
 
 

@@ -33,7 +33,7 @@ struct Fp8Args {
   int32_t tile;    // side of a tile: 64, 128 or 256; or 32: few results (not for kParts)
   Plane pack;      // up to 32 rows of kForward: x of pack_type and pack_cols columns that is put into 8 bits first, or null
   int32_t pack_type, pack_cols;
-  int32_t exact;   // kForward in bf16, in tiles: see fp8_mma
+  int32_t exact;   // bf16 results in tiles, not kParts: see fp8_mma
   uint32_t by_all, by_group;  // reciprocals of the tiles of a split and of a group: set_reciprocals
 };
 
@@ -110,7 +110,7 @@ __device__ __forceinline__ S8 widened(uint32_t lo, uint32_t hi, float unit) {
 // take it where that rate counts: products in tiles.  It is more than half a step of f16 or f32, which are exact, and so is a layer
 // with ReLU, whose slope jumps with z's sign: 20,011 x 132 -> 517 had a z in 100,000 on the other side of 0, and db ended 0.4 % of its
 // rms off.
-// What it does to a step of 65,536 x 1024 -> 2048, beside 64 bits: y 1.665e-3 of its norm off (half a step of bf16), with exact products
+// GOSH_FP8_EXACT asks for exact ones.  What the others do to a step of 65,536 x 1024 -> 2048, beside 64 bits: y 1.665e-3 of its norm off (half a step of bf16), with exact products
 // 1.664e-3; dx and dw 1.81e-3 and 1.66e-3, since a z that bf16 rounds to its other neighbour moves dz's 8 bits.  The forward product
 // takes 194 us, an exact one 321.
 template <bool Exact>

@@ -369,6 +369,13 @@ int product_of_rows_fp8(int32_t type, ProductOut out, Fp8Args a, int64_t rows, h
   return GOSH_OK;
 }
 
+// Whether GOSH_FP8_EXACT is in act, which it is taken out of.
+bool take_exact(int32_t &act) {
+  const bool exact = act >= 0 && (act & GOSH_FP8_EXACT) != 0;
+  if (exact) act -= GOSH_FP8_EXACT;
+  return exact;
+}
+
 uint64_t round_up(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // How dw is split along the rows: the parts are written and read again, at 5 TB/s.  Few results (32) are not split; what is not is
@@ -471,6 +478,7 @@ int gosh_linear_fp8(const gosh_mat *x, const gosh_fp8 *x8, const gosh_fp8 *w, co
   if (int rc = check_mat(y, "y")) return rc;
   if (int rc = check_mat(residual, "residual", kOptional)) return rc;
   if (int rc = check_mat(z, "z", kOptional | kMayBePacked)) return rc;
+  const bool exact = take_exact(act);
   if (act < GOSH_ACT_NONE || act > GOSH_ACT_SILU) return fail(GOSH_EINVAL, "act = %d: no activation", act);
   if (w->rows < 1 || w->rows > GOSH_MAT_MAX_COLS)
     return fail(GOSH_EINVAL, "w: rows = %lld: must be in [1, %d]", (long long)w->rows, GOSH_MAT_MAX_COLS);
@@ -492,7 +500,7 @@ int gosh_linear_fp8(const gosh_mat *x, const gosh_fp8 *x8, const gosh_fp8 *w, co
   Fp8Args a{};
   a.x = fp8_plane(x8);
   a.w = fp8_plane(w);
-  a.exact = act == GOSH_ACT_RELU;
+  a.exact = exact || act == GOSH_ACT_RELU;
   a.g.N = out;
   a.g.K = ceil_div(in, kFp8Block);
   a.g.forward = ForwardOut{bias, plane_of(residual), plane_of(y), plane_of(z), Plane{nullptr, nullptr, 0, 0}, act, z != nullptr && z->packed,
@@ -519,6 +527,7 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
   if (int rc = check_mat(dy, "dy")) return rc;
   if (int rc = check_fp8(xt, "xt", dw == nullptr ? kOptional : 0)) return rc;
   if (int rc = check_fp8(wt, "wt", dx == nullptr ? kOptional : 0)) return rc;
+  const bool exact = take_exact(act);
   if (act < GOSH_ACT_NONE || act > GOSH_ACT_SILU) return fail(GOSH_EINVAL, "act = %d: no activation", act);
   if (int rc = check_mat(z, "z", kMayBePacked | (act == GOSH_ACT_NONE ? kOptional : 0))) return rc;
   if (int rc = check_mat(dx, "dx", kOptional)) return rc;
@@ -559,6 +568,7 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
     if (int rc = pack_fp8(dy->type, a, false, true, st)) return rc;
   }
   Fp8Args gx{}, gw{};
+  gx.exact = gw.exact = exact;
   if (dx != nullptr) {
     gx.x = Fp8Plane{ws + p.q, ws + p.exps, p.ld, p.ld_exps, 0, kFp8Block};
     gx.w = fp8_plane(wt);
@@ -583,7 +593,7 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
   }
   const JoinJob db_job{sums, out, db != nullptr ? out : 0, out, db, static_cast<int32_t>(ceil_div(rows, kFp8Block)), out, GOSH_F32};
   const bool few = rows > 0 && dw != nullptr && p.dw.tile == 32;
-  if (few && (dx == nullptr || fp8_tile_for(rows, in, gx.g.K, dy->type != GOSH_BF16) == 32)) {
+  if (few && (dx == nullptr || fp8_tile_for(rows, in, gx.g.K, dy->type != GOSH_BF16 || exact) == 32)) {
     if (dx != nullptr) {
       gx.g.M = rows;
       gx.g.tiles_m = static_cast<int32_t>(ceil_div(rows, 32));
@@ -600,7 +610,7 @@ int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_
   if (dw != nullptr && rows > 0) {
     // parts are in 32 bits: here the type says by which products
     if (int rc = p.dw.splits == 1 ? product_fp8(dw->type, kStore, gw, st)
-                     : dw->type == GOSH_BF16 ? launch_fp8<Bf16>(kParts, gw, st) : launch_fp8<F32>(kParts, gw, st))
+                     : dw->type == GOSH_BF16 && !exact ? launch_fp8<Bf16>(kParts, gw, st) : launch_fp8<F32>(kParts, gw, st))
       return rc;
   }
   if (dw != nullptr && (rows == 0 || p.dw.splits > 1)) {

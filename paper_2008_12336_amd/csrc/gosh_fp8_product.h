@@ -444,7 +444,7 @@ template <typename T>
 int launch_fp8_any(ProductOut out, const Fp8Args &a, hipStream_t st) {
   constexpr bool exact = T::kType != GOSH_BF16;
   if (out == kForward) return a.exact ? launch_fp8_out<T, true, kForward>(a, st) : launch_fp8_out<T, exact, kForward>(a, st);
-  if (out == kStore) return launch_fp8_out<T, exact, kStore>(a, st);
+  if (out == kStore) return a.exact ? launch_fp8_out<T, true, kStore>(a, st) : launch_fp8_out<T, exact, kStore>(a, st);
   if constexpr (T::kType != GOSH_F16) return launch_fp8_out<T, exact, kParts>(a, st);
   return fail(GOSH_EINVAL, "parts are of F32 or Bf16");
 }

@@ -4,7 +4,9 @@ import torch
 
 import paper_2008_12336_amd as G
 from tests import head_model as H
-from tests.test_gpu_head import DEV
+from tests import step_model as S
+from tests.test_gpu_fp8 import values
+from tests.test_gpu_head import DEV, gen, within
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +54,51 @@ def test_gradients_of_few_results_lose_nothing(rows, k, n, dtype):
     dw = torch.zeros(n, k, dtype=dtype, device=DEV)
     G.gosh_linear_fp8_backward(dy.t().contiguous().to(dtype), xt, None, None, H.NONE, dw=dw)
     assert (dw == torch.tensor(of_w).to(dtype).to(DEV)).all()
+
+
+@pytest.mark.parametrize("rows, k, n", [(9000, 520, 1030), (700, 2048, 130), (33000, 264, 520)])
+def test_exact_sums_of_bfloat16_results_on_request(rows, k, n):
+    """In tiles of every kind: dx and the results of the layer; dw split along the rows or not, in either type."""
+    t = torch.bfloat16
+    x, w, want = cancelling(rows, k, k)
+    y = torch.zeros(rows, n, dtype=t, device=DEV)
+    for given in (x.to(t), None):
+        G.gosh_linear_fp8(given, forms(x)[0], forms(w.repeat(n, 1), 128)[0], y, act=H.RELU, exact=True)
+        assert (y == torch.tensor(want).to(t).to(DEV)).all()
+        y.zero_()
+        G.gosh_linear_fp8(given, forms(x)[0], forms(w.repeat(n, 1), 128)[0], y, exact=True)
+        assert (y == torch.tensor(want).to(t).to(DEV)).all()
+    dy, v, of_x = cancelling(rows, n, 1)
+    dx = torch.zeros(rows, k, dtype=t, device=DEV)
+    G.gosh_linear_fp8_backward(dy.to(t), None, forms(v[:, None].repeat(1, k), 128)[1], None, H.NONE, dx=dx, exact=True)
+    assert (dx == torch.tensor(of_x).to(t).to(DEV)).all()
+    dy, u, of_w = cancelling(n, rows, 2)
+    xt = forms(u[:, None].repeat(1, k))[1]
+    for kind in (t, torch.float32):
+        dw = torch.zeros(n, k, dtype=kind, device=DEV)
+        G.gosh_linear_fp8_backward(dy.t().contiguous().to(t), xt, None, None, H.NONE, dw=dw, exact=True)
+        assert (dw == torch.tensor(of_w).to(kind).to(DEV)).all()
+
+
+@pytest.mark.parametrize("rows, k, n", [(300, 97, 131), (9000, 520, 1030), (2000, 2000, 3000)])
+def test_exact_layers_have_the_bounds_of_32_bits(rows, k, n):
+    """Those of step_model.py without what the matrix cores cut off, and as f16 and f32 results are by themselves."""
+    rnd, t = gen(rows), torch.bfloat16
+    x, w, b, dy = rnd(rows, k) * torch.exp(rnd(rows, 1)), rnd(n, k) / k ** 0.5, 0.3 * rnd(n), 0.1 * rnd(rows, n)
+    (x8, xt), (w8, wt) = forms(x.to(t)), forms(w.to(t), 128)
+    y, z, dx, dw = (torch.zeros(*s, dtype=t, device=DEV) for s in ((rows, n), (rows, n), (rows, k), (n, k)))
+    db = torch.zeros(n, device=DEV)
+    G.gosh_linear_fp8(None, x8, w8, y, bias=b, act=H.GELU, z=z, exact=True)
+    wy, wz, ey, ez = S.linear_fp8(values(x8), values(w8), b.double(), H.GELU, None, torch.float32)
+    within(y, wy, H.rounded(ey, wy, t), "y")
+    within(z, wz, H.rounded(ez, wz, t), "z")
+    G.gosh_linear_fp8_backward(dy.to(t), xt, wt, z, H.GELU, dx=dx, dw=dw, db=db, exact=True)
+    want, bound = S.linear_fp8_backward(dy.to(t).double(), values(xt), values(wt).t(), z.double(), H.GELU, torch.float32, torch.float32)
+    within(dx, want[0], H.rounded(bound[0], want[0], t), "dx")
+    within(dw, want[1], H.rounded(bound[1], want[1], t), "dw")
+    within(db, want[2], H.rounded(bound[2], want[2], torch.float32), "db")
+    for other in (torch.float16, torch.float32):  # they are exact anyway
+        out = [torch.zeros(rows, n, dtype=other, device=DEV) for _ in range(2)]
+        for o, e in zip(out, (False, True)):
+            G.gosh_linear_fp8(None, x8, w8, o, bias=b, act=H.GELU, exact=e)
+        assert torch.equal(*out)

@@ -40,9 +40,15 @@ class LinkHead:
         self.rstd = torch.empty(rows, device=DEV)
         self.xhat8, self.h8, self.z8, self.a8 = eight(dim), eight(dim), eight(wide), eight(wide)
 
+    def weights(self) -> dict:
+        """The weights as the layers read them, from the parameters as they are."""
+        return {name: self.params[name].to(self.dtype) for name in ("w1", "w2", "w3")}
+
     def optimiser(self):
-        """AdamW over all parameters, which keeps the copies up to date."""
+        """AdamW over all parameters, which keeps the copies up to date from here on: with every step it takes."""
         names = list(self.params)
+        for name, w in self.weights().items():
+            self.copies[name].copy_(w)
         return G.gosh_adamw_create([self.params[n] for n in names], [self.grads[n] for n in names], bits=8,
                                    copies=[self.copies.get(n) for n in names])
 
@@ -66,7 +72,7 @@ class LinkHead:
 
     def score(self, x: torch.Tensor) -> torch.Tensor:
         """Logits of any number of pairs, nothing kept."""
-        p, w, n = self.params, self.copies, x.shape[0]
+        p, w, n = self.params, self.weights(), x.shape[0]
         new = lambda k: torch.empty(n, k, dtype=self.dtype, device=DEV)  # noqa: E731
         h, a, o, s = new(x.shape[1]), new(4 * x.shape[1]), new(x.shape[1]), new(1)
         G.gosh_layer_norm(x, p["gamma"], p["beta"], h)

@@ -32,7 +32,7 @@ class LinkHead:
         self.params = dict(gamma=torch.ones(dim, device=DEV), beta=zeros(dim), w1=init(wide, dim), b1=zeros(wide),
                            w2=0.1 * init(dim, wide), b2=zeros(dim), w3=init(1, dim), b3=zeros(1))
         self.grads = {name: torch.empty_like(p) for name, p in self.params.items()}
-        self.copies = {name: self.params[name].to(dtype) for name in ("w1", "w2", "w3")}
+        self.copies = self.weights()  # of float32: the parameters themselves
         act = lambda n: torch.empty(rows, n, dtype=dtype, device=DEV)  # noqa: E731
         eight = lambda n: G.Packed8(rows, n, dtype, DEV)  # noqa: E731
         self.h, self.a, self.o, self.s = act(dim), act(wide), act(dim), act(1)
@@ -49,8 +49,8 @@ class LinkHead:
         names = list(self.params)
         for name, w in self.weights().items():
             self.copies[name].copy_(w)
-        return G.gosh_adamw_create([self.params[n] for n in names], [self.grads[n] for n in names], bits=8,
-                                   copies=[self.copies.get(n) for n in names])
+        copies = None if self.dtype == torch.float32 else [self.copies.get(n) for n in names]
+        return G.gosh_adamw_create([self.params[n] for n in names], [self.grads[n] for n in names], bits=8, copies=copies)
 
     def forward(self, x: torch.Tensor, w: dict) -> torch.Tensor:
         """The logits of `rows` pairs' features."""

@@ -2,7 +2,9 @@
 import pytest
 import torch
 
-from tests.test_gpu_head import DEV, gen
+import paper_2008_12336_amd as G
+from tests import head_model as H
+from tests.test_gpu_head import DEV, gen, within
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +25,36 @@ def test_scores_are_those_of_the_parameters_of_that_moment():
         p.zero_()
     head.params["b3"].fill_(2.5)
     assert (head.score(x) == 2.5).all()
+
+
+def in_64_bits(head, x):
+    """The logits, and how far they may be off: each layer by its own bound (twice: its inputs are off too, by less than their
+    magnitudes) and its rounding, and by what its inputs are off times the weights' magnitudes (GELU: at most 1.13 of that)."""
+    p, w, t = {n: v.double() for n, v in head.params.items()}, {n: v.double() for n, v in head.weights().items()}, head.dtype
+    (h, *_), (e, *_) = H.norm(x.double(), p["gamma"], p["beta"], 1e-5)
+    e = H.rounded(e, h, t)
+    for layer, kind, residual in ((1, H.GELU, None), (2, H.NONE, x.double()), (3, H.NONE, None)):
+        y, _, ey, _ = H.linear(h, w[f"w{layer}"], p[f"b{layer}"], kind, residual)
+        h, e = y, H.rounded(2 * ey + 1.13 * (e @ w[f"w{layer}"].abs().t()), y, t)
+    return h[:, 0], e[:, 0]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=["f32", "bf16", "f16"])
+def test_a_head_of_any_type_takes_steps(dtype):
+    from paper_2008_12336_amd.examples.link_head import LinkHead
+
+    rows, dim = 300, 32
+    head, x = LinkHead(dim, rows, dtype=dtype), gen(2)(rows, dim).to(dtype)
+    target = (torch.arange(rows, device=DEV) % 2).float()
+    opt = head.optimiser()
+    for step in (1, 2):
+        before = {n: p.clone() for n, p in head.params.items()}
+        s = head.forward(x, head.copies).float()
+        head.backward(((torch.sigmoid(s) - target) / rows).to(dtype), head.copies)
+        G.gosh_adamw_step(opt, lr=1e-3, step=step)
+        for n, p in head.params.items():
+            assert (p != before[n]).any(), n
+            assert n not in head.copies or torch.equal(head.copies[n], p.to(dtype)), n
+    want, bound = in_64_bits(head, x)
+    within(head.score(x), want, bound, "score")  # the layers that keep nothing for a backward pass
+    within(head.forward(x, head.copies).float(), want, bound, "logits")

@@ -907,8 +907,9 @@ def gosh_adamw_state_bytes(n: int, bits: int) -> int:
     return int(lib().gosh_adamw_state_bytes(n, bits))
 
 
-def gosh_adamw_create(params, grads, bits=8, states=None, copies=None, weight_decay=0.0) -> AdamW:
-    """params: float32 tensors; grads: theirs, of any type of the head.  bits (8 or 32) and weight_decay: of all, or a list.
+def gosh_adamw_create(params, grads, bits=32, states=None, copies=None, weight_decay=0.0) -> AdamW:
+    """params: float32 tensors; grads: theirs, of any type of the head.  bits (of the moments: 32, or 8) and weight_decay:
+    of all, or a list.
     states: uint8 tensors of gosh_adamw_state_bytes, or None for new ones, zero.  copies: None, or a list of bfloat16 or float16
     tensors (or None) that receive the parameters rounded."""
     params, grads = list(params), list(grads)

@@ -1,13 +1,13 @@
 """A link predictor on an embedding, trained with 8-bit activations: embeds a synthetic graph, trains a small head on
 products of the rows of vertex pairs, and says how well it tells held-out edges from pairs that are none.
 
-    python -m paper_2008_12336_amd.examples.link_head [--scale 14] [--dim 64] [--steps 200]
+    python -m paper_2008_12336_amd.examples.link_head [--scale 14] [--dim 64] [--steps 200] [--bits 32]
 
 The head is layer norm (rows of hubs are orders of magnitude longer than others), a linear layer with GELU to four
 times the width, one back with the features added, and one to a single logit.  Between the passes it keeps the normalised
 rows, the layers' inputs and the pre-activations in 8 bits, a byte an entry, of which the backward calls read them.  The
-optimiser keeps its moments in 8 bits too and writes the weights' 16-bit copies, of which the layers read them.  torch holds the
-parameters and takes the loss; every operator of the head and its optimiser is one of the library's kernels."""
+optimiser keeps its moments in 32 bits, or in 8 with --bits 8, and writes the weights' 16-bit copies, which the layers read.  torch
+holds the parameters and takes the loss; every operator of the head and its optimiser is one of the library's kernels."""
 from __future__ import annotations
 
 import argparse
@@ -44,13 +44,14 @@ class LinkHead:
         """The weights as the layers read them, from the parameters as they are."""
         return {name: self.params[name].to(self.dtype) for name in ("w1", "w2", "w3")}
 
-    def optimiser(self):
-        """AdamW over all parameters, which keeps the copies up to date from here on: with every step it takes."""
+    def optimiser(self, bits: int = 32):
+        """AdamW over all parameters, moments in 32 or 8 bits, which keeps the copies up to date from here on: with every step it
+        takes."""
         names = list(self.params)
         for name, w in self.weights().items():
             self.copies[name].copy_(w)
         copies = None if self.dtype == torch.float32 else [self.copies.get(n) for n in names]
-        return G.gosh_adamw_create([self.params[n] for n in names], [self.grads[n] for n in names], bits=8, copies=copies)
+        return G.gosh_adamw_create([self.params[n] for n in names], [self.grads[n] for n in names], bits=bits, copies=copies)
 
     def forward(self, x: torch.Tensor, w: dict) -> torch.Tensor:
         """The logits of `rows` pairs' features."""
@@ -93,8 +94,8 @@ def auc(pos: torch.Tensor, neg: torch.Tensor) -> float:
     return float(below.double().mean() / (2 * neg.numel()))
 
 
-def train(scale: int = 14, dim: int = 64, steps: int = 200, rows: int = 16384, seed: int = 1):
-    """(held-out AUC before training, after it, the loss of every step)."""
+def train(scale: int = 14, dim: int = 64, steps: int = 200, rows: int = 16384, seed: int = 1, bits: int = 32):
+    """(held-out AUC before training, after it, the loss of every step); bits: of the optimiser's moments."""
     n = 1 << scale
     edges = graphgen.rmat(scale, 16 << scale, seed=seed)
     kept, held = (e.long() for e in graphgen.holdout_split(edges, 0.1, seed + 1000))
@@ -113,7 +114,7 @@ def train(scale: int = 14, dim: int = 64, steps: int = 200, rows: int = 16384, s
     head = LinkHead(dim, rows, seed=seed)
     test_pos, test_neg = (features(M, p, unit, head.dtype) for p in (held, none(held.shape[0])))
     before = auc(head.score(test_pos), head.score(test_neg))
-    optimiser = head.optimiser()
+    optimiser = head.optimiser(bits)
     target = torch.cat((torch.ones(rows // 2, device=DEV), torch.zeros(rows - rows // 2, device=DEV)))
     losses = []
     for step in range(1, steps + 1):
@@ -131,6 +132,7 @@ if __name__ == "__main__":
     ap.add_argument("--scale", type=int, default=14, help="2^scale vertices")
     ap.add_argument("--dim", type=int, default=64)
     ap.add_argument("--steps", type=int, default=200)
+    ap.add_argument("--bits", type=int, default=32, choices=(8, 32), help="of the optimiser's moments")
     args = ap.parse_args()
-    before, after, losses = train(args.scale, args.dim, args.steps)
+    before, after, losses = train(args.scale, args.dim, args.steps, bits=args.bits)
     print(f"held-out AUC {before:.3f} before, {after:.3f} after {args.steps} steps; loss {losses[0]:.3f} -> {losses[-1]:.3f}")

@@ -58,3 +58,17 @@ def test_a_head_of_any_type_takes_steps(dtype):
     want, bound = in_64_bits(head, x)
     within(head.score(x), want, bound, "score")  # the layers that keep nothing for a backward pass
     within(head.forward(x, head.copies).float(), want, bound, "logits")
+
+
+def test_moments_have_the_bits_that_were_asked_for():
+    """32, unless a caller chooses 8."""
+    from paper_2008_12336_amd.examples import link_head
+
+    p, g = torch.zeros(300, device=DEV), torch.ones(300, device=DEV)
+    for how, bits in ((dict(), 32), (dict(bits=32), 32), (dict(bits=8), 8)):
+        assert G.gosh_adamw_create([p], [g], **how).states[0].numel() == G.gosh_adamw_state_bytes(300, bits)
+        head = link_head.LinkHead(32, 64)
+        sizes = [v.numel() for v in head.params.values()]
+        assert [s.numel() for s in head.optimiser(**how).states] == [G.gosh_adamw_state_bytes(n, bits) for n in sizes]
+    before, after, losses = link_head.train(scale=10, dim=16, steps=3, rows=512, bits=8)
+    assert len(losses) == 3 and 0 <= before <= 1 and 0 <= after <= 1

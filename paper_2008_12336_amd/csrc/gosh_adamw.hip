@@ -275,6 +275,9 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(const Tensor *tensors
     } else {
       if (t.bits == 8) load_moments<8>(t, i, count, m, v);
       else load_moments<32>(t, i, count, m, v);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)  // what is not there, 0, times a block's NaN
+        if (e >= count) m[e] = v[e] = 0.f;
       Entries<To, kEach>::store(m_flat + t.flat + i, kEach, m);
       Entries<To, kEach>::store(v_flat + t.flat + i, kEach, v);
     }

@@ -1,0 +1,32 @@
+"""gosh_adamw_* as a program may use it beside test_gpu_adamw.py: moments that are not finite and are read out, states made on a busy
+stream, rates from the device with weight decay, empty tensors, steps that count themselves."""
+import math
+
+import pytest
+import torch
+
+import paper_2008_12336_amd as G
+from tests import step_model as S
+from tests.test_gpu_head import DEV, MARK, gen, within
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_zeros_between_moments_that_are_not_finite(bits, dtype):
+    sizes = [1, 127, 300, 128, 4097, 5]
+    ps, gs = ([torch.ones(n, device=DEV) for n in sizes] for _ in range(2))
+    for g in gs:
+        g[-1] = math.nan
+    opt = G.gosh_adamw_create(ps, gs, bits=bits)
+    G.gosh_adamw_step(opt, lr=1e-3, step=1)
+    m, v = (torch.full((G.gosh_adamw_entries(opt),), MARK, dtype=dtype, device=DEV) for _ in range(2))
+    G.gosh_adamw_save(opt, m, v)
+    at = 0
+    for n in sizes:
+        end = at + -(-n // 128) * 128
+        for x in (m, v):
+            assert torch.isnan(x[at + n - 1]) and (x[at + n:end] == 0).all(), n
+        at = end
+    assert at == m.numel()

@@ -690,7 +690,7 @@ typedef struct {
 uint64_t gosh_adamw_state_bytes(int64_t n, int32_t bits);
 
 /* An optimiser over `count` tensors (host array, read by the call): checks them and puts their addresses into device memory
- * of the current device (waits for the device).  The arrays stay the caller's and must live, where they are, as long as the
+ * of the current device (waits for the device: for what any of its streams was given before).  The arrays stay the caller's and must live, where they are, as long as the
  * optimiser is used.  GOSH_EINVAL also where anything that a step writes overlaps another tensor's arrays. */
 int gosh_adamw_create(const gosh_param *params, int32_t count, void **optimiser_out);
 void gosh_adamw_free(void *optimiser); /* waits for the device's work */

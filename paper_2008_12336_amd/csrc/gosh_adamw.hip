@@ -362,6 +362,8 @@ int create(const gosh_param *params, int32_t count, void **out) {
   }
   o->count = static_cast<int64_t>(chunks.size());
   GOSH_TRY_HIP(hipGetDevice(&o->device), "device of the optimiser");
+  // what other streams are still writing (states that were cleared on one of them) is there before a step on any stream
+  GOSH_TRY_HIP(hipDeviceSynchronize(), "what the optimiser's tensors wait for");
   if (o->count > 0) {
     const size_t at = padded(tensors.size() * sizeof(Tensor), 256);
     char *memory = nullptr;

@@ -30,3 +30,21 @@ def test_zeros_between_moments_that_are_not_finite(bits, dtype):
             assert torch.isnan(x[at + n - 1]) and (x[at + n:end] == 0).all(), n
         at = end
     assert at == m.numel()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_states_that_a_busy_stream_clears_are_there_for_a_step_on_another(bits):
+    n = 5000
+    p, g, long_ = gen(1)(n), gen(2)(n), torch.zeros(1 << 28, device=DEV)
+    q = p.clone()
+    want = G.gosh_adamw_create([q], [g], bits=bits)
+    G.gosh_adamw_step(want, lr=1e-2, step=1)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(60):  # 2 GB of traffic each, some 25 ms in all
+            long_.add_(1)
+        opt = G.gosh_adamw_create([p], [g], bits=bits)  # its states are cleared behind them
+    G.gosh_adamw_step(opt, lr=1e-2, step=1)
+    torch.cuda.synchronize()
+    assert torch.equal(p, q) and torch.equal(opt.states[0], want.states[0]) and opt.states[0].any()

@@ -869,11 +869,12 @@ def gosh_softmax_loss(logits: torch.Tensor, targets: torch.Tensor, loss: torch.T
 
 
 class AdamW:
-    """An optimiser of gosh_adamw_create.  Holds the tensors that it was made with (their memory must not be replaced), and
-    `states`, the uint8 tensors of its moments."""
+    """An optimiser of gosh_adamw_create.  Holds the tensors that it was made with (their memory must not be replaced),
+    `states`, the uint8 tensors of its moments, and `step`, the number of the last step that was taken with it: None where that is not
+    known, for moments that came from elsewhere and steps that the device counts."""
 
-    def __init__(self, handle, tensors, states):
-        self.handle, self._tensors, self.states = handle, tensors, states
+    def __init__(self, handle, tensors, states, step=0):
+        self.handle, self._tensors, self.states, self.step = handle, tensors, states, step
 
     def free(self) -> None:
         if self.handle:
@@ -916,6 +917,7 @@ def gosh_adamw_create(params, grads, bits=32, states=None, copies=None, weight_d
     count = len(params)
     each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * count  # noqa: E731
     bits, decay, copies = each(bits), each(weight_decay), each(copies)
+    taken = 0 if states is None else None
     if states is None:  # slices of one allocation
         sizes = [gosh_adamw_state_bytes(p.numel(), b) for p, b in zip(params, bits)]
         starts = [0]
@@ -941,7 +943,7 @@ def gosh_adamw_create(params, grads, bits=32, states=None, copies=None, weight_d
                               p.numel(), _TYPES[g.dtype], GOSH_BF16 if c is None else _TYPES[c.dtype], bits[i], decay[i])
     handle = C.c_void_p()
     _check(lib().gosh_adamw_create(array, count, C.byref(handle)))
-    return AdamW(handle.value, (params, grads, copies), states)
+    return AdamW(handle.value, (params, grads, copies), states, taken)
 
 
 def gosh_adamw_free(opt: AdamW) -> None:
@@ -956,13 +958,25 @@ def _device_scalar(t, name: str, dtype):
     return t.data_ptr()
 
 
-def gosh_adamw_step(opt: AdamW, lr: float = 0.0, step: int = 1, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+def gosh_adamw_step(opt: AdamW, lr: float = None, step: int = None, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                     lr_dev=None, scale=None, steps=None, stream=None) -> None:
-    """A step of all tensors, the step-th from 1 on.  Device tensors of one entry: lr_dev in place of lr, scale that gradients are
-    multiplied by (the step is left out where it is not finite), steps (int64) in place of `step`: how many were taken."""
+    """A step of all tensors, the step-th from 1 on; None: the one after opt.step, which a call with a number or without one sets (also
+    where the step is left out, and once for all replays where it is captured).  Device tensors of one entry: lr_dev in place of lr, scale
+    that gradients are multiplied by (the step is left out where it is not finite), steps (int64) in place of `step`: how many were taken."""
+    if lr is None:
+        if lr_dev is None:
+            raise TypeError("lr or lr_dev is needed")
+        lr = 0.0
+    if steps is not None:
+        step = 1
+    elif step is None:
+        if opt.step is None:
+            raise TypeError("step is needed: how many were taken is not known")
+        step = opt.step + 1
     options = gosh_adamw_options(lr, beta1, beta2, eps, step, _device_scalar(lr_dev, "lr_dev", torch.float32),
                                  _device_scalar(scale, "scale", torch.float32), _device_scalar(steps, "steps", torch.int64))
     _check(lib().gosh_adamw_step(opt.handle, options, _stream(stream)))
+    opt.step = step if steps is None else None  # the device counts
 
 
 def gosh_adamw_entries(opt: AdamW) -> int:
@@ -988,3 +1002,4 @@ def gosh_adamw_load(opt: AdamW, m: torch.Tensor, v: torch.Tensor, stream=None) -
     if m.dtype != torch.float32:
         raise TypeError("moments are loaded from float32")
     _check(lib().gosh_adamw_load(opt.handle, pm, pv, m.numel(), _stream(stream)))
+    opt.step = None

@@ -48,3 +48,40 @@ def test_states_that_a_busy_stream_clears_are_there_for_a_step_on_another(bits):
     G.gosh_adamw_step(opt, lr=1e-2, step=1)
     torch.cuda.synchronize()
     assert torch.equal(p, q) and torch.equal(opt.states[0], want.states[0]) and opt.states[0].any()
+
+
+def test_steps_that_nobody_numbers():
+    """They count themselves; where that cannot be, or without a rate, they are refused."""
+    rnd = gen(3)
+    p, g = rnd(700), rnd(700)
+    q = p.clone()
+    opt, other = (G.gosh_adamw_create([t], [g]) for t in (p, q))
+    for step in (1, 2, 3):
+        G.gosh_adamw_step(opt, lr=1e-2)
+        G.gosh_adamw_step(other, lr=1e-2, step=step)
+        assert torch.equal(p, q) and opt.step == step
+    G.gosh_adamw_step(opt, lr=1e-2, step=10)
+    G.gosh_adamw_step(opt, lr=1e-2)
+    for step in (10, 11):
+        G.gosh_adamw_step(other, lr=1e-2, step=step)
+    assert torch.equal(p, q) and opt.step == 11
+    before = p.clone()
+    with pytest.raises(TypeError, match="lr or lr_dev"):
+        G.gosh_adamw_step(opt)
+    with pytest.raises(TypeError, match="lr or lr_dev"):
+        G.gosh_adamw_step(opt, step=12)
+    m, v = (torch.ones(G.gosh_adamw_entries(opt), device=DEV) for _ in range(2))
+    G.gosh_adamw_load(opt, m, v)
+    given = G.gosh_adamw_create([q], [g], states=[torch.zeros(G.gosh_adamw_state_bytes(700, 32), dtype=torch.uint8, device=DEV)])
+    device = G.gosh_adamw_create([q], [g])
+    G.gosh_adamw_step(device, lr=0.0, steps=torch.zeros(1, dtype=torch.int64, device=DEV))
+    for o in (opt, given, device):
+        with pytest.raises(TypeError, match="step is needed"):
+            G.gosh_adamw_step(o, lr=1e-2)
+    assert torch.equal(p, before)
+    G.gosh_adamw_step(opt, lr=1e-2, step=5)
+    G.gosh_adamw_step(opt, lr=1e-2)
+    assert opt.step == 6
+    with pytest.raises(G.GoshError):  # a call that is refused counts no step
+        G.gosh_adamw_step(opt, lr=math.nan)
+    assert opt.step == 6

@@ -896,6 +896,8 @@ class AdamW:
 
 def _dense(t: torch.Tensor) -> bool:
     """No two entries at one place and no gaps between them."""
+    if t.numel() == 0:
+        return True
     at = 1
     for n, s in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n != 1), key=lambda v: v[1]):
         if s != at:

@@ -85,3 +85,11 @@ def test_steps_that_nobody_numbers():
     with pytest.raises(G.GoshError):  # a call that is refused counts no step
         G.gosh_adamw_step(opt, lr=math.nan)
     assert opt.step == 6
+
+
+def test_tensors_of_no_entries_beside_others():
+    p, g = torch.ones(9, device=DEV), torch.ones(9, device=DEV)
+    none = [torch.empty(s, device=DEV) for s in ((5, 0), (0, 5), (0,), (2, 0, 3))]
+    opt = G.gosh_adamw_create([none[0], p, *none[1:]], [torch.empty_like(none[0]), g, *map(torch.empty_like, none[1:])], bits=8)
+    G.gosh_adamw_step(opt, lr=0.5)
+    assert ((p - 0.5).abs() < 1e-6).all() and G.gosh_adamw_entries(opt) == 128

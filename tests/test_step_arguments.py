@@ -21,3 +21,10 @@ def test_exact_products_are_an_activation_that_the_calls_take():
     lib, m, f = G.lib(), mat(cols=128), fp8()
     for act in range(4):  # refused further on, for a w without rows
         refused(lib.gosh_linear_fp8(None, C.byref(f), C.byref(f), None, act | G.GOSH_FP8_EXACT, None, C.byref(m), None, None), "w: rows")
+
+
+@pytest.mark.parametrize("shape", [(0,), (5, 0), (0, 5), (3, 0, 4), (2, 3, 0)])
+def test_tensors_of_no_entries_have_no_gaps(shape):
+    assert G.binding._dense(torch.empty(shape))
+    if len(shape) > 1:
+        assert G.binding._dense(torch.empty(shape).transpose(0, 1))

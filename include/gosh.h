@@ -701,7 +701,7 @@ void gosh_adamw_free(void *optimiser); /* waits for the device's work */
  * from the moments as they are before they are put back into 8 bits.  t: step, from 1 on; or, where steps is not NULL (device memory),
  * *steps + 1, which the call leaves there.  lr_dev, scale: device floats in place of lr and of 1, or NULL.  Where *scale is
  * not finite nothing changes, *steps neither: a step with gradients that overflowed is left out.
- * 0 <= beta1, beta2 < 1, eps >= 0.
+ * 0 <= beta1, beta2 < 1, eps >= 0; lr and eps within the range of 32 bits (eps: 0, or 2^-149 or more).
  * Moments in 8 bits: the bits of a float below the third of its mantissa are cut off, after the addition of 20 bits
  * (i * 2654435769 + t * 1779033703 mod 2^32) / 2^12 (of the complement for v), i the entry's index: so that, over the steps,
  * the mean is right, and a v that shrinks by a thousandth of itself a step does not stay where it is.  A v over 0 does not

@@ -6,6 +6,7 @@
 // memory: 2^27 entries with 32-bit gradients and 8-bit moments (16 bytes each) 392 us, 5.5 TB/s; 50,000,017 with 16-bit gradients
 // and copies and 32-bit moments (28 bytes) 260 us, 5.4 TB/s; 192 tensors of 3,000,000 entries in all 11.8.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <memory>
 #include <new>
@@ -451,10 +452,11 @@ int gosh_adamw_step(void *optimiser, const gosh_adamw_options *options, void *hi
   using namespace gosh;
   if (options == nullptr) return fail(GOSH_EINVAL, "options is null");
   const gosh_adamw_options &q = *options;
-  if (!std::isfinite(q.lr)) return fail(GOSH_EINVAL, "lr = %g: must be a number", q.lr);
+  if (!(std::fabs(q.lr) <= FLT_MAX)) return fail(GOSH_EINVAL, "lr = %g: must be a number of 32 bits", q.lr);
   if (!(q.beta1 >= 0 && q.beta1 < 1) || !(q.beta2 >= 0 && q.beta2 < 1))
     return fail(GOSH_EINVAL, "beta1 = %g, beta2 = %g: must be in [0, 1)", q.beta1, q.beta2);
-  if (!(q.eps >= 0) || !std::isfinite(q.eps)) return fail(GOSH_EINVAL, "eps = %g: must be a number from 0 on", q.eps);
+  if (!(q.eps >= 0 && q.eps <= FLT_MAX) || (q.eps > 0 && static_cast<float>(q.eps) == 0.f))  // as 0 it would make 0 / 0 of no gradient
+    return fail(GOSH_EINVAL, "eps = %g: must be 0 or a number over it of 32 bits", q.eps);
   if (q.steps == nullptr && q.step < 1) return fail(GOSH_EINVAL, "step = %lld: the first is 1", (long long)q.step);
   if (int rc = check_optimiser(optimiser)) return rc;
   if (int rc = check_floats(q.lr_dev, 1, "lr_dev", true)) return rc;

@@ -28,3 +28,12 @@ def test_tensors_of_no_entries_have_no_gaps(shape):
     assert G.binding._dense(torch.empty(shape))
     if len(shape) > 1:
         assert G.binding._dense(torch.empty(shape).transpose(0, 1))
+
+
+@pytest.mark.parametrize("fields, text", [(dict(lr=1e39), "lr"), (dict(lr=-1e39), "lr"), (dict(eps=1e39), "eps"), (dict(eps=1e-46), "eps"),
+                                          (dict(eps=5e-324), "eps")])
+def test_rates_that_32_bits_do_not_hold(fields, text):
+    ok = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1)
+    refused(G.lib().gosh_adamw_step(None, C.byref(G.gosh_adamw_options(**{**ok, **fields})), None), text)
+    for fine in (dict(lr=3.4e38), dict(eps=0.0), dict(eps=1e-45), dict(lr=1e-300)):
+        refused(G.lib().gosh_adamw_step(None, C.byref(G.gosh_adamw_options(**{**ok, **fine})), None), "optimiser is null")

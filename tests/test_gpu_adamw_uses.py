@@ -93,3 +93,37 @@ def test_tensors_of_no_entries_beside_others():
     opt = G.gosh_adamw_create([none[0], p, *none[1:]], [torch.empty_like(none[0]), g, *map(torch.empty_like, none[1:])], bits=8)
     G.gosh_adamw_step(opt, lr=0.5)
     assert ((p - 0.5).abs() < 1e-6).all() and G.gosh_adamw_entries(opt) == 128
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_rates_from_the_device_with_weight_decay(bits, captured):
+    """Each step against 64 bits from the state before it, at the rate of that moment."""
+    rnd, sizes, decay, beta = gen(9), [5000, 33, 300], [0.1, 0.0, 0.3], dict(beta1=0.9, beta2=0.99)
+    ps, gs = ([rnd(n) for n in sizes] for _ in range(2))
+    opt = G.gosh_adamw_create(ps, gs, bits=bits, weight_decay=decay)
+    lr, steps = torch.full((1,), 1.0, device=DEV), torch.zeros(1, dtype=torch.int64, device=DEV)
+    flat = [torch.empty(G.gosh_adamw_entries(opt), device=DEV) for _ in range(2)]
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    if captured:
+        with torch.cuda.graph(graph):
+            G.gosh_adamw_step(opt, lr_dev=lr, steps=steps, **beta)
+    for t, rate in enumerate((0.25, 0.03125, 0.5), 1):
+        lr.fill_(rate)
+        for g in gs:
+            g.copy_(rnd(g.numel()))
+        G.gosh_adamw_save(opt, *flat)
+        before, m, v = ([x.double().clone() for x in xs] for xs in (ps, flat[:1], flat[1:]))
+        torch.cuda.synchronize()
+        if captured:
+            graph.replay()
+        else:
+            G.gosh_adamw_step(opt, lr_dev=lr, steps=steps, **beta)
+        torch.cuda.synchronize()
+        assert int(steps) == t
+        at = 0
+        for p, g, b, n, d in zip(ps, gs, before, sizes, decay):
+            args = (b, g.double(), m[0][at:at + n], v[0][at:at + n], t, rate, 0.9, 0.99, 1e-8, d)
+            within(p, S.adamw(*args)[0], S.adamw_bound(*args), f"step {t}, {n} parameters")
+            at += -(-n // 128) * 128

@@ -648,7 +648,8 @@ int gosh_linear_fp8(const gosh_mat *x, const gosh_fp8 *x8, const gosh_fp8 *w, co
  * NULL with GOSH_ACT_NONE.  act: GOSH_FP8_EXACT may be added.  xt: in x rows, x transposed, block_rows 1 (gosh_pack_fp8's qt); may be NULL if dw is.  wt: in x
  * out, w transposed, of either block_rows; may be NULL if dx is.  dx: rows x in, of dy's type; dw: out x in, of dy's type or
  * GOSH_F32; db: out floats.  dx or dw may be NULL, db too (db alone: gosh_linear_backward).  in, out <= GOSH_MAT_MAX_COLS;
- * with dw rows <= GOSH_FP8_MAX_LD.  With rows = 0 dw and db are zero.  dx must not overlap dy, z or wt.
+ * with dw rows <= GOSH_FP8_MAX_LD.  With rows = 0 dw and db are zero.  dx must not overlap dy, z, wt
+ * or xt, nor dw wt or xt.
  * workspace: as above, at least gosh_linear_fp8_backward_workspace bytes (0 for sizes that the call refuses). */
 int gosh_linear_fp8_backward(const gosh_mat *dy, const gosh_fp8 *xt, const gosh_fp8 *wt, const gosh_mat *z, int32_t act,
                              const gosh_mat *dx, const gosh_mat *dw, float *db, void *workspace, uint64_t workspace_bytes,
@@ -662,7 +663,7 @@ uint64_t gosh_linear_fp8_backward_workspace(int64_t rows, int32_t in, int32_t ou
  * targets: rows int32, or int64 with targets_are64 = 1.  A negative target is none: loss and gradient of the row are 0, as
  * they are for a row of weight 0 and for one all of whose logits are -infinity (which takes a class out).  A target of `classes` or more makes
  * both NaN, and so does a logit that is NaN or +infinity.  weight: rows floats, or NULL for 1.  loss: rows floats.
- * dlogits: as logits, may be logits; NULL: the loss alone.  One reading of the logits; 32 bits within. */
+ * dlogits: as logits; may be logits, but must not overlap it otherwise (GOSH_EINVAL); NULL: the loss alone.  One reading of the logits; 32 bits within. */
 int gosh_softmax_loss(const gosh_mat *logits, const void *targets, int32_t targets_are64, const float *weight, float scale,
                       float *loss, const gosh_mat *dlogits, void *hip_stream);
 

@@ -184,6 +184,22 @@ int loss_of(const LossArgs &a, hipStream_t st) {
   return fail(GOSH_EINVAL, "logits: cols = %d: too many", a.cols);
 }
 
+// Two matrices of one shape and type that are one, or have no entry in common.  (A row of one that lies on another row of the other
+// would be written before it is read.)
+bool same_or_apart(const gosh_mat &a, const gosh_mat &b) {
+  if (a.rows == 0) return true;
+  if (a.data == b.data) return a.ld == b.ld || a.rows == 1;
+  const bool a_first = reinterpret_cast<uintptr_t>(a.data) < reinterpret_cast<uintptr_t>(b.data);
+  const gosh_mat &low = a_first ? a : b, &high = a_first ? b : a;
+  const int64_t size = a.type == GOSH_F32 ? 4 : 2;
+  const uint64_t bytes = reinterpret_cast<uintptr_t>(high.data) - reinterpret_cast<uintptr_t>(low.data);
+  const int64_t span = (low.rows - 1) * low.ld + low.cols;
+  if (bytes >= static_cast<uint64_t>(span * size)) return true;
+  if (a.ld != b.ld && a.rows > 1) return false;
+  const int64_t entries = static_cast<int64_t>(bytes) / size, row = entries / low.ld, col = entries % low.ld;  // where high begins in low
+  return col >= low.cols && (row + 1 >= low.rows || low.ld - col >= low.cols);
+}
+
 }  // namespace
 }  // namespace gosh
 
@@ -196,6 +212,8 @@ int gosh_softmax_loss(const gosh_mat *logits, const void *targets, int32_t targe
   if (int rc = check_mat(dlogits, "dlogits", kOptional)) return rc;
   if (int rc = check_shape(dlogits, "dlogits", logits->rows, logits->cols)) return rc;
   if (int rc = check_type(dlogits, "dlogits", logits->type)) return rc;
+  if (dlogits != nullptr && !same_or_apart(*logits, *dlogits))
+    return fail(GOSH_EINVAL, "dlogits overlaps logits: it must be logits, or have no entry of it");
   if (targets_are64 != 0 && targets_are64 != 1) return fail(GOSH_EINVAL, "targets_are64 = %d: must be 0 or 1", targets_are64);
   const int64_t rows = logits->rows, size = targets_are64 ? 8 : 4;
   if (rows > 0) {

@@ -831,7 +831,7 @@ def gosh_unpack_fp8(q: PackedFp8, x: torch.Tensor, stream=None) -> None:
 def gosh_linear_fp8(x, x8: PackedFp8, w: PackedFp8, y: torch.Tensor, bias=None, act: int = GOSH_ACT_NONE, residual=None, z=None,
                     exact: bool = False, stream=None) -> None:
     """y = act(x8 w^T + bias) + residual, after x was put into x8; x None: x8 holds it.  z: a tensor or a Packed8 that
-    receives x8 w^T + bias.  exact: sums of exact products for bfloat16 results too, at half the rate."""
+    receives x8 w^T + bias.  exact: sums of exact products for bfloat16 results too, at half the rate or less."""
     v = _fp8(w, "w")
     if v is None:
         raise TypeError("w must be a PackedFp8")

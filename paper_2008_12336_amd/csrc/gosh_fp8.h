@@ -110,9 +110,9 @@ __device__ __forceinline__ S8 widened(uint32_t lo, uint32_t hi, float unit) {
 // take it where that rate counts: products in tiles.  It is more than half a step of f16 or f32, which are exact, and so is a layer
 // with ReLU, whose slope jumps with z's sign: 20,011 x 132 -> 517 had a z in 100,000 on the other side of 0, and db ended 0.4 % of its
 // rms off.
-// GOSH_FP8_EXACT asks for exact ones.  What the others do to a step of 65,536 x 1024 -> 2048, beside 64 bits: y 1.665e-3 of its norm off (half a step of bf16), with exact products
-// 1.664e-3; dx and dw 1.81e-3 and 1.66e-3, since a z that bf16 rounds to its other neighbour moves dz's 8 bits.  The forward product
-// takes 194 us, an exact one 321.
+// GOSH_FP8_EXACT asks for exact ones.  What the others do to a step of 65,536 x 1024 -> 2048, beside 64 bits: y is 1.665e-3 of its norm
+// off (half a step of bf16), with exact products 1.664e-3; dx and dw 1.81e-3 and 1.66e-3, since a z that bf16 rounds to its other
+// neighbour (1.2 % of them) moves dz's 8 bits.  The forward product takes 194 us, an exact one 321.
 template <bool Exact>
 __device__ __forceinline__ F16x fp8_mma(const U4 (&a)[2], const U4 (&b)[2], uint32_t byte_a, uint32_t byte_b, F16x c) {
   if constexpr (Exact) {
